@@ -68,7 +68,9 @@
  *    weights and the layer output.  Router logits, probabilities, block
  *    scores, combine weights and gaps are always float32; expert indices and
  *    schedules are int32.  Accumulation is float32 throughout.
- *  - Alignment: every pointer must be 16-byte aligned.
+ *  - Alignment: every pointer must be 16-byte aligned (in the attention
+ *    section at the end, int32 arrays, positions, turns and lse only as their
+ *    type needs).
  */
 #ifndef DMOE_H
 #define DMOE_H
@@ -536,6 +538,227 @@ dmoe_status dmoe_moe_forward(const void* x, const void* w_router, const float* b
                              int block_size, int H, int E, int I, int I_s, int k, dmoe_routing routing, float top_p,
                              int min_coreset, const dmoe_layer_buffers* buf, void* y, dmoe_dtype y_dt,
                              void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Attention of a decode step over a paged key/value cache
+ * ---------------------------------------------------------------------------
+ * What a transformer layer of the decode step does before its MoE layer: the
+ * new tokens of every sequence (a block of them in block diffusion, one in
+ * autoregressive decoding, a chunk of a prompt) are given their positions and
+ * stored in the cache (dmoe_cache_append), then attend to it
+ * (dmoe_attention_plan once per step, dmoe_attention per layer).  Pages are
+ * handed out, shared, freed and moved by dmoe_cache_update and
+ * dmoe_cache_compact.  All of it is enqueued on the stream without a look at
+ * device memory from the host, so a step can be captured in a HIP graph.
+ */
+
+/*
+ * Rotary positions.  With R = rot_dim and turns f_i per position, the pair i
+ * of a head at position p is turned by a = 2 pi p f_i:
+ *   y1 = scale (x1 cos a - x2 sin a),  y2 = scale (x2 cos a + x1 sin a);
+ * pairs are elements (2i, 2i + 1) if interleaved, else (i, i + R/2); elements
+ * from R on pass through unchanged.  Angles are formed in binary64 (p f_i is
+ * reduced to a fraction of a turn), so far positions lose nothing; the
+ * rotation is float32, rounded once to the storage type.
+ */
+typedef struct dmoe_rotary {
+  const double* turns;  /* [rot_dim/2] device: turns per position (dmoe_rope_turns) */
+  int rot_dim;          /* even, 2 <= rot_dim <= head_dim */
+  int interleaved;      /* pairs (2i, 2i+1) instead of (i, i + rot_dim/2) */
+  float scale;          /* 1, or what dmoe_rope_turns returned */
+} dmoe_rotary;
+
+typedef enum dmoe_rope_scaling {
+  DMOE_ROPE_NONE = 0,    /* f_i = base^(-2i/R) / 2 pi */
+  DMOE_ROPE_LINEAR = 1,  /* f_i / factor: positions interpolated */
+  DMOE_ROPE_NTK = 2,     /* base * factor^(R/(R-2)) in place of base (R > 2) */
+  DMOE_ROPE_YARN = 3     /* slow pairs (under one turn in `original` positions)
+                            interpolated, fast ones (over 32 turns) kept, a
+                            linear ramp over the pairs between; scale
+                            0.1 ln(factor) + 1 */
+} dmoe_rope_scaling;
+
+/*
+ * Turns per position of every pair into turns[rot_dim/2], a HOST array, and
+ * the factor of the rotated values into *scale (HOST).  Host only.
+ * Limits: rot_dim even and >= 2; base > 1; factor >= 1 (1 for
+ * DMOE_ROPE_NONE); original >= 1 (used by DMOE_ROPE_YARN).
+ */
+dmoe_status dmoe_rope_turns(int rot_dim, double base, dmoe_rope_scaling scaling, double factor, double original,
+                            double* turns, float* scale);
+
+/*
+ * Rotates x [T][n_heads][head_dim] at positions [T] (int32, any value) into
+ * out of the same type.  Rows are x_stride and out_stride elements apart
+ * (>= n_heads*head_dim, multiples of 16 bytes); out may be x itself with the
+ * same stride, else they must not overlap.  inverse: turned the other way
+ * (a -> -a, the same scale): the gradient with respect to x of a forward call,
+ * given the gradient of its output.
+ * Limits: T, n_heads >= 1; head_dim a multiple of 8 in [8, 256].
+ */
+dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, dmoe_dtype dt, int T, int n_heads,
+                      int head_dim, const int32_t* positions, dmoe_rotary rope, int inverse, void* stream);
+
+/*
+ * A paged cache: keys and values of n_layers layers in pages of page_tokens
+ * tokens, and the page table of n_slots sequences.  All arrays are device
+ * memory of the caller's (the struct itself is a HOST struct, read during the
+ * call).
+ *   k, v   [n_layers][n_pages][page], page = dmoe_cache_page_bytes bytes
+ *   table  [n_slots][max_pages] page ids; those of tokens from lens on are -1
+ *   lens   [n_slots] tokens of the sequence (its new ones included)
+ *   refs   [n_pages] sequences that hold the page; 0: free
+ * A page holds, per kv head and tile of 32 tokens, 16-byte chunks of c values
+ * (c = 8 for DMOE_BF16, 4 for DMOE_F32) in the order in which the attention's
+ * matrix instructions read them; dp is head_dim rounded up to 32, 64, 96, 128,
+ * 192 or 256, and what lies beyond head_dim is written as 0:
+ *   k page [n_kv_heads][page_tokens/32][dp/2c][2][32][c]:
+ *     token r of the tile, element 2c*s + c*h + e at [s][h][r][e]
+ *   v page [n_kv_heads][page_tokens/32][dp/32][16/c][2][32][c/4][4]:
+ *     token 2c*s + 8j + 4h + t of the tile, element 32b + d at [b][s][h][d][j][t]
+ * so that one matrix operand is one contiguous KiB.
+ * A page id outside [0, n_pages) where a token should be is never followed:
+ * nothing is stored there and no key is seen there.
+ * Limits: n_layers, n_pages, n_slots, max_pages >= 1; page_tokens a multiple
+ * of 32 up to 1024; n_kv_heads in [1, 256]; head_dim a multiple of 8 in [8, 256];
+ * n_slots <= 65536; max_pages * page_tokens < 2^31.
+ */
+typedef struct dmoe_cache {
+  void* k;
+  void* v;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs; /* used by dmoe_cache_update and dmoe_cache_compact only, else may be NULL */
+  dmoe_dtype dt;
+  int n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages;
+} dmoe_cache;
+
+/* Bytes of one page of keys (or of values) of one layer; 0 on invalid sizes. */
+size_t dmoe_cache_page_bytes(dmoe_dtype dt, int page_tokens, int n_kv_heads, int head_dim);
+
+/*
+ * The new tokens of a step.  Sequence i of n_seqs is slot slots[i] of the
+ * cache and its new tokens are rows q_offsets[i] .. q_offsets[i+1] of the
+ * step's tensors (n of them, 0 allowed); they are the LAST n tokens of the
+ * sequence: token j is at position lens[slot] - n + j.  A token whose
+ * position is negative (n > lens) has no place in the sequence: it is not
+ * stored, and attends to nothing.  Rows from q_offsets[n_seqs] on belong to
+ * nobody and are neither read nor written.
+ * q_offsets [n_seqs + 1] non-decreasing from 0, q_offsets[n_seqs] <= T;
+ * slots [n_seqs] in [0, n_slots), or NULL: sequence i is slot i.  Offsets and
+ * slots out of range are cut to the range (rows outside [0, T) are never
+ * touched, a sequence of a slot outside the table has no tokens).  max_new: an
+ * upper bound of every sequence's new tokens (more are ignored).
+ * Limits: 1 <= n_seqs <= 4096, n_slots if slots is NULL; T, max_new >= 1.
+ */
+typedef struct dmoe_batch {
+  const int32_t* q_offsets;
+  const int32_t* slots;
+  int n_seqs, T, max_new;
+} dmoe_batch;
+
+/*
+ * Stores the step's new keys and values [T][n_kv_heads][head_dim] in layer
+ * `layer` of the cache, the keys rotated to their positions, and rotates the
+ * queries [T][n_heads][head_dim] into q_out (which may be q with the same
+ * stride; q and q_out may both be NULL).  rope.turns NULL: nothing is
+ * rotated.  The positions' pages must have been given out (dmoe_cache_update)
+ * and must be the sequence's own.  Storing the same positions again (a block
+ * denoised over several steps) overwrites them.  Strides in elements between
+ * rows, multiples of 16 bytes.  Two sequences of a batch must not be the same
+ * slot.
+ * Limits: n_heads a multiple of n_kv_heads up to 1024 * n_kv_heads if q is set.
+ */
+dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch batch, const void* k, long k_stride,
+                              const void* v, long v_stride, const void* q, long q_stride, void* q_out,
+                              long q_out_stride, int n_heads, dmoe_rotary rope, void* stream);
+
+/*
+ * Attention of the step's new tokens over the cache.  Query head h reads kv
+ * head h / (n_heads / n_kv_heads).  The token at position p sees the keys
+ * below
+ *   lens                                  if mask_block == 0 (everything),
+ *   min(lens, (p / mask_block + 1) * mask_block)   if mask_block >= 1
+ * (1: causal; a block size: blocks of that many tokens see each other and all
+ * before them, as block diffusion does), and none if p < 0:
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j]) v[j],
+ *   lse[t][h] = log sum_j exp(scale * q[t][h] . k[j])      (float32, optional).
+ * A row that sees no key is 0 with lse -inf.  What a row does not see does not
+ * reach it, whatever it holds (NaN and infinities included).  Scores, softmax statistics and
+ * sums are float32; with DMOE_BF16 the probabilities are rounded to bf16
+ * (relative 2^-8, the matrix operand's type), their sum is not.
+ *
+ * dmoe_attention_plan cuts the step's rows and keys into work items: long
+ * sequences are split along their keys so that a few rows still use the whole
+ * device.  It reads q_offsets, slots and lens and is valid until they change;
+ * every layer of a step uses the same plan.
+ *   plan       int32 [dmoe_attention_plan_ints] device memory
+ *   workspace  dmoe_attention_workspace_size bytes; holds the partial results
+ *              of one dmoe_attention call at a time: calls that share it must
+ *              not overlap in time
+ * batch, n_heads and mask_block of dmoe_attention must be those of its plan.
+ * q, out: [T][n_heads][head_dim] of the cache's type, rows q_stride and
+ * out_stride elements apart (multiples of 16 bytes); out must not overlap q.
+ * lse: [T][n_heads].
+ * Limits: n_heads a multiple of n_kv_heads, n_heads / n_kv_heads <= 1024;
+ * scale > 0 and finite; T * n_heads < 2^31.
+ */
+size_t dmoe_attention_plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
+size_t dmoe_attention_workspace_size(dmoe_dtype dt, int n_seqs, int T, int max_new, int n_heads, int n_kv_heads,
+                                     int head_dim);
+dmoe_status dmoe_attention_plan(const dmoe_cache* cache, dmoe_batch batch, int n_heads, int mask_block, int32_t* plan,
+                                size_t plan_ints, void* stream);
+dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch, int n_heads, int mask_block,
+                           const void* q, long q_stride, float scale, const int32_t* plan, size_t plan_ints, void* out,
+                           long out_stride, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Gives out, shares, copies and frees pages.  Entry i of n makes sequence
+ * dst[i] hold the first keep[i] tokens of sequence src[i] and room for
+ * new_lens[i] tokens, as the tables stood before the call:
+ *   - full pages among the kept tokens are shared with src (refs + 1);
+ *   - a last page that is kept only in part becomes dst's own: it stays where
+ *     src is dst and nobody else holds it, else it is copied (all layers);
+ *   - the remaining pages are fresh ones: the lowest-numbered free pages, in
+ *     order of entries, then of tokens (pages that this call frees are free,
+ *     those it copies from are not);
+ *   - what dst held before is released (refs - 1).
+ * src NULL: src is dst.  keep NULL: min(lens[src], new_lens).  So new_lens
+ * alone grows and truncates, new_lens 0 frees, src another slot forks it.
+ * table, lens and refs are updated; a sequence's pages are its own from its
+ * last fork, or truncation, on: tokens before that are shared and must not be stored again.
+ * *status (device int32, may be NULL): 0, done; n > 0, n pages are lacking; -1,
+ * a slot out of range, a dst twice, a length or keep out of range, or a table
+ * entry out of range.  Unless 0, nothing was changed.
+ * dst, src, keep, new_lens: int32 [n] device arrays.  workspace:
+ * dmoe_cache_update_workspace_size bytes, not shared with a concurrent call.
+ * Limits: 1 <= n <= 4096; n * max_pages < 2^31.
+ */
+size_t dmoe_cache_update_workspace_size(int n, int max_pages, int n_pages);
+dmoe_status dmoe_cache_update(const dmoe_cache* cache, const int32_t* dst, const int32_t* src, const int32_t* keep,
+                              const int32_t* new_lens, int n, int32_t* status, void* workspace, size_t ws_bytes,
+                              void* stream);
+
+/*
+ * Brings the live pages together: with n_live pages in use, those numbered
+ * n_live and above move into the free ones below, lowest to lowest (all
+ * layers), so that the pool's end is free.  table_out [n_slots][max_pages] and
+ * refs_out [n_pages] receive the new table and counts and may be the cache's
+ * own arrays; ids outside [0, n_pages) are copied as they are.  counts (device
+ * int32 [2], optional): n_live and the pages moved.  Moved pages keep their
+ * old contents behind.  workspace: dmoe_cache_compact_workspace_size bytes.
+ */
+size_t dmoe_cache_compact_workspace_size(int n_pages);
+dmoe_status dmoe_cache_compact(const dmoe_cache* cache, int32_t* table_out, int32_t* refs_out, int32_t* counts,
+                               void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Copies page pairs[i][0] to page pairs[i][1] for i < n, keys and values of all layers.
+ * pairs: int32 [n][2] device array; a pair with an id out of range is left out.
+ * No page may be written twice, or written and read, in one call.
+ */
+dmoe_status dmoe_cache_copy_pages(const dmoe_cache* cache, const int32_t* pairs, int n, void* stream);
 
 /* Message describing the last non-OK status returned on this thread ("" if none). */
 const char* dmoe_last_error(void);

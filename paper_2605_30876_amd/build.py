@@ -21,13 +21,15 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdmoe.so")
 SOURCES = ["dmoe_api.cpp", "router.hip", "routing.hip", "topp.hip", "schedule.hip", "route.hip", "pack.hip",
-           "ffn.hip", "ffn_f32.hip", "combine.hip", "noalloc.hip", "layer.hip"]
+           "ffn.hip", "ffn_f32.hip", "combine.hip", "noalloc.hip", "layer.hip", "attn/attn_api.cpp", "attn/rope.hip",
+           "attn/pages.hip", "attn/plan.hip", "attn/attention_bf16.hip", "attn/attention_f32.hip"]
 ARCH = os.environ.get("DMOE_OFFLOAD_ARCH", "gfx950")
 
 
 def kernel_source_hash() -> str:
-    """Hash of the code of every kernel source (line comments and blank
-    lines left out): hardware-counter figures taken on other code are stale."""
+    """Hash of the code of every kernel source of the MoE layer (line comments
+    and blank lines left out): hardware-counter figures taken on other code
+    are stale."""
     import hashlib
     import re
 
@@ -64,7 +66,7 @@ def build(jobs: int = 0, debug: bool = False, verbose: bool = False) -> str:
     flags = _flags(debug)
 
     def compile_one(src):
-        obj = os.path.join(objdir, os.path.splitext(src)[0] + ".o")
+        obj = os.path.join(objdir, os.path.splitext(src)[0].replace("/", "_") + ".o")
         cmd = [cc, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj] + flags
         r = subprocess.run(cmd, capture_output=True, text=True)
         out = "\n".join(l for l in (r.stdout + r.stderr).splitlines()

@@ -1,0 +1,366 @@
+// Pages of the cache: handed out, shared, copied, freed and moved.
+//
+// The bookkeeping (page tables, counts) is a few thousand integers, so one
+// workgroup does it, in fixed order: the page ids it hands out depend on
+// nothing but the tables.  The page data are moved by a second launch over
+// the whole device, which reads the pairs and their number from memory.
+#include "cache.h"
+
+namespace dmoe {
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kMaxSlots = 65536;
+
+template <typename V>
+__device__ __forceinline__ V scan_exclusive(V v, V* waves, V* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  V x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const V y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  V base = 0, sum = 0;
+  for (int i = 0; i < kThreads / 64; ++i) {
+    base += i < wave ? waves[i] : 0;
+    sum += waves[i];
+  }
+  __syncthreads();
+  *total = sum;
+  return base + x - v;
+}
+
+// Counts are changed with atomics, which act in L2: they are read past L1,
+// and a barrier between the two waits for them.
+__device__ __forceinline__ int count_of(const int32_t* refs, int p) {
+  return __hip_atomic_load(refs + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void sync_counts() {
+  __threadfence();
+  __syncthreads();
+}
+
+// Page pairs to copy, in a workspace: their number, then from and to.
+struct PairList {
+  const int32_t* n;     // nullptr: all of `most`
+  const int32_t* from;  // pair i: from[i * step], to[i * step]
+  const int32_t* to;
+  int step, most;
+};
+
+// What an update keeps of every entry between its phases.
+struct Entry {
+  int dst, src, keep, len;
+  int full, count, had;  // shared pages; pages after and before the call
+  int part;              // page kept in part, or -1
+  int mine;              // the part stays where it is
+  int fresh;             // first of its pages in the list of free ones
+  int pad[2];
+};
+
+__global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const int32_t* dst, const int32_t* src, const int32_t* keep,
+                                                          const int32_t* new_lens, int n, int32_t* status, int32_t* n_pairs,
+                                                          Entry* entries, int32_t* from, int32_t* to, int32_t* rows,
+                                                          int32_t* owner, int32_t* free_list) {
+  __shared__ uint32_t seen[kMaxSlots / 32];
+  __shared__ int waves[kThreads / 64];
+  __shared__ int bad;
+  const int tid = threadIdx.x, mp = c.max_pages, pt = c.page_tokens;
+  auto pages = [&](int tokens) { return (tokens + pt - 1) / pt; };
+  for (int i = tid; i < (c.n_slots + 31) / 32; i += kThreads) seen[i] = 0;
+  if (tid == 0) {
+    bad = 0;
+    *n_pairs = 0;
+  }
+  __syncthreads();
+  bool ok = true;
+  for (int i = tid; i < n; i += kThreads) {
+    Entry e{};
+    e.dst = dst[i];
+    e.src = src ? src[i] : e.dst;
+    e.len = new_lens[i];
+    const bool in = e.dst >= 0 && e.dst < c.n_slots && e.src >= 0 && e.src < c.n_slots && e.len >= 0 && e.len <= mp * pt;
+    ok = ok && in;
+    if (in) {
+      ok = ok && !(atomicOr(&seen[e.dst / 32], 1u << (e.dst % 32)) >> (e.dst % 32) & 1);
+      const int held = c.lens[e.src], old = c.lens[e.dst];
+      e.keep = keep ? keep[i] : min(held, e.len);
+      ok = ok && held >= 0 && held <= mp * pt && old >= 0 && old <= mp * pt && e.keep >= 0 && e.keep <= min(held, e.len);
+      if (ok) {
+        e.full = e.keep / pt;
+        e.count = pages(e.len);
+        e.had = pages(old);
+        e.part = -1;
+        entries[i] = e;
+      }
+    }
+  }
+  if (!ok) atomicOr(&bad, 1);
+  __syncthreads();
+  if (bad) {
+    if (tid == 0 && status) *status = -1;
+    return;
+  }
+  // the pages kept, as the tables stand
+  const long cells = static_cast<long>(n) * mp;
+  for (long x = tid; x < cells; x += kThreads) {
+    const int i = static_cast<int>(x / mp), j = static_cast<int>(x - static_cast<long>(i) * mp);
+    const Entry& e = entries[i];
+    if (j < pages(e.keep)) {
+      const int p = c.table[static_cast<long>(e.src) * mp + j];
+      ok = ok && p >= 0 && p < c.n_pages;
+      rows[x] = p;
+    }
+    if (j < e.had) {
+      const int p = c.table[static_cast<long>(e.dst) * mp + j];
+      ok = ok && p >= 0 && p < c.n_pages;
+    }
+  }
+  if (!ok) atomicOr(&bad, 1);
+  __syncthreads();
+  if (bad) {
+    if (tid == 0 && status) *status = -1;
+    return;
+  }
+  auto count_shared = [&](int sign) {
+    for (long x = tid; x < cells; x += kThreads) {
+      const int i = static_cast<int>(x / mp), j = static_cast<int>(x - static_cast<long>(i) * mp);
+      const Entry& e = entries[i];
+      if (j < e.full) atomicAdd(&c.refs[rows[x]], sign);
+      if (j < e.had) atomicAdd(&c.refs[c.table[static_cast<long>(e.dst) * mp + j]], -sign);
+    }
+  };
+  count_shared(1);
+  for (int i = tid; i < n; i += kThreads) {
+    Entry& e = entries[i];
+    if (e.keep % pt) {
+      e.part = rows[static_cast<long>(i) * mp + e.full];
+      owner[e.part] = n;
+    }
+  }
+  sync_counts();
+  // a part that nobody holds any more stays with the first entry that had it
+  for (int i = tid; i < n; i += kThreads) {
+    const Entry& e = entries[i];
+    if (e.part >= 0 && e.src == e.dst && count_of(c.refs, e.part) == 0) atomicMin(&owner[e.part], i);
+  }
+  sync_counts();
+  // parts that stay are held by their entry, the others until they are copied
+  for (int i = tid; i < n; i += kThreads) {
+    Entry& e = entries[i];
+    if (e.part >= 0) {
+      e.mine = __hip_atomic_load(&owner[e.part], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
+      atomicAdd(&c.refs[e.part], 1);
+    }
+  }
+  sync_counts();
+  int need = 0, copies = 0;
+  for (int i0 = 0; i0 < n; i0 += kThreads) {
+    const int i = i0 + tid;
+    int fresh = 0, copied = 0;
+    if (i < n) {
+      const Entry& e = entries[i];
+      copied = e.part >= 0 && !e.mine;
+      fresh = e.count - e.full - (e.part >= 0) + copied;
+    }
+    int total, ctotal;
+    const int at = scan_exclusive(fresh, waves, &total);
+    const int cat = scan_exclusive(copied, waves, &ctotal);
+    if (i < n) {
+      entries[i].fresh = need + at;
+      if (copied) {
+        from[copies + cat] = entries[i].part;
+        to[copies + cat] = need + at;  // of the free list, below
+      }
+    }
+    need += total;
+    copies += ctotal;
+  }
+  // free pages, lowest first: a stretch of the counts per thread
+  const int stretch = (c.n_pages + kThreads - 1) / kThreads;
+  const int q0 = min(tid * stretch, c.n_pages), q1 = min(q0 + stretch, c.n_pages);
+  int zeros = 0;
+  for (int p = q0; p < q1; ++p) zeros += count_of(c.refs, p) == 0;
+  int total;
+  int at = scan_exclusive(zeros, waves, &total);
+  if (need > total) {  // as it was
+    count_shared(-1);
+    for (int i = tid; i < n; i += kThreads)
+      if (entries[i].part >= 0) atomicAdd(&c.refs[entries[i].part], -1);
+    if (tid == 0 && status) *status = need - total;
+    return;
+  }
+  for (int p = q0; p < q1 && at < need; ++p)
+    if (count_of(c.refs, p) == 0) free_list[at++] = p;
+  __syncthreads();
+  for (int i = tid; i < copies; i += kThreads) {
+    atomicAdd(&c.refs[from[i]], -1);
+    to[i] = free_list[to[i]];
+  }
+  for (int i = tid; i < need; i += kThreads) c.refs[free_list[i]] = 1;
+  for (long x = tid; x < cells; x += kThreads) {
+    const int i = static_cast<int>(x / mp), j = static_cast<int>(x - static_cast<long>(i) * mp);
+    const Entry& e = entries[i];
+    if (j >= max(e.count, e.had)) continue;
+    int p = -1;
+    if (j < e.full || (e.mine && j == e.full))
+      p = rows[x];
+    else if (j < e.count)
+      p = free_list[e.fresh + j - e.full - e.mine];
+    c.table[static_cast<long>(e.dst) * mp + j] = p;
+  }
+  for (int i = tid; i < n; i += kThreads) c.lens[entries[i].dst] = entries[i].len;
+  if (tid == 0) {
+    *n_pairs = copies;
+    if (status) *status = 0;
+  }
+}
+
+// Live pages from n_live on move into the holes below it, lowest to lowest.
+__global__ __launch_bounds__(kThreads) void compact_kernel(dmoe_cache c, int32_t* refs_out, int32_t* counts, int32_t* n_pairs,
+                                                           int32_t* from, int32_t* to, int32_t* moved) {
+  __shared__ int waves[kThreads / 64];
+  const int tid = threadIdx.x, n = c.n_pages;
+  const int stretch = (n + kThreads - 1) / kThreads;
+  const int q0 = min(tid * stretch, n), q1 = min(q0 + stretch, n);
+  int live = 0;
+  for (int p = q0; p < q1; ++p) live += c.refs[p] > 0;
+  int n_live;
+  scan_exclusive(live, waves, &n_live);
+  int holes = 0, movers = 0;
+  for (int p = q0; p < q1; ++p) {
+    const bool used = c.refs[p] > 0;
+    holes += !used && p < n_live;
+    movers += used && p >= n_live;
+  }
+  int n_holes, n_movers;  // equal
+  int h = scan_exclusive(holes, waves, &n_holes);
+  int m = scan_exclusive(movers, waves, &n_movers);
+  for (int p = q0; p < q1; ++p) {
+    const bool used = c.refs[p] > 0;
+    if (!used && p < n_live) to[h++] = p;
+    if (used && p >= n_live) from[m++] = p;
+    moved[p] = p;
+  }
+  __syncthreads();
+  for (int i = tid; i < n_movers; i += kThreads) moved[from[i]] = to[i];
+  // refs_out may be refs: holes take their movers' counts before those go
+  for (int p = q0; p < min(q1, n_live); ++p) {
+    const int r = c.refs[p];
+    if (r > 0) refs_out[p] = r;
+  }
+  for (int i = tid; i < n_movers; i += kThreads) refs_out[to[i]] = c.refs[from[i]];
+  __syncthreads();
+  for (int p = max(q0, n_live); p < q1; ++p) refs_out[p] = 0;
+  if (tid == 0) {
+    *n_pairs = n_movers;
+    if (counts) {
+      counts[0] = n_live;
+      counts[1] = n_movers;
+    }
+  }
+}
+
+constexpr int kCopyThreads = 256;
+constexpr int kUnroll = 4;
+constexpr long kUnit = kCopyThreads * kUnroll;  // 16-byte pieces of a unit: 16 KiB
+constexpr unsigned kCopyGrid = 4096;
+
+// Units of 16 KiB: (pair, layer, keys or values, part of the page).  With
+// `moved`, the table is rewritten too.
+__global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairList l, long page_len, const int32_t* moved,
+                                                            int32_t* table_out) {
+  const long gtid = static_cast<long>(blockIdx.x) * kCopyThreads + threadIdx.x;
+  if (moved) {
+    const long cells = static_cast<long>(c.n_slots) * c.max_pages;
+    for (long x = gtid; x < cells; x += static_cast<long>(gridDim.x) * kCopyThreads) {
+      const int p = c.table[x];
+      table_out[x] = p >= 0 && p < c.n_pages ? moved[p] : p;
+    }
+  }
+  const int n = l.n ? min(*l.n, l.most) : l.most;
+  const long per_page = (page_len + kUnit - 1) / kUnit;
+  const long units = n * static_cast<long>(c.n_layers) * 2 * per_page;
+  for (long u = blockIdx.x; u < units; u += gridDim.x) {
+    const long part = u % per_page, rest = u / per_page;
+    const int kv = static_cast<int>(rest % 2), layer = static_cast<int>(rest / 2 % c.n_layers), i = static_cast<int>(rest / 2 / c.n_layers);
+    const int a = l.from[static_cast<long>(i) * l.step], b = l.to[static_cast<long>(i) * l.step];
+    if (a < 0 || a >= c.n_pages || b < 0 || b >= c.n_pages) continue;
+    uint4* pool = static_cast<uint4*>(kv ? c.v : c.k) + static_cast<long>(layer) * c.n_pages * page_len;
+    const uint4* s = pool + a * page_len + part * kUnit;
+    uint4* d = pool + b * page_len + part * kUnit;
+    const long len = min(kUnit, page_len - part * kUnit);
+    uint4 x[kUnroll];
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j)
+      if (threadIdx.x + j * kCopyThreads < len) x[j] = s[threadIdx.x + j * kCopyThreads];
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j)
+      if (threadIdx.x + j * kCopyThreads < len) d[threadIdx.x + j * kCopyThreads] = x[j];
+  }
+}
+
+hipError_t copy_pages(const dmoe_cache& c, const PairList& l, const int32_t* moved, int32_t* table_out, hipStream_t s) {
+  const long page_len = page_elems(c.page_tokens, c.n_kv_heads, c.head_dim) * static_cast<long>(dtype_bytes(c.dt)) / 16;
+  const long units = l.most * static_cast<long>(c.n_layers) * 2 * ((page_len + kUnit - 1) / kUnit);
+  const unsigned grid = units < static_cast<long>(kCopyGrid) ? static_cast<unsigned>(units) : kCopyGrid;
+  copy_kernel<<<grid, kCopyThreads, 0, s>>>(c, l, page_len, moved, table_out);
+  return hipGetLastError();
+}
+
+size_t align16(size_t b) { return (b + 15) & ~static_cast<size_t>(15); }
+
+}  // namespace
+
+// Workspace: pairs' number | entries | from | to | rows | owner | free list.
+size_t update_workspace_bytes(long n, long max_pages, long n_pages) {
+  const long most = n * max_pages < n_pages ? n * max_pages : n_pages;  // pages handed out
+  return 16 + align16(n * sizeof(Entry)) + 2 * align16(n * 4) + align16(n * max_pages * 4) + align16(n_pages * 4) + align16(most * 4);
+}
+
+hipError_t launch_update(const dmoe_cache& c, const int32_t* dst, const int32_t* src, const int32_t* keep,
+                         const int32_t* new_lens, int n, int32_t* status, void* ws, hipStream_t s) {
+  char* at = static_cast<char*>(ws);
+  auto take = [&](size_t bytes) {
+    char* p = at;
+    at += align16(bytes);
+    return reinterpret_cast<int32_t*>(p);
+  };
+  int32_t* n_pairs = take(16);
+  Entry* entries = reinterpret_cast<Entry*>(take(n * sizeof(Entry)));
+  int32_t* from = take(n * 4l);
+  int32_t* to = take(n * 4l);
+  int32_t* rows = take(static_cast<long>(n) * c.max_pages * 4);
+  int32_t* owner = take(c.n_pages * 4l);
+  int32_t* free_list = take(0);
+  update_kernel<<<1, kThreads, 0, s>>>(c, dst, src, keep, new_lens, n, status, n_pairs, entries, from, to, rows, owner, free_list);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  return copy_pages(c, PairList{n_pairs, from, to, 1, n}, nullptr, nullptr, s);
+}
+
+// Workspace: pairs' number | from | to | moved.
+size_t compact_workspace_bytes(long n_pages) { return 16 + 3 * align16(n_pages * 4); }
+
+hipError_t launch_compact(const dmoe_cache& c, int32_t* table_out, int32_t* refs_out, int32_t* counts, void* ws,
+                          hipStream_t s) {
+  int32_t* n_pairs = static_cast<int32_t*>(ws);
+  const size_t step = align16(c.n_pages * 4l) / 4;
+  int32_t* from = n_pairs + 4;
+  int32_t* to = from + step;
+  int32_t* moved = to + step;
+  compact_kernel<<<1, kThreads, 0, s>>>(c, refs_out, counts, n_pairs, from, to, moved);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  return copy_pages(c, PairList{n_pairs, from, to, 1, c.n_pages}, moved, table_out, s);
+}
+
+hipError_t launch_copy_pages(const dmoe_cache& c, const int32_t* pairs, int n, hipStream_t s) {
+  return copy_pages(c, PairList{nullptr, pairs, pairs + 1, 2, n}, nullptr, nullptr, s);
+}
+
+}  // namespace dmoe

@@ -1,0 +1,161 @@
+// The attention's work items, made on the device: a step's lengths never
+// visit the host, and every layer of the step uses the one plan.
+#include "cache.h"
+
+namespace dmoe {
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kMaxSeqs = 4096;
+constexpr int kSplitWorkgroups = 512;  // items that splitting aims at, all kv heads together: two per CU
+constexpr int kMinTiles = 4;           // key tiles of an item at least: one per wave
+
+// Exclusive prefix sums over the workgroup's threads; *total is their sum.
+template <typename V>
+__device__ __forceinline__ V scan_exclusive(V v, V* waves, V* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  V x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const V y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  V base = 0, sum = 0;
+  for (int i = 0; i < kThreads / 64; ++i) {
+    base += i < wave ? waves[i] : 0;
+    sum += waves[i];
+  }
+  __syncthreads();
+  *total = sum;
+  return base + x - v;
+}
+
+// Largest i with a[i] <= x, for a[0] = 0 <= x < a[n].
+__device__ __forceinline__ int find(const int* a, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// A row tile's sequence and its key tiles.
+struct Tile {
+  Seq q;
+  int first, rows, kt;
+};
+
+__device__ __forceinline__ Tile load_tile(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
+                                          const int* tiles, int t) {
+  Tile r;
+  const int i = find(tiles, b.n_seqs, t);
+  r.q = load_seq(c, b, i);
+  r.rows = r.q.n * sh.group;
+  r.first = (t - tiles[i]) * sh.tile_rows;
+  const int last = min(r.first + sh.tile_rows, r.rows) - 1;
+  r.kt = (visible_end(r.q.pos0 + last / sh.group, r.q.len, mask_block) + kTileTokens - 1) / kTileTokens;
+  return r;
+}
+
+__global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch b, AttnShape sh, int mask_block, int32_t* plan) {
+  __shared__ int tiles[kMaxSeqs + 1];  // row tiles before each sequence
+  __shared__ int items[kThreads + 1];  // items before each row tile of a pass
+  __shared__ int parts[kThreads];
+  __shared__ Tile tile[kThreads];
+  __shared__ int iwaves[kThreads / 64];
+  __shared__ long lwaves[kThreads / 64];
+  const int tid = threadIdx.x;
+  int n_tiles = 0;
+  for (int i0 = 0; i0 < b.n_seqs; i0 += kThreads) {
+    const int i = i0 + tid;
+    int n = 0;
+    if (i < b.n_seqs) n = static_cast<int>((static_cast<long>(load_seq(c, b, i).n) * sh.group + sh.tile_rows - 1) / sh.tile_rows);
+    int total;
+    const int at = scan_exclusive(n, iwaves, &total);
+    if (i < b.n_seqs) tiles[i] = n_tiles + at;
+    n_tiles += total;
+  }
+  // offsets that break their contract could make more row tiles than the arrays hold
+  n_tiles = min(n_tiles, static_cast<int>(sh.max_tiles));
+  if (tid == 0) tiles[b.n_seqs] = n_tiles;
+  __syncthreads();
+
+  long keys = 0;
+  for (int t = tid; t < n_tiles; t += kThreads) keys += load_tile(c, b, sh, mask_block, tiles, t).kt;
+  long all;
+  scan_exclusive(keys, lwaves, &all);
+  const long split = sh.split_items;
+  const int chunk = static_cast<int>(max(static_cast<long>(kMinTiles), (all + split - 1) / split));
+
+  AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
+  AttnItem* out = reinterpret_cast<AttnItem*>(head + 1);
+  AttnMerge* merges = reinterpret_cast<AttnMerge*>(out + sh.max_items());
+  int n_items = 0, n_parts = 0, n_merges = 0;
+  // longest rows first under a causal mask: the last tiles see the most keys
+  for (int t0 = 0; t0 < n_tiles; t0 += kThreads) {
+    const int t = n_tiles - 1 - (t0 + tid);
+    int pieces = 0;
+    if (t >= 0) {
+      tile[tid] = load_tile(c, b, sh, mask_block, tiles, t);
+      pieces = max(1, (tile[tid].kt + chunk - 1) / chunk);
+    }
+    int total, ptotal, mtotal;
+    const int at = scan_exclusive(pieces, iwaves, &total);
+    const int pat = scan_exclusive(pieces > 1 ? pieces : 0, iwaves, &ptotal);
+    const int mat = scan_exclusive(pieces > 1 ? 1 : 0, iwaves, &mtotal);
+    items[tid] = at;
+    parts[tid] = pieces > 1 ? n_parts + pat : -1;
+    if (pieces > 1) {
+      const Tile& r = tile[tid];
+      merges[n_merges + mat] = AttnMerge{r.q.row0, r.first, r.rows, n_parts + pat, pieces, {0, 0, 0}};
+    }
+    if (tid == 0) items[kThreads] = total;
+    __syncthreads();
+    for (int x = tid; x < total; x += kThreads) {
+      const int j = find(items, kThreads, x);
+      const Tile& r = tile[j];
+      const int p = x - items[j], n = max(1, (r.kt + chunk - 1) / chunk);
+      AttnItem it{r.q.slot, r.q.row0, r.q.n, r.q.len, r.first, r.rows, 0, 0, parts[j] < 0 ? -1 : parts[j] + p, {0, 0, 0}};
+      it.kt0 = static_cast<int>(static_cast<long>(r.kt) * p / n);
+      it.kt1 = static_cast<int>(static_cast<long>(r.kt) * (p + 1) / n);
+      out[n_items + x] = it;
+    }
+    n_items += total;
+    n_parts += ptotal;
+    n_merges += mtotal;
+    __syncthreads();
+  }
+  if (tid == 0) {
+    head->n_items = n_items;
+    head->n_merges = n_merges;
+  }
+}
+
+}  // namespace
+
+AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
+  AttnShape s;
+  s.group = n_heads / n_kv_heads;
+  const long most = static_cast<long>(max_new < T ? max_new : T) * s.group;
+  s.tile_rows = most <= 32 ? 32 : 128;
+  const long by_seq = n_seqs * ((most + s.tile_rows - 1) / s.tile_rows);
+  const long by_rows = static_cast<long>(T) * s.group / s.tile_rows + n_seqs;
+  s.max_tiles = by_seq < by_rows ? by_seq : by_rows;
+  s.split_items = kSplitWorkgroups / n_kv_heads > 1 ? kSplitWorkgroups / n_kv_heads : 1;
+  return s;
+}
+
+hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
+                                 int32_t* plan, hipStream_t s) {
+  plan_kernel<<<1, kThreads, 0, s>>>(c, b, sh, mask_block, plan);
+  return hipGetLastError();
+}
+
+}  // namespace dmoe

@@ -1,57 +1,17 @@
 // C ABI of libdmoe: argument validation on the host, then the kernel
 // launchers.  Validation touches no GPU state, so every error path can be
 // exercised on a machine without a GPU.
-#include <cstdarg>
-#include <cstdio>
-#include <string>
-
-#include "dmoe_common.h"
+#include "host/checks.h"
 
 namespace {
 
-thread_local std::string g_last_error;
+using namespace dmoe::host;
 
-dmoe_status fail(dmoe_status st, const char* fn, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  g_last_error = std::string(fn) + ": " + buf;
-  return st;
-}
-
-dmoe_status ok() {
-  g_last_error.clear();
-  return DMOE_OK;
-}
-
-dmoe_status hip_status(hipError_t err, const char* fn) {
-  if (err == hipSuccess) return ok();
-  return fail(DMOE_ERR_HIP, fn, "kernel launch failed: %s", hipGetErrorString(err));
-}
-
-bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-bool valid_dtype(dmoe_dtype dt) { return dt == DMOE_F32 || dt == DMOE_BF16; }
 bool valid_slot_format(dmoe_slot_format f) { return f == DMOE_SLOT_F32 || f == DMOE_SLOT_F16S; }
 
 constexpr int kMaxE = 4096;
 constexpr int kMaxScheduleE = 512;
 constexpr int kMaxK = 64;
-constexpr long kIntLimit = 0x7fffffffL;
-
-// Name of the entry point in error messages.
-#define DMOE_FN __func__
-#define REQUIRE(cond, ...)                                  \
-  do {                                                      \
-    if (!(cond)) return fail(DMOE_ERR_INVALID_ARG, DMOE_FN, __VA_ARGS__); \
-  } while (0)
-#define SUPPORT(cond, ...)                                  \
-  do {                                                      \
-    if (!(cond)) return fail(DMOE_ERR_UNSUPPORTED, DMOE_FN, __VA_ARGS__); \
-  } while (0)
-#define ALIGNED(p) REQUIRE(!misaligned(p), #p " is not 16-byte aligned")
 
 }  // namespace
 

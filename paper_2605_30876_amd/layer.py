@@ -243,7 +243,8 @@ class MoELayer:
         return [rows[b, :n].tolist() for b, n in enumerate(sizes)]
 
 
-def decode_step(layers: list, weights: list, xs: list, routing: str = "block", stream=None) -> torch.Tensor:
+def decode_step(layers: list, weights: list, xs: list, routing: str = "block", stream=None,
+                attention: list | None = None) -> torch.Tensor:
     """The MoE layers of one decode step, chained: layer l runs on xs[l], and
     the step's input plus layer l's output, rounded once to the storage
     type, is layer l+1's input xs[l+1].  Each layer thus waits for its
@@ -257,9 +258,21 @@ def decode_step(layers: list, weights: list, xs: list, routing: str = "block", s
     weights, ``xs`` len(layers) preallocated [T, H] tensors of the storage
     type with xs[0] the step's input.  Returns the last layer's output y.
     Each layer's call writes the next layer's input itself (the add is
-    fused into its last kernel), so the step runs in libdmoe only."""
+    fused into its last kernel), so the step runs in libdmoe only.
+
+    ``attention``: one :class:`.attention.AttentionLayer` per layer.  Layer l
+    then runs on xs[l] plus its attention over the cache (whose keys and
+    values it stores first); their batch must have been begun, and
+    the step plans it once, before its first layer."""
+    if attention is not None:
+        if len(attention) != len(layers):
+            raise ValueError(f"{len(attention)} attention layers for {len(layers)} layers")
+        for i, a in enumerate(attention):
+            if all(a.att is not b.att for b in attention[:i]):
+                a.att.plan(stream)
     y = None
     L = len(layers)
     for l, (m, w) in enumerate(zip(layers, weights)):
-        y = m.forward(xs[l], w, routing, stream, residual=(xs[0], xs[l + 1]) if l + 1 < L else None)
+        x = xs[l] if attention is None else attention[l](xs[l], stream)
+        y = m.forward(x, w, routing, stream, residual=(xs[0], xs[l + 1]) if l + 1 < L else None)
     return y

@@ -35,7 +35,10 @@ EXPORTS = ("dmoe_router_workspace_size", "dmoe_router_logits", "dmoe_block_aggre
            "dmoe_route_token", "dmoe_route_topp", "dmoe_pack_activations", "dmoe_pack_expert_weights", "dmoe_ffn_workspace_size",
            "dmoe_slot_out_bytes", "dmoe_expert_ffn", "dmoe_expert_ffn_noalloc", "dmoe_shared_ffn_workspace_size", "dmoe_shared_expert_ffn", "dmoe_combine",
            "dmoe_moe_forward_workspace_size", "dmoe_moe_forward_fused", "dmoe_moe_forward", "dmoe_last_error",
-           "dmoe_version")
+           "dmoe_version", "dmoe_rope_turns", "dmoe_rope", "dmoe_cache_page_bytes", "dmoe_cache_append",
+           "dmoe_attention_plan_ints", "dmoe_attention_workspace_size", "dmoe_attention_plan", "dmoe_attention",
+           "dmoe_cache_update_workspace_size", "dmoe_cache_update", "dmoe_cache_compact_workspace_size",
+           "dmoe_cache_compact", "dmoe_cache_copy_pages")
 
 
 class DmoeError(RuntimeError):
@@ -68,9 +71,33 @@ class dmoe_layer_buffers(ctypes.Structure):
                 ("res_in", ctypes.c_void_p), ("res_out", ctypes.c_void_p)]
 
 
+DMOE_ROPE_NONE, DMOE_ROPE_LINEAR, DMOE_ROPE_NTK, DMOE_ROPE_YARN = 0, 1, 2, 3
+ROPE_SCALING = {"none": DMOE_ROPE_NONE, "linear": DMOE_ROPE_LINEAR, "ntk": DMOE_ROPE_NTK, "yarn": DMOE_ROPE_YARN}
+
+
+class dmoe_rotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("scale", ctypes.c_float)]
+
+
+class dmoe_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("dt", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("page_tokens", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("n_slots", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+
+class dmoe_batch(ctypes.Structure):
+    _fields_ = [("q_offsets", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("n_seqs", ctypes.c_int), ("T", ctypes.c_int),
+                ("max_new", ctypes.c_int)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
+_L = ctypes.c_long
 _S = ctypes.c_size_t
+_D = ctypes.c_double
+_CACHE = ctypes.POINTER(dmoe_cache)
 _SIGS = {
     "dmoe_router_workspace_size": ([_I, _I, _I, _I], _S),
     "dmoe_router_logits": ([_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _S, _P], _I),
@@ -98,6 +125,19 @@ _SIGS = {
     "dmoe_moe_forward_fused": ([_I] * 9, _I),
     "dmoe_moe_forward": ([_P] * 7 + [_I] * 8 + [_I, ctypes.c_float, _I, ctypes.POINTER(dmoe_layer_buffers), _P, _I, _P],
                          _I),
+    "dmoe_rope_turns": ([_I, _D, _I, _D, _D, _P, ctypes.POINTER(ctypes.c_float)], _I),
+    "dmoe_rope": ([_P, _L, _P, _L, _I, _I, _I, _I, _P, dmoe_rotary, _I, _P], _I),
+    "dmoe_cache_page_bytes": ([_I] * 4, _S),
+    "dmoe_cache_append": ([_CACHE, _I, dmoe_batch] + [_P, _L] * 4 + [_I, dmoe_rotary, _P], _I),
+    "dmoe_attention_plan_ints": ([_I] * 5, _S),
+    "dmoe_attention_workspace_size": ([_I] * 7, _S),
+    "dmoe_attention_plan": ([_CACHE, dmoe_batch, _I, _I, _P, _S, _P], _I),
+    "dmoe_attention": ([_CACHE, _I, dmoe_batch, _I, _I, _P, _L, ctypes.c_float, _P, _S, _P, _L, _P, _P, _S, _P], _I),
+    "dmoe_cache_update_workspace_size": ([_I] * 3, _S),
+    "dmoe_cache_update": ([_CACHE, _P, _P, _P, _P, _I, _P, _P, _S, _P], _I),
+    "dmoe_cache_compact_workspace_size": ([_I], _S),
+    "dmoe_cache_compact": ([_CACHE, _P, _P, _P, _P, _S, _P], _I),
+    "dmoe_cache_copy_pages": ([_CACHE, _P, _I, _P], _I),
     "dmoe_last_error": ([], ctypes.c_char_p),
     "dmoe_version": ([], ctypes.c_char_p),
 }
@@ -343,6 +383,79 @@ def dmoe_moe_forward(x, w_router, bias, w13, w2, ws13, ws2, n_blocks, block_size
                                    dtype_code(x), n_blocks, block_size, H, E, I, I_s, k, ROUTING[routing],
                                    float(top_p), min_coreset, ctypes.byref(buf), ptr(y), dtype_code(y),
                                    stream_handle(stream)))
+
+
+def _row_stride(t) -> int:
+    return 0 if t is None else t.stride(0)
+
+
+NO_ROTATION = dmoe_rotary(None, 0, 0, 1.0)
+
+
+def dmoe_rope_turns(rot_dim, base, scaling: str, factor, original) -> tuple:
+    """Turns per position of every pair (a list of rot_dim/2 floats) and the factor of the rotated values."""
+    turns = (ctypes.c_double * max(rot_dim // 2, 1))()
+    scale = ctypes.c_float()
+    _check(load().dmoe_rope_turns(rot_dim, float(base), ROPE_SCALING[scaling], float(factor), float(original),
+                                  ctypes.cast(turns, ctypes.c_void_p), ctypes.byref(scale)))
+    return list(turns)[:rot_dim // 2], scale.value
+
+
+def dmoe_rope(x, out, T, n_heads, head_dim, positions, rope: dmoe_rotary, inverse=False, stream=None):
+    _check(load().dmoe_rope(ptr(x), _row_stride(x), ptr(out), _row_stride(out), dtype_code(x), T, n_heads, head_dim,
+                            ptr(positions), rope, int(inverse), stream_handle(stream)))
+
+
+def dmoe_cache_page_bytes(dt, page_tokens, n_kv_heads, head_dim) -> int:
+    return int(load().dmoe_cache_page_bytes(dt, page_tokens, n_kv_heads, head_dim))
+
+
+def dmoe_cache_append(cache: dmoe_cache, layer, batch: dmoe_batch, k, v, q, q_out, n_heads,
+                      rope: dmoe_rotary | None = None, stream=None):
+    _check(load().dmoe_cache_append(cache, layer, batch, ptr(k), _row_stride(k), ptr(v), _row_stride(v), ptr(q),
+                                    _row_stride(q), ptr(q_out), _row_stride(q_out), n_heads,
+                                    NO_ROTATION if rope is None else rope, stream_handle(stream)))
+
+
+def dmoe_attention_plan_ints(n_seqs, T, max_new, n_heads, n_kv_heads) -> int:
+    return int(load().dmoe_attention_plan_ints(n_seqs, T, max_new, n_heads, n_kv_heads))
+
+
+def dmoe_attention_workspace_size(dt, n_seqs, T, max_new, n_heads, n_kv_heads, head_dim) -> int:
+    return int(load().dmoe_attention_workspace_size(dt, n_seqs, T, max_new, n_heads, n_kv_heads, head_dim))
+
+
+def dmoe_attention_plan(cache: dmoe_cache, batch: dmoe_batch, n_heads, mask_block, plan, stream=None):
+    _check(load().dmoe_attention_plan(cache, batch, n_heads, mask_block, ptr(plan), plan.numel(), stream_handle(stream)))
+
+
+def dmoe_attention(cache: dmoe_cache, layer, batch: dmoe_batch, n_heads, mask_block, q, scale, plan, out, lse, workspace,
+                   stream=None):
+    _check(load().dmoe_attention(cache, layer, batch, n_heads, mask_block, ptr(q), _row_stride(q), float(scale), ptr(plan),
+                                 plan.numel(), ptr(out), _row_stride(out), ptr(lse), ptr(workspace), _nbytes(workspace),
+                                 stream_handle(stream)))
+
+
+def dmoe_cache_update_workspace_size(n, max_pages, n_pages) -> int:
+    return int(load().dmoe_cache_update_workspace_size(n, max_pages, n_pages))
+
+
+def dmoe_cache_update(cache: dmoe_cache, dst, src, keep, new_lens, n, status, workspace, stream=None):
+    _check(load().dmoe_cache_update(cache, ptr(dst), ptr(src), ptr(keep), ptr(new_lens), n, ptr(status), ptr(workspace),
+                                    _nbytes(workspace), stream_handle(stream)))
+
+
+def dmoe_cache_compact_workspace_size(n_pages) -> int:
+    return int(load().dmoe_cache_compact_workspace_size(n_pages))
+
+
+def dmoe_cache_compact(cache: dmoe_cache, table_out, refs_out, counts, workspace, stream=None):
+    _check(load().dmoe_cache_compact(cache, ptr(table_out), ptr(refs_out), ptr(counts), ptr(workspace), _nbytes(workspace),
+                                     stream_handle(stream)))
+
+
+def dmoe_cache_copy_pages(cache: dmoe_cache, pairs, n, stream=None):
+    _check(load().dmoe_cache_copy_pages(cache, ptr(pairs), n, stream_handle(stream)))
 
 
 def dmoe_version() -> str:

@@ -1,0 +1,301 @@
+"""Attention over the paged cache against the 64-bit definition: head layouts
+and types, lengths from nothing to many key tiles, masks that leave rows
+empty, what lies in masked places, strides, other streams, graphs, and pages
+far into a large pool.  Marked ``gpu``."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as R
+from paper_2605_30876_amd import lib
+from paper_2605_30876_amd.attention import BlockAttention, PagedCache
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+class Setup:
+    """A batch over a cache whose unused places hold NaN, pages in random order."""
+
+    def __init__(self, dtype, heads, kv_heads, dim, page, lens, new, mask, seed=0, layers=1, extra_rows=2, slack=3, scale=None):
+        g = torch.Generator().manual_seed(seed)
+        self.dtype, self.dim, self.lens, self.new, self.mask = dtype, dim, lens, new, mask
+        n = len(lens)
+        held = [-(-x // page) for x in lens]
+        pages = sum(held) + slack
+        ids = torch.randperm(pages, generator=g).tolist()
+        slots = torch.randperm(n + 2, generator=g)[:n].tolist()
+        width = max(held + [0]) + 1
+        table = torch.full((n + 2, width), -1, dtype=torch.int32)
+        all_lens = torch.full((n + 2,), 3, dtype=torch.int32)  # other slots: of no concern
+        at = 0
+        for s, h, m in zip(slots, held, lens):
+            table[s, :h] = torch.tensor(ids[at:at + h], dtype=torch.int32)
+            all_lens[s] = m
+            at += h
+        elems = page * kv_heads * R.padded(dim)
+        self.kpool = torch.full((layers, pages * elems), float("nan"), dtype=dtype)
+        self.vpool = torch.full((layers, pages * elems), float("nan"), dtype=dtype)
+        self.k = [torch.randn(layers, m, kv_heads, dim, generator=g).to(dtype) for m in lens]
+        self.v = [(torch.randn(layers, m, kv_heads, dim, generator=g) + 0.25).to(dtype) for m in lens]
+        self.slots, self.table, self.page, self.kv_heads = slots, table, page, kv_heads
+        for i, m in enumerate(lens):
+            if m == 0:
+                continue
+            pos = torch.arange(m)
+            ka, va = R.places(dtype, page, kv_heads, R.padded(dim), pos, table[slots[i]][pos // page])
+            pad = (0, R.padded(dim) - dim)
+            for l in range(layers):
+                self.kpool[l, ka.view(-1)] = torch.nn.functional.pad(self.k[i][l], pad).reshape(-1)
+                self.vpool[l, va.view(-1)] = torch.nn.functional.pad(self.v[i][l], pad).reshape(-1)
+        off = [0]
+        for x in new:
+            off.append(off[-1] + x)
+        self.off, rows = off, off[-1] + extra_rows
+        self.q = (1.5 * torch.randn(layers, max(rows, 1), heads, dim, generator=g)).to(dtype)
+        self.scale = 1.0 / math.sqrt(dim) if scale is None else scale
+        self.cache = PagedCache(layers, pages, page, kv_heads, dim, n + 2, width, dtype=dtype,
+                                k=self.kpool.view(layers, pages, elems).cuda(), v=self.vpool.view(layers, pages, elems).cuda(),
+                                table=table.cuda(), lens=all_lens.cuda())
+        self.qd = self.q.cuda()
+        self.att = BlockAttention(self.cache, heads, n, max(new + [1]), self.q.shape[1], mask_block=mask, scale=scale)
+        self.offd, self.slotsd = (torch.tensor(x, dtype=torch.int32).cuda() for x in (off, slots))
+
+    def run(self, layer=0):
+        out = torch.full(self.q.shape[1:], 7.0, dtype=self.dtype, device="cuda")
+        lse = torch.full(self.q.shape[1:3], 7.0, device="cuda")
+        self.att.begin(self.offd, self.slotsd)
+        self.att.plan()
+        self.att.attend(layer, self.qd[layer], out, lse)
+        torch.cuda.synchronize()
+        return out.cpu(), lse.cpu()
+
+    def check(self, out, lse, layer=0, see=None):
+        for i, (m, n) in enumerate(zip(self.lens, self.new)):
+            rows = slice(self.off[i], self.off[i + 1])
+            end = R.ends(range(m - n, m), m, self.mask) if see is None else see(i)
+            ref = R.attention(self.q[layer, rows], self.k[i][layer], self.v[i][layer], end, self.scale)
+            tol, ltol = R.bounds(self.dtype, self.dim, max(m, 1), *ref)
+            empty = torch.isinf(ref[1])
+            assert torch.equal(empty, torch.isinf(lse[rows].double()) & (lse[rows] < 0)), f"sequence {i}: empty rows"
+            assert (out[rows][empty] == 0).all()
+            e = (out[rows].double() - ref[0]).abs()
+            assert bool((e <= tol).all()), f"sequence {i} (len {m}, new {n}): off by {float((e / tol).max()):.3g} of the bound"
+            le = (lse[rows].double() - ref[1]).abs()[~empty]
+            assert bool((le <= ltol[~empty]).all()), f"sequence {i}: lse off by {float((le / ltol[~empty]).max()):.3g} of the bound"
+        assert (out[self.off[-1]:] == 7.0).all() and (lse[self.off[-1]:] == 7.0).all(), "rows behind the last sequence"
+
+
+HEADS = [(BF16, 4, 4, 64, 32), (BF16, 8, 2, 128, 32), (BF16, 5, 1, 80, 64), (BF16, 6, 2, 96, 32), (BF16, 16, 1, 256, 128),
+         (BF16, 3, 3, 8, 32), (BF16, 8, 4, 184, 64), (F32, 4, 2, 64, 32), (F32, 3, 1, 40, 64), (F32, 4, 4, 128, 32),
+         (F32, 2, 1, 256, 32), (F32, 6, 2, 136, 32), (F32, 4, 4, 96, 64)]
+
+
+@pytest.mark.parametrize("mask", [0, 1, 8, 32])
+@pytest.mark.parametrize("dtype,heads,kv,dim,page", HEADS)
+def test_head_layouts_and_masks(gpu_lib, dtype, heads, kv, dim, page, mask):
+    s = Setup(dtype, heads, kv, dim, page, lens=[33, 1, 0, 70, 5, 32], new=[8, 1, 3, 21, 9, 0], mask=mask, seed=dim + mask)
+    s.check(*s.run())
+
+
+LENGTHS = [([1], [1]), ([31], [1]), ([32], [1]), ([33], [1]), ([64], [64]), ([257], [32]), ([1000], [3]), ([2049], [1]), ([700], [130]),
+           ([300, 1, 77], [300, 1, 40]), ([5000], [1]), ([4100, 40], [32, 32]), ([0], [4]), ([2], [40]), ([650, 0, 3], [0, 0, 1])]
+
+
+@pytest.mark.parametrize("mask", [0, 1, 24])
+@pytest.mark.parametrize("lens,new", LENGTHS)
+def test_lengths(gpu_lib, lens, new, mask):
+    s = Setup(BF16, 8, 2, 64, 32, lens, new, mask, seed=sum(lens) + mask)
+    s.check(*s.run())
+    s = Setup(F32, 2, 1, 32, 64, lens, new, mask, seed=sum(lens) + mask, extra_rows=0)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_sequences(gpu_lib, dtype):
+    lens = [(7 * i * i) % 211 for i in range(150)]
+    new = [min(x, i % 4) for i, x in enumerate(lens)]
+    s = Setup(dtype, 4, 2, 32, 32, lens, new, 1, seed=5)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("scale", [1e-3, 3.0])
+def test_flat_and_sharp_scores(gpu_lib, scale):
+    """All keys alike, and one key that takes everything (the running maximum jumps)."""
+    s = Setup(BF16, 4, 1, 128, 32, [900], [40], 32, seed=9, scale=scale)
+    s.check(*s.run())
+
+
+def _poison(s, i, positions, value, which):
+    pos = torch.tensor(positions)
+    at = R.places(s.dtype, s.page, s.kv_heads, s.dim, pos, s.table[s.slots[i]][pos // s.page])[which == "v"].view(-1)
+    pool = (s.cache.v if which == "v" else s.cache.k).view(-1)
+    pool[at.cuda()] = value
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), torch.finfo(BF16).min])
+@pytest.mark.parametrize("dtype,new", [(BF16, 8), (BF16, 40), (F32, 8)])
+def test_masked_places_do_not_matter(gpu_lib, dtype, new, value, which):
+    """Later tokens that hold NaN, infinities or the lowest value: rows that do not see them are what they were, to the
+    bit where no value is summed in another order."""
+    s = Setup(dtype, 4, 2, 64, 32, [150], [new], 1, seed=3)
+    before, lse0 = s.run()
+    s.check(before, lse0)
+    first = 150 - new + new // 2  # poisoned from here on
+    _poison(s, 0, list(range(first, 150)), value, which)
+    out, lse = s.run()
+    rows = slice(0, new // 2)
+    assert torch.equal(lse[rows], lse0[rows])
+    # a tile whose values are not finite is summed key by key
+    ref = R.attention(s.q[0, rows], s.k[0][0], s.v[0][0], R.ends(range(150 - new, first), 150, 1), s.scale)
+    tol, _ = R.bounds(dtype, 64, 150, *ref)
+    assert bool(((out[rows].double() - ref[0]).abs() <= tol).all())
+    if not (abs(value) < float("inf")):
+        assert not torch.isfinite(out[new // 2:new]).any() if which == "v" else True
+
+
+def test_visible_nan_and_infinity_spread_as_they_do_in_the_definition(gpu_lib):
+    s = Setup(BF16, 4, 2, 64, 32, [100], [10], 1, seed=3)
+    _poison(s, 0, [95], float("nan"), "v")
+    _poison(s, 0, [40], float("inf"), "v")
+    out, lse = s.run()
+    assert torch.isfinite(lse[:10]).all()
+    assert (out[:5] == float("inf")).all() and torch.isnan(out[5:10]).all()
+
+
+def test_pages_outside_the_pool_are_not_followed(gpu_lib):
+    s = Setup(BF16, 4, 2, 64, 32, [200, 50], [6, 2], 0, seed=4)
+    row = s.slots[0]
+    for j, bad in ((1, -1), (3, 1 << 30), (6, -7)):
+        s.cache.table[row, j] = bad
+    out, lse = s.run()
+    keep = [p for p in range(200) if p // 32 not in (1, 3, 6)]
+    s.k[0], s.v[0] = s.k[0][:, keep], s.v[0][:, keep]
+    s.check(out, lse, see=lambda i: torch.tensor([len(keep)] * 6) if i == 0 else torch.tensor([50] * 2))
+
+
+def test_slots_and_offsets_out_of_range_touch_nothing(gpu_lib):
+    s = Setup(BF16, 4, 2, 64, 32, [60, 50], [6, 2], 0, seed=4)
+    s.slotsd[0] = 1 << 20
+    out, lse = s.run()
+    assert (out[:6] == 7.0).all() and (lse[:6] == 7.0).all()
+    s.slotsd[0] = s.slots[0]
+    s.offd[2] = 1 << 30  # the second sequence's rows run on: cut to T, and to max_new
+    out, _ = s.run()
+    assert out.shape[0] == 10 and torch.isfinite(out[:6]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_strided_rows(gpu_lib, dtype):
+    """q a part of a wider tensor, out a part of another."""
+    s = Setup(dtype, 6, 2, 72, 32, [90, 40], [33, 2], 8, seed=6)
+    ref, lse0 = s.run()
+    T, W = s.q.shape[1], 6 * 72
+    wide = torch.full((T, W + 64), 3.0, dtype=dtype, device="cuda")
+    wide[:, 8:8 + W] = s.qd[0].view(T, W)
+    res = torch.full((T, W + 16), 7.0, dtype=dtype, device="cuda")
+    s.att.attend(0, wide[:, 8:8 + W].view(T, 6, 72), res[:, 8:8 + W].view(T, 6, 72))
+    assert torch.equal(res[:, 8:8 + W].reshape(T, 6, 72).cpu(), ref)
+    assert (res[:, :8] == 7.0).all() and (res[:, 8 + W:] == 7.0).all()
+
+
+def test_layers_share_a_plan_and_results_repeat(gpu_lib):
+    s = Setup(BF16, 8, 2, 128, 32, [3000, 40], [32, 8], 32, seed=7, layers=3)
+    runs = [[s.run(l) for l in range(3)] for _ in range(3)]
+    for l in range(3):
+        s.check(*runs[0][l], layer=l)
+        for r in runs[1:]:
+            assert torch.equal(r[l][0], runs[0][l][0]) and torch.equal(r[l][1], runs[0][l][1])
+
+
+def test_other_stream(gpu_lib):
+    s = Setup(BF16, 8, 2, 64, 32, [500], [8], 8, seed=8)
+    want, _ = s.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = torch.zeros_like(s.qd[0])
+    s.att.plan(stream=side)
+    s.att.attend(0, s.qd[0], out, stream=side)
+    side.synchronize()
+    assert torch.equal(out[:8].cpu(), want[:8])
+
+
+def test_captured_step_follows_the_lengths(gpu_lib):
+    """One graph of plan and attend, replayed while the sequences grow; two graphs that share the workspace."""
+    s = Setup(BF16, 8, 2, 64, 32, [600, 90], [4, 4], 1, seed=10)
+    a = Setup(BF16, 8, 2, 64, 32, [600, 90], [4, 4], 1, seed=10)
+    out, out2 = torch.zeros_like(s.qd[0]), torch.zeros_like(s.qd[0])
+    s.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    with torch.cuda.stream(side):
+        for o in (out, out2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                s.att.plan()
+                s.att.attend(0, s.qd[0], o)
+            graphs.append(g)
+    torch.cuda.current_stream().wait_stream(side)
+    for lens in ([600, 90], [333, 4], [64, 65], [600, 1]):
+        for c in (s.cache, a.cache):
+            for slot, m in zip(s.slots, lens):
+                c.lens[slot] = m
+        want, _ = a.run()
+        out.fill_(7.0)
+        out2.fill_(7.0)
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu(), want) and torch.equal(out2.cpu(), want)
+    del graphs
+
+
+def test_pages_beyond_32_bit_offsets(gpu_lib):
+    """A pool whose last pages start past 2^32 elements."""
+    page, dim = 1024, 128
+    elems = page * dim
+    pages = (1 << 32) // elems + 40
+    cache = PagedCache(1, pages, page, 1, dim, 1, 4)
+    g = torch.Generator().manual_seed(1)
+    n, new = 3 * page + 100, 5
+    k, v = (torch.randn(n, 1, dim, generator=g).to(BF16) for _ in range(2))
+    ids = torch.tensor([pages - 1, 3, pages - 7, pages - 2], dtype=torch.int32)
+    cache.table[0] = ids.cuda()
+    att = BlockAttention(cache, 4, 1, n, n, mask_block=1)
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    cache.lens[0] = n
+    att.begin(off)
+    att.append(0, k.cuda(), v.cuda())
+    q = torch.randn(new, 4, dim, generator=g).to(BF16)
+    short = BlockAttention(cache, 4, 1, new, new, mask_block=1)
+    short.begin(torch.tensor([0, new], dtype=torch.int32, device="cuda"))
+    short.plan()
+    out = short.attend(0, q.cuda()).cpu()
+    ref = R.attention(q, k, v, R.ends(range(n - new, n), n, 1), 1 / math.sqrt(dim))
+    tol, _ = R.bounds(BF16, dim, n, *ref)
+    assert bool(((out.double() - ref[0]).abs() <= tol).all())
+    del cache
+    torch.cuda.empty_cache()
+
+
+def test_wrong_tensors_are_refused(gpu_lib):
+    s = Setup(BF16, 4, 2, 64, 32, [60], [6], 0)
+    s.run()
+    q = s.qd[0]
+    with pytest.raises(ValueError):
+        s.att.attend(0, q.float())
+    with pytest.raises(ValueError):
+        s.att.attend(0, q[:, :2])
+    with pytest.raises(ValueError):
+        s.att.attend(0, q[:3])
+    with pytest.raises(lib.DmoeError, match="overlap"):
+        s.att.attend(0, q, q)
+    with pytest.raises(lib.DmoeError, match="layer"):
+        s.att.attend(1, q)
+    with pytest.raises(RuntimeError):
+        BlockAttention(s.cache, 4, 1, 6, 8).plan()

@@ -1,0 +1,187 @@
+"""Pages handed out, shared, copied, freed and moved, against the bookkeeping
+on lists.  Marked ``gpu``."""
+import random
+
+import pytest
+import torch
+
+import attention_ref as R
+from paper_2605_30876_amd.attention import PagedCache
+
+pytestmark = pytest.mark.gpu
+
+
+class Both:
+    """A cache and its model on lists; every page's data is known."""
+
+    def __init__(self, n_pages, page, n_slots, max_pages, layers=2, dtype=torch.bfloat16):
+        self.m = R.Pages(n_pages, page, n_slots, max_pages)
+        self.c = PagedCache(layers, n_pages, page, 2, 40, n_slots, max_pages, dtype=dtype)
+        self.c.k.copy_(torch.randn_like(self.c.k, dtype=torch.float32))
+        self.c.v.copy_(torch.randn_like(self.c.v, dtype=torch.float32))
+        self.k, self.v = self.c.k.clone(), self.c.v.clone()
+
+    def _move(self, pairs):
+        if pairs:
+            a, b = ([p[i] for p in pairs] for i in (0, 1))
+            self.k[:, b], self.v[:, b] = self.k[:, a], self.v[:, a]
+
+    def same(self):
+        assert self.c.lens.tolist() == self.m.lens
+        assert self.c.refs.tolist() == self.m.refs
+        assert self.c.table.tolist() == self.m.table
+        assert torch.equal(self.c.k, self.k) and torch.equal(self.c.v, self.v)
+
+    def update(self, dst, size, src=None, keep=None):
+        want, copies = self.m.update(dst, size, src, keep)
+        t = [None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda") for x in (dst, size, src, keep)]
+        self.c.update(t[0], t[1], src=t[2], keep=t[3])
+        self._move(copies)
+        assert int(self.c.status[0]) == want
+        self.same()
+        return want
+
+    def compact(self):
+        n, moves = self.m.compact()
+        counts = torch.zeros(2, dtype=torch.int32, device="cuda")
+        self.c.compact(counts=counts)
+        self._move(moves)
+        assert counts.tolist() == [n, len(moves)]
+        self.same()
+
+
+def test_grow_truncate_free(gpu_lib):
+    b = Both(20, 32, 4, 8)
+    assert b.update([2, 0], [33, 64]) == 0
+    assert b.m.table[2][:2] == [0, 1] and b.m.table[0][:2] == [2, 3]  # the lowest free pages, in order of entries
+    b.update([2], [1])
+    b.update([1, 2], [100, 40])
+    b.update([0], [0])
+    b.update([0, 1, 2, 3], [0, 0, 0, 256])
+    b.update([3], [256])
+
+
+def test_fork_shares_full_pages_and_copies_the_last(gpu_lib):
+    b = Both(20, 32, 4, 8)
+    b.update([0], [80])
+    b.update([1, 2], [90, 64], [0, 0], [80, 64])
+    assert b.m.refs[:3] == [3, 3, 1] and b.m.table[1][2] == 3
+    b.update([0], [0])  # the shared pages stay
+    assert b.m.refs[:3] == [2, 2, 0]
+    b.update([2], [40])  # truncated into a shared page: it becomes a copy of its own
+    assert b.m.table[2][1] != b.m.table[1][1]
+
+
+def test_a_search_exchanges_its_hypotheses(gpu_lib):
+    """Every slot replaced by another, sources overwritten in the same call."""
+    b = Both(40, 32, 4, 6)
+    b.update([0, 1, 2, 3], [70, 50, 33, 96])
+    b.update([0, 1, 2, 3], [71, 71, 97, 51], [1, 0, 3, 1], [50, 70, 96, 50])
+    b.update([3, 0], [51, 52], [0, 3], [51, 50])
+
+
+def test_pages_lacking_change_nothing(gpu_lib):
+    b = Both(6, 32, 3, 8)
+    assert b.update([0], [150]) == 0
+    assert b.update([1, 2], [33, 20]) == 2
+    assert b.update([1], [1], [0], [33 - 32]) == 0
+    assert b.update([1, 0], [32 * 6, 10]) == 1
+    assert b.update([0, 1], [0, 32 * 6]) == 0  # what the call frees it may give out
+
+
+def test_refused_calls_change_nothing(gpu_lib):
+    b = Both(10, 32, 3, 4)
+    b.update([0], [60])
+    for dst, size, src, keep in (([0, 0], [10, 20], None, None), ([3], [1], None, None), ([-1], [1], None, None), ([1], [129], None, None),
+                                 ([1], [-1], None, None), ([1], [70], [0], [61]), ([1], [20], [0], [30]), ([1], [20], [0], [-1]),
+                                 ([1], [20], [5], [0]), ([2, 1, 2], [1, 1, 1], None, None)):
+        assert b.update(dst, size, src, keep) == -1
+    b.c.table[0, 1] = 99  # a table that names a page there is not
+    t = torch.tensor([0], dtype=torch.int32, device="cuda")
+    refs = b.c.refs.clone()
+    b.c.free(t)
+    assert int(b.c.status[0]) == -1 and torch.equal(b.c.refs, refs) and int(b.c.lens[0]) == 60
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_random_calls(gpu_lib, seed):
+    r = random.Random(seed)
+    slots, max_pages, page = r.choice([(5, 6, 32), (40, 5, 64), (9, 20, 32)])
+    b = Both(r.choice([25, 60, 130]), page, slots, max_pages, layers=r.choice([1, 3]), dtype=r.choice([torch.bfloat16, torch.float32]))
+    for _ in range(25):
+        n = r.randint(1, slots)
+        dst = r.sample(range(slots), n)
+        kind = r.random()
+        if kind < 0.15:
+            b.compact()
+        elif kind < 0.5:
+            b.update(dst, [r.randint(0, max_pages * page) if r.random() < 0.3 else r.randint(0, page) for _ in dst])
+        else:
+            src = [r.randrange(slots) for _ in dst]
+            keep = [r.randint(0, b.m.lens[s]) for s in src]
+            b.update(dst, [min(max_pages * page, k + r.randint(0, 40)) for k in keep], src, keep)
+
+
+def test_many_entries_and_pages(gpu_lib):
+    """More entries than threads, and more pages than a thread each."""
+    b = Both(9000, 32, 1500, 6, layers=1)
+    r = random.Random(1)
+    b.update(list(range(1500)), [r.randint(0, 150) for _ in range(1500)])
+    src = [r.randrange(1500) for _ in range(1400)]
+    b.update(list(range(50, 1450)), [max(1, b.m.lens[s]) for s in src], src, [r.randint(0, b.m.lens[s]) for s in src])
+    b.compact()
+
+
+def test_compaction_out_of_place(gpu_lib):
+    b = Both(30, 32, 4, 6)
+    b.update([0, 1, 2, 3], [100, 90, 190, 33])
+    b.update([0, 2], [0, 0])
+    table, refs = b.c.table.clone(), b.c.refs.clone()
+    t2, r2, n = torch.zeros_like(table), torch.zeros_like(refs), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for _ in range(2):  # twice with the same outcome: the inputs are not touched
+        b.c.compact(table_out=t2, refs_out=r2, counts=n)
+        assert torch.equal(b.c.table, table) and torch.equal(b.c.refs, refs)
+    live, moves = b.m.compact()
+    b._move(moves)
+    assert t2.tolist() == b.m.table and r2.tolist() == b.m.refs and n.tolist() == [live, len(moves)]
+    assert torch.equal(b.c.k, b.k) and torch.equal(b.c.v, b.v)
+
+
+def test_copy_pages(gpu_lib):
+    b = Both(12, 96, 1, 2, layers=3)
+    pairs = [[0, 5], [0, 6], [11, 1], [3, 12], [-1, 2], [4, 4]]
+    b.c.copy_pages(torch.tensor(pairs, dtype=torch.int32, device="cuda"))
+    b._move(pairs[:3])
+    b.same()
+
+
+def test_captured_calls(gpu_lib):
+    """Grow, fork and compact as one graph, replayed from different states."""
+    b, e = Both(40, 32, 3, 6), Both(40, 32, 3, 6)
+    e.c.k.copy_(b.c.k), e.c.v.copy_(b.c.v)
+    dst, src = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([1, 2], [0, 0]))
+    one, size, keep = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0], [70], [65, 33]))
+
+    def step(c):
+        c.resize(one, size)
+        c.fork(dst, src, keep)
+        c.compact()
+
+    step(b.c), step(e.c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step(b.c)
+    torch.cuda.current_stream().wait_stream(side)
+    for n, k in ((70, [65, 33]), (190, [190, 1]), (10, [0, 9]), (70, [65, 33])):
+        size.fill_(n)
+        keep.copy_(torch.tensor(k, dtype=torch.int32))
+        torch.cuda.synchronize()
+        g.replay()
+        step(e.c)
+        torch.cuda.synchronize()
+        for name in ("table", "lens", "refs", "k", "v"):
+            assert torch.equal(getattr(b.c, name), getattr(e.c, name)), name
+    del g
