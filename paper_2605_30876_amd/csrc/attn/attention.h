@@ -30,6 +30,11 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // covers 2c elements of the head dimension (keys) or 2c tokens (values).
 template <typename T>
 struct Types;
+__device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4);
+}
 template <>
 struct Types<bf16_t> {
   typedef bf16x8 Frag;
@@ -44,11 +49,11 @@ struct Types<bf16_t> {
     for (int i = 0; i < 8; ++i) f[i] = static_cast<__bf16>(p[8 * s + i]);
     return f;
   }
-  static __device__ __forceinline__ float rounded(float p) { return static_cast<float>(static_cast<__bf16>(p)); }
-  static __device__ __forceinline__ bool finite(const Frag& f) {
+  // the largest exponent field of f's values, in its place in a float32
+  static __device__ __forceinline__ uint32_t exponent(const Frag& f) {
     const uint4 u = __builtin_bit_cast(uint4, f);
-    auto bad = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
-    return !(bad(u.x) || bad(u.y) || bad(u.z) || bad(u.w));
+    auto top = [](uint32_t w) { return max(w & 0x7f800000u, w << 16 & 0x7f800000u); };
+    return max(max(top(u.x), top(u.y)), max(top(u.z), top(u.w)));
   }
 };
 template <>
@@ -62,12 +67,9 @@ struct Types<float> {
   static __device__ __forceinline__ Frag probs(const f32x16& p, int s) {
     return Frag{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]};
   }
-  static __device__ __forceinline__ float rounded(float p) { return p; }
-  static __device__ __forceinline__ bool finite(const Frag& f) {
-    bool ok = true;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) ok = ok && (__float_as_uint(f[i]) & 0x7f800000u) != 0x7f800000u;
-    return ok;
+  static __device__ __forceinline__ uint32_t exponent(const Frag& f) {
+    const uint4 u = __builtin_bit_cast(uint4, f);
+    return max(max(u.x & 0x7f800000u, u.y & 0x7f800000u), max(u.z & 0x7f800000u, u.w & 0x7f800000u));
   }
 };
 
@@ -117,35 +119,38 @@ struct WaveRows {
     return s;
   }
 
-  // Scores (times scale log2 e) to probabilities relative to the running
-  // maximum, which they raise first if they have to.  masked: keys from
-  // `end - key0` on are not seen.
-  __device__ __forceinline__ void softmax(f32x16& s, float scale2, int key0, bool masked, int half) {
+  // Scores (times scale log2 e) of consecutive tiles to probabilities relative
+  // to the running maximum, which they raise first if they have to.  masked:
+  // keys from `end - key0` on are not seen.
+  template <int NT>
+  __device__ __forceinline__ void softmax(f32x16 (&s)[NT], float scale2, int key0, bool masked, int half) {
     if (masked) {
       const int seen = end - key0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = tile_key(i, half) < seen ? s[i] : -INFINITY;
-    }
-    float t = s[0];
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int i = 1; i < 16; ++i) t = fmaxf(t, s[i]);
+        for (int i = 0; i < 16; ++i) s[n][i] = n * kTileTokens + tile_key(i, half) < seen ? s[n][i] : -INFINITY;
+    }
+    float t = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = fmaxf(t, s[n][i]);
     t = other_half_max(t) * scale2;
     if (__any(t > m + kLazy)) {
       const float nm = fmaxf(m, t);
       const float a = nm == m ? 1.f : exp2_hw(m - nm);
       m = nm;
-      l *= a;
-#pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[b][i] *= a;
+      scale(a);
     }
     const float off = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = exp2_hw(__builtin_fmaf(s[i], scale2, -off));
-      l += s[i];
-    }
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = exp2_hw(__builtin_fmaf(s[n][i], scale2, -off));
+        l += s[n][i];
+      }
   }
 
   __device__ __forceinline__ void add(const f32x16& p, const Frag (&v)[kB][kS]) {
@@ -157,43 +162,67 @@ struct WaveRows {
     }
   }
 
-  // A tile in which some row does not see every key.  Values that no row of
-  // the wave sees are not the sequence's, or a later token's: they become 0,
-  // whatever they are.  A value that some rows see and others do not must not
-  // reach the others through 0 * value: where one is not finite (v0: the
-  // tile's values in memory), the tile is added key by key.
-  __device__ __forceinline__ void add_masked(const f32x16& p, Frag (&v)[kB][kS], int key0, int half, const T* v0) {
+  // For a tile in which some row does not see every key: values that no row
+  // of the wave sees are not the sequence's, or a later token's, and become 0,
+  // whatever they are.  True if the rest is finite; a value that some rows see
+  // and others do not must not reach the others through 0 * value.
+  __device__ __forceinline__ bool cut(Frag (&v)[kB][kS], int key0, int half) const {
     const int seen = hi - key0;
-    bool fine = true;
+    uint32_t top = 0;
 #pragma unroll
-    for (int s = 0; s < kS; ++s)
+    for (int s = 0; s < kS; ++s) {
+      // all ones in the words (halves of words) of tokens that are seen
+      uint32_t m[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        constexpr int per = c / 4;
+        auto on = [&](int e) { return 2 * c * s + 8 * (e / 4) + 4 * half + e % 4 < seen; };
+        if constexpr (per == 1)
+          m[x] = on(x) ? ~0u : 0u;
+        else
+          m[x] = (on(2 * x) ? 0xffffu : 0u) | (on(2 * x + 1) ? 0xffff0000u : 0u);
+      }
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
-#pragma unroll
-        for (int e = 0; e < c; ++e)
-          if (2 * c * s + 8 * (e / 4) + 4 * half + e % 4 >= seen) v[b][s][e] = 0;
-        fine = fine && Ty::finite(v[b][s]);
+        const uint4 u = __builtin_bit_cast(uint4, v[b][s]);
+        v[b][s] = __builtin_bit_cast(Frag, make_uint4(u.x & m[0], u.y & m[1], u.z & m[2], u.w & m[3]));
+        top = max(top, Ty::exponent(v[b][s]));
       }
-    if (__all(fine)) {
-      add(p, v);
-      return;
     }
-    const int lane = threadIdx.x & 63;
-    for (int key = 0; key < kTileTokens; ++key) {
-      if (key >= seen) break;
-      const int reg = 4 * (key >> 3) + (key & 3), kh = (key >> 2) & 1;
-      float w = 0.f;
+    return __all(top != 0x7f800000u);
+  }
+  // f with all elements but one set to 0 (slot -1: all).
+  static __device__ __forceinline__ Frag only(const Frag& f, int slot) {
+    constexpr int kPer = c / 4;  // elements of a 32-bit word
+    const uint4 u = __builtin_bit_cast(uint4, f);
+    const uint32_t bits = kPer == 1 ? ~0u : slot & 1 ? 0xffff0000u : 0x0000ffffu;
+    const int word = slot < 0 ? -1 : slot / kPer;
+    return __builtin_bit_cast(Frag, make_uint4(u.x & (word == 0 ? bits : 0), u.y & (word == 1 ? bits : 0), u.z & (word == 2 ? bits : 0),
+                                               u.w & (word == 3 ? bits : 0)));
+  }
+  // Such a tile key by key: a key's products are added to the rows that see it.
+  __device__ __forceinline__ void add_by_key(const f32x16& p, const Frag (&v)[kB][kS], int key0, int half) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w = i == reg ? p[i] : w;
-      w = Ty::rounded(__shfl(w, (lane & 31) + 32 * kh));
-      if (key0 + key >= end) continue;
-      const int r = key % (2 * c);
+    for (int s = 0; s < kS; ++s) {
+      const Frag f = Ty::probs(p, s);
+#pragma unroll 1
+      for (int r = 0; r < 2 * c; ++r) {
+        const bool mine = (r >> 2 & 1) == half;
+        const int slot = mine ? (r >> 3) * 4 + (r & 3) : -1;
+        const bool sees = key0 + 2 * c * s + r < end;
+        const Frag one = only(f, slot);
 #pragma unroll
-      for (int b = 0; b < kB; ++b)
+        for (int b = 0; b < kB; ++b) {
+          const Frag x = only(v[b][s], slot);
+          f32x16 t;
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          o[b][i] += w * load_as_f32<T>(v0 + value_chunk<c>(32 * b + tile_key(i, half), key / (2 * c), r % 8 / 4) +
-                                        r / 8 * 4 + r % 4);
+          for (int i = 0; i < 16; ++i) t[i] = 0.f;
+          Ty::mma(t, x, one);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[b][i] += sees ? t[i] : 0.f;
+          __builtin_amdgcn_sched_barrier(0);  // one block's products at a time: registers are short here
+        }
+      }
     }
   }
 
@@ -208,10 +237,106 @@ struct WaveRows {
   }
 };
 
-// One item of one kv head per workgroup: kWR waves along the rows (tiles of
-// 32*kWR), kWK along the keys (every kWK-th tile), joined through LDS.
-template <typename T, int DP, int kWR, int kWK>
-__global__ __launch_bounds__(64 * kWR * kWK) void attention_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+// Waves a SIMD holds: two where the sums, the queries and a tile fit half of its registers.
+template <typename T>
+constexpr int waves_per_simd(int dp) {
+  return dp * sizeof(T) <= 256 ? 2 : 1;
+}
+
+// Where a sequence's tiles of one kv head lie.
+template <typename T, int DP>
+struct TileMap {
+  const T *k, *v;
+  // nothing of a launch writes the table: scalar loads, as the constant address space has them
+  const __attribute__((address_space(4))) int32_t* table;
+  long page_len, layer0;
+  int hkv, n_pages, shift;  // tiles of a page: 1 << shift, or -shift of them
+  __device__ __forceinline__ TileMap(const AttnArgs& a, int slot, int hk)
+      : table((const __attribute__((address_space(4))) int32_t*)(a.cache.table + static_cast<long>(slot) * a.cache.max_pages)), hkv(a.cache.n_kv_heads), n_pages(a.cache.n_pages) {
+    const int tpp = a.cache.page_tokens / kTileTokens;
+    shift = (tpp & (tpp - 1)) == 0 ? 31 - __builtin_clz(tpp) : -tpp;
+    page_len = static_cast<long>(a.cache.page_tokens) * DP;
+    layer0 = static_cast<long>(a.layer) * n_pages;
+    k = static_cast<const T*>(a.cache.k) + hk * page_len;
+    v = static_cast<const T*>(a.cache.v) + hk * page_len;
+  }
+  // page of a tile before `end`, else -1
+  __device__ __forceinline__ int page(int kt, int end) const { return kt < end ? table[shift >= 0 ? kt >> shift : kt / -shift] : -1; }
+  __device__ __forceinline__ bool holds(int page) const { return static_cast<unsigned>(page) < static_cast<unsigned>(n_pages); }
+  // elements from k and v to a tile on a page that is held
+  __device__ __forceinline__ long at(int kt, int page) const {
+    const int in = shift >= 0 ? kt & ((1 << shift) - 1) : kt % -shift;
+    return (layer0 + page) * hkv * page_len + in * (kTileTokens * DP);
+  }
+};
+
+// The item's rows of this wave: row index, head and what they see; queries loaded.
+template <typename T, int DP>
+struct RowPlace {
+  int row, tok, qh;
+  bool live, any;
+  __device__ __forceinline__ RowPlace(WaveRows<T, DP>& w, const AttnArgs& a, const AttnItem& it, int g, int hk, int row_lo, int lane) {
+    constexpr int c = Types<T>::c;
+    typedef typename Types<T>::Frag Frag;
+    const int row_hi = min(row_lo + 32, it.rows) - 1;
+    const int pos0 = it.len - it.n;
+    row = row_lo + (lane & 31);
+    live = row < it.rows;
+    any = row_hi >= row_lo;
+    tok = live ? row / g : 0;
+    qh = hk * g + (live ? row - tok * g : 0);
+    w.end = live ? visible_end(pos0 + tok, it.len, a.mask_block) : 0;
+    // the ends grow with the rows; rows past the last are computed and dropped
+    w.lo = any ? visible_end(pos0 + row_lo / g, it.len, a.mask_block) : 0;
+    w.hi = any ? visible_end(pos0 + row_hi / g, it.len, a.mask_block) : 0;
+    const T* qp = static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
+#pragma unroll
+    for (int j = 0; j < WaveRows<T, DP>::kK; ++j) {
+      const int d = (2 * j + (lane >> 5)) * c;
+      Frag f{};
+      if (live && d < a.cache.head_dim) f = *reinterpret_cast<const Frag*>(qp + d);
+      w.q[j] = f;
+    }
+  }
+  // The wave's sums: divided into out, or as they are into the workspace.
+  __device__ __forceinline__ void store(const WaveRows<T, DP>& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk,
+                                        int half, int part_rows) const {
+    constexpr int kB = WaveRows<T, DP>::kB;
+    if (!live) return;
+    if (it.part >= 0) {
+      const long at = (static_cast<long>(it.part) * a.cache.n_kv_heads + hk) * sh.tile_rows + (row - it.first);
+      float* po = static_cast<float*>(a.workspace) + at * DP;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(po + 32 * b + tile_key(i, half)) = f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
+      if (half == 0)
+        *reinterpret_cast<float2*>(static_cast<float*>(a.workspace) + static_cast<long>(part_rows) * DP + at * 2) = make_float2(w.m, w.l);
+      return;
+    }
+    const bool some = w.l > 0.f || w.l != w.l;
+    const float inv = some ? 1.f / w.l : 0.f;
+    T* op = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim;
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * b + tile_key(i, half);
+        if (d < a.cache.head_dim)
+          store4(op + d, f32x4{w.o[b][i] * inv, w.o[b][i + 1] * inv, w.o[b][i + 2] * inv, w.o[b][i + 3] * inv});
+      }
+    if (a.lse && half == 0)
+      a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = some ? (w.m + log2f(w.l)) * kLn2 : -INFINITY;
+  }
+};
+
+// Few rows (one token a sequence, a small block): 32 of one kv head per
+// workgroup, its kWK waves on every kWK-th key tile, joined through LDS.  The
+// cache is read once, straight into registers; the next tile's keys are
+// issued when this one's are used up, its values likewise.
+template <typename T, int DP, int kWK>
+__global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef WaveRows<T, DP> Rows;
   typedef typename Rows::Frag Frag;
   constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS;
@@ -222,176 +347,325 @@ __global__ __launch_bounds__(64 * kWR * kWK) void attention_kernel(AttnArgs a, A
   if (item_i >= head->n_items) return;
   const AttnItem it = plan_items(a.plan)[item_i];
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave / kWK, wk = wave % kWK;
-  const int g = sh.group;
-
+  const int wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Rows w;
   w.clear();
-  const int row_lo = it.first + 32 * wr;
-  const int row_hi = min(row_lo + 32, it.rows) - 1;
-  const int row = row_lo + (lane & 31);
-  const bool live = row < it.rows;
-  const int pos0 = it.len - it.n;
-  const int tok = live ? row / g : 0;
-  const int qh = hk * g + (live ? row - tok * g : 0);
-  w.end = live ? visible_end(pos0 + tok, it.len, a.mask_block) : 0;
-  if (row_hi >= row_lo) {
-    // the ends grow with the rows; rows past the last are computed and dropped
-    w.lo = visible_end(pos0 + row_lo / g, it.len, a.mask_block);
-    w.hi = visible_end(pos0 + row_hi / g, it.len, a.mask_block);
-    const T* qp = static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
+  const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first, lane);
+  const float scale2 = a.scale * kLog2e;
+  const TileMap<T, DP> map(a, it.slot, hk);
+  const int kt1 = min(it.kt1, (w.hi + kTileTokens - 1) / kTileTokens);
+  Frag k[kK], v[kB][kS];
+  auto load_k = [&](const T* p) {
 #pragma unroll
-    for (int j = 0; j < kK; ++j) {
-      const int d = (2 * j + half) * c;
-      Frag f{};
-      if (live && d < a.cache.head_dim) f = *reinterpret_cast<const Frag*>(qp + d);
-      w.q[j] = f;
-    }
-    const float scale2 = a.scale * kLog2e;
-    const int tpp = a.cache.page_tokens / kTileTokens;
-    const long page_len = static_cast<long>(a.cache.page_tokens) * DP;
-    const int32_t* table = a.cache.table + static_cast<long>(it.slot) * a.cache.max_pages;
-    const T* kbase = static_cast<const T*>(a.cache.k) + hk * page_len;
-    const T* vbase = static_cast<const T*>(a.cache.v) + hk * page_len;
-    const int kt1 = min(it.kt1, (w.hi + kTileTokens - 1) / kTileTokens);
-    for (int kt = it.kt0 + wk; kt < kt1; kt += kWK) {
-      const int page = __builtin_amdgcn_readfirstlane(table[kt / tpp]);
-      if (page < 0 || page >= a.cache.n_pages) continue;
-      const long at = (static_cast<long>(a.layer) * a.cache.n_pages + page) * hkv * page_len + (kt % tpp) * (kTileTokens * DP);
-      const T* kp = kbase + at;
-      const T* vp = vbase + at;
-      Frag k[kK], v[kB][kS];
-#pragma unroll
-      for (int j = 0; j < kK; ++j) k[j] = *reinterpret_cast<const Frag*>(kp + j * 64 * c + lane * c);
-#pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int s = 0; s < kS; ++s) v[b][s] = *reinterpret_cast<const Frag*>(vp + (b * kS + s) * 64 * c + lane * c);
-      f32x16 s = w.scores(k);
-      const int key0 = kt * kTileTokens;
-      const bool masked = key0 + kTileTokens > w.lo;
-      w.softmax(s, scale2, key0, masked, half);
-      if (masked)
-        w.add_masked(s, v, key0, half, vp);
-      else
-        w.add(s, v);
-    }
-  }
-  w.l = other_half_sum(w.l);
-
-  if constexpr (kWK > 1) {
-    // join the waves of a row tile two by two: the upper ones hand their sums
-    // to the lower ones (fixed order)
-    constexpr int kLen = (16 * kB + 2) * 64;
-#pragma unroll
-    for (int n = kWK / 2; n >= 1; n /= 2) {
-      float* buf = lds + (wr * (kWK / 2) + wk % n) * kLen;
-      if (wk >= n && wk < 2 * n) {
-        buf[lane] = w.m;
-        buf[64 + lane] = w.l;
-#pragma unroll
-        for (int b = 0; b < kB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4) =
-                f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
-      }
-      __syncthreads();
-      if (wk < n) {
-        const float om = buf[lane], ol = buf[64 + lane];
-        const float nm = fmaxf(w.m, om);
-        const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = om == nm ? 1.f : exp2_hw(om - nm);
-        w.scale(fa);
-        w.m = nm;
-        w.l += fb * ol;
-#pragma unroll
-        for (int b = 0; b < kB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
-          }
-      }
-      __syncthreads();
-    }
-  }
-  if (wk != 0 || !live) return;
-
-  if (it.part >= 0) {
-    const long slot = static_cast<long>(it.part) * hkv + hk;
-    float* po = static_cast<float*>(a.workspace) + (slot * sh.tile_rows + (row - it.first)) * DP;
+    for (int j = 0; j < kK; ++j) k[j] = *reinterpret_cast<const Frag*>(p + j * 64 * c + lane * c);
+  };
+  auto load_v = [&](const T* p) {
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4*>(po + 32 * b + tile_key(i, half)) = f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
-    if (half == 0) {
-      float* ml = static_cast<float*>(a.workspace) + static_cast<long>(part_rows) * DP + (slot * sh.tile_rows + (row - it.first)) * 2;
-      ml[0] = w.m;
-      ml[1] = w.l;
-    }
-    return;
+      for (int s = 0; s < kS; ++s) v[b][s] = *reinterpret_cast<const Frag*>(p + (b * kS + s) * 64 * c + lane * c);
+  };
+  // page ids are known two of this wave's tiles ahead, its keys and values one
+  int kt = it.kt0 + wk;
+  int page = map.page(kt, kt1), page1 = map.page(kt + kWK, kt1);
+  if (map.holds(page)) {
+    load_k(map.k + map.at(kt, page));
+    load_v(map.v + map.at(kt, page));
   }
-  const float inv = w.l > 0.f || w.l != w.l ? 1.f / w.l : 0.f;
-  T* op = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim;
-#pragma unroll
-  for (int b = 0; b < kB; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d = 32 * b + tile_key(i, half);
-      if (d < a.cache.head_dim)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) store_from_f32<T>(op + d + t, w.o[b][i + t] * inv);
+  auto turn = [&](auto masked) {
+    const int page2 = map.page(kt + 2 * kWK, kt1);
+    const bool here = map.holds(page), more = map.holds(page1);
+    const long at1 = more ? map.at(kt + kWK, page1) : 0;
+    f32x16 s[1];
+    if (here) s[0] = w.scores(k);
+    if (more) load_k(map.k + at1);
+    if (here) {
+      const int key0 = kt * kTileTokens;
+      w.template softmax<1>(s, scale2, key0, masked, half);
+      if (masked && !w.cut(v, key0, half))
+        w.add_by_key(s[0], v, key0, half);
+      else
+        w.add(s[0], v);
     }
-  if (a.lse && half == 0)
-    a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = w.l > 0.f || w.l != w.l ? (w.m + log2f(w.l)) * kLn2 : -INFINITY;
+    if (more) load_v(map.v + at1);
+    kt += kWK;
+    page = page1;
+    page1 = page2;
+  };
+  // tiles that every row sees whole, then the others
+  const int whole = min(kt1, w.lo / kTileTokens);
+  while (kt < whole) turn(std::false_type());
+  while (kt < kt1) turn(std::true_type());
+  w.l = other_half_sum(w.l);
+
+  // join the waves two by two: the upper ones hand their sums to the lower
+  // ones (fixed order)
+  constexpr int kLen = (16 * kB + 2) * 64;
+#pragma unroll
+  for (int n = kWK / 2; n >= 1; n /= 2) {
+    float* buf = lds + (wk % n) * kLen;
+    if (wk >= n && wk < 2 * n) {
+      buf[lane] = w.m;
+      buf[64 + lane] = w.l;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4) =
+              f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
+    }
+    __syncthreads();
+    if (wk < n) {
+      const float om = buf[lane], ol = buf[64 + lane];
+      const float nm = fmaxf(w.m, om);
+      const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = om == nm ? 1.f : exp2_hw(om - nm);
+      w.scale(fa);
+      w.m = nm;
+      w.l += fb * ol;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
+        }
+    }
+    __syncthreads();
+  }
+  if (wk == 0) rows.store(w, a, sh, it, hk, half, part_rows);
 }
 
-// Partial results of a row tile joined: a wave per row, its lanes along the
-// head dimension, pieces in order.
+// 16 bytes per lane from global memory straight into LDS at dst + 16*lane.
+template <typename T, typename Frag>
+__device__ __forceinline__ void dma16(const T* src, Frag* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// Many rows: 128 of one kv head per workgroup, 32 to a wave, all four waves on
+// the same keys.  Keys and values of kTS tiles go from memory straight into
+// LDS, one stage ahead, in two buffers; one barrier a stage.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+struct BlockStage {
+  static constexpr int kTileFrags = DP / (2 * Types<T>::c);           // operands of a tile's keys, or of its values
+  static constexpr int kTS = DP * sizeof(T) * kTileTokens <= 8192 ? 2 : 1;  // tiles of a stage: up to 32 KiB, or one
+  typename Types<T>::Frag f[kTS][2][kTileFrags][64];                  // [tile][keys, values][operand][lane]
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+  typedef WaveRows<T, DP> Rows;
+  typedef typename Rows::Frag Frag;
+  typedef BlockStage<T, DP> Stage;
+  constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS, kTS = Stage::kTS;
+  __shared__ Stage s0, s1;  // apart, so that reads of one do not wait for loads into the other
   const int hkv = a.cache.n_kv_heads;
   const AttnPlanHead* head = reinterpret_cast<const AttnPlanHead*>(a.plan);
-  const int mi = blockIdx.x / hkv, hk = blockIdx.x % hkv;
-  if (mi >= head->n_merges) return;
-  const AttnMerge* merges = reinterpret_cast<const AttnMerge*>(plan_items(a.plan) + sh.max_items());
-  const AttnMerge mg = merges[mi];
-  const int lane = threadIdx.x & 63;
-  const int r = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = mg.first + r;
-  if (r >= sh.tile_rows || row >= mg.rows) return;
-  const float* po = static_cast<const float*>(a.workspace);
-  const float* ml = po + static_cast<long>(part_rows) * DP;
-  const long step = static_cast<long>(hkv) * sh.tile_rows;
-  const long at = (static_cast<long>(mg.part) * hkv + hk) * sh.tile_rows + r;
-  float m = -INFINITY;
-  for (int i = lane; i < mg.pieces; i += 64) m = fmaxf(m, ml[(at + i * step) * 2]);
+  const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
+  if (item_i >= head->n_items) return;
+  const AttnItem it = plan_items(a.plan)[item_i];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Rows w;
+  w.clear();
+  const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wave, lane);
+  const float scale2 = a.scale * kLog2e;
+  const TileMap<T, DP> map(a, it.slot, hk);
+
+  struct Ids {
+    int id[kTS];
+  };
+  auto pages = [&](int kt) {
+    Ids p;
 #pragma unroll
-  for (int x = 32; x >= 1; x /= 2) m = fmaxf(m, __shfl_xor(m, x));
-  constexpr int kV = (DP + 63) / 64;
-  float o[kV] = {}, l = 0.f;
-  const float off = m == -INFINITY ? 0.f : m;
-  for (int i = 0; i < mg.pieces; ++i) {
-    const float pm = ml[(at + i * step) * 2];
-    const float f = pm == m ? 1.f : exp2_hw(pm - off);
-    l += f * ml[(at + i * step) * 2 + 1];
+    for (int n = 0; n < kTS; ++n) p.id[n] = map.page(kt + n, it.kt1);
+    return p;
+  };
+  // a wave's share of a stage: with two tiles the keys or the values of one,
+  // with one tile half of its keys or values
+  const T *mk = map.k, *mv = map.v;
+  const T* share = wave & 1 ? mv : mk;
+  auto load = [&](int kt, const Ids& pg, Stage& st) {
+    const int n = kTS == 2 ? wave >> 1 : 0, kv = wave & 1;
+    const int page = kTS == 2 && n ? pg.id[kTS - 1] : pg.id[0];
+    if (!map.holds(page)) return;
+    const T* p = share + map.at(kt + n, page) + lane * c;
+    constexpr int kShare = kTS == 2 ? kK : kK / 2;
+    const int j0 = kTS == 2 ? 0 : (wave >> 1) * kShare;
 #pragma unroll
-    for (int j = 0; j < kV; ++j)
-      if (lane + 64 * j < DP) o[j] += f * po[(at + i * step) * DP + lane + 64 * j];
+    for (int j = 0; j < kShare; ++j) dma16(p + (j0 + j) * 64 * c, &st.f[n][kv][j0 + j][0]);
+  };
+  auto compute = [&](auto masked, int kt, const Ids& pg, const Stage& st) {
+    if (!rows.any) return;
+    // tiles that are there, and that some row of the wave sees
+    bool on[kTS];
+    bool all = true, none = true;
+#pragma unroll
+    for (int n = 0; n < kTS; ++n) {
+      on[n] = map.holds(pg.id[n]);
+      if (masked) on[n] = on[n] && (kt + n) * kTileTokens < w.hi;
+      all = all && on[n];
+      none = none && !on[n];
+    }
+    if (none) return;
+    const int key0 = kt * kTileTokens;
+    f32x16 s[kTS];
+#pragma unroll
+    for (int n = 0; n < kTS; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kK; ++j) Types<T>::mma(s[n], st.f[n][0][j][lane], w.q[j]);
+    }
+    if (!all) {
+#pragma unroll
+      for (int n = 0; n < kTS; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] = on[n] ? s[n][i] : -INFINITY;
+    }
+    w.template softmax<kTS>(s, scale2, key0, masked, half);
+#pragma unroll
+    for (int n = 0; n < kTS; ++n) {
+      if (!on[n]) continue;
+      if constexpr (masked) {
+        Frag v[kB][kS];
+#pragma unroll
+        for (int b = 0; b < kB; ++b)
+#pragma unroll
+          for (int x = 0; x < kS; ++x) v[b][x] = st.f[n][1][b * kS + x][lane];
+        if (w.cut(v, key0 + n * kTileTokens, half))
+          w.add(s[n], v);
+        else
+          w.add_by_key(s[n], v, key0 + n * kTileTokens, half);
+      } else {
+#pragma unroll
+        for (int x = 0; x < kS; ++x) {
+          const Frag f = Types<T>::probs(s[n], x);
+#pragma unroll
+          for (int b = 0; b < kB; ++b) Types<T>::mma(w.o[b], st.f[n][1][b * kS + x][lane], f);
+        }
+      }
+    }
+  };
+  // page ids are known two stages ahead, keys and values one.  A stage's loads
+  // are waited for by the wave that issued them, then by all: the barrier also
+  // tells that the other buffer has been read.
+  int kt = it.kt0;
+  Ids pg = pages(kt), pg1 = pages(kt + kTS);
+  load(kt, pg, s0);
+  __builtin_amdgcn_sched_barrier(0);
+  auto turn = [&](auto masked, Stage& cur, Stage& fill) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    load(kt + kTS, pg1, fill);
+    const Ids pg2 = pages(kt + 2 * kTS);
+    __builtin_amdgcn_sched_barrier(0);
+    compute(masked, kt, pg, cur);
+    __builtin_amdgcn_sched_barrier(0);
+    kt += kTS;
+    pg = pg1;
+    pg1 = pg2;
+  };
+  // pairs of stages whose keys every row of the workgroup sees, then the others
+  const int whole = min(it.kt1, visible_end(it.len - it.n + it.first / sh.group, it.len, a.mask_block) / kTileTokens);
+  while (kt + 2 * kTS <= whole) {
+    turn(std::false_type(), s0, s1);
+    turn(std::false_type(), s1, s0);
   }
-  const bool any = l > 0.f || l != l;
-  const float inv = any ? 1.f / l : 0.f;
-  const int tok = row / sh.group, qh = hk * sh.group + row - tok * sh.group;
-  T* op = static_cast<T*>(a.out) + (mg.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim;
-#pragma unroll
-  for (int j = 0; j < kV; ++j)
-    if (lane + 64 * j < a.cache.head_dim) store_from_f32<T>(op + lane + 64 * j, o[j] * inv);
-  if (a.lse && lane == 0)
-    a.lse[static_cast<long>(mg.row0 + tok) * a.n_heads + qh] = any ? (m + log2f(l)) * kLn2 : -INFINITY;
+  while (kt < it.kt1) {
+    turn(std::true_type(), s0, s1);
+    if (kt >= it.kt1) break;
+    turn(std::true_type(), s1, s0);
+  }
+  w.l = other_half_sum(w.l);
+  rows.store(w, a, sh, it, hk, half, part_rows);
 }
+
+// Partial results of a row tile joined: a workgroup per row, its waves on
+// every fourth piece, a wave's lanes over the head dimension and, where it is
+// short, over several pieces.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+  constexpr int kLanes = DP / 4, kPar = 64 / kLanes;  // lanes of a row, pieces at once
+  __shared__ f32x4 so[4][kLanes];
+  __shared__ float2 sml[4];
+  const int hkv = a.cache.n_kv_heads;
+  const AttnPlanHead* head = reinterpret_cast<const AttnPlanHead*>(a.plan);
+  const AttnMerge* merges = reinterpret_cast<const AttnMerge*>(plan_items(a.plan) + sh.max_items());
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane % kLanes, par = lane / kLanes;
+  const float* po = static_cast<const float*>(a.workspace);
+  const float2* ml = reinterpret_cast<const float2*>(po + static_cast<long>(part_rows) * DP);
+  const long step = static_cast<long>(hkv) * sh.tile_rows;
+  const int units = head->n_merges * hkv * sh.tile_rows;
+  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    const int r = u % sh.tile_rows, hk = u / sh.tile_rows % hkv;
+    const AttnMerge mg = merges[u / sh.tile_rows / hkv];
+    const int row = mg.first + r;
+    if (row >= mg.rows) continue;
+    const long at = (static_cast<long>(mg.part) * hkv + hk) * sh.tile_rows + r;
+    // pieces wave, wave + 4, ...: their maximum, then their sums relative to it
+    float m = -INFINITY;
+    for (int i = wave + 4 * lane; i < mg.pieces; i += 256) m = fmaxf(m, ml[at + i * step].x);
+#pragma unroll
+    for (int x = 32; x >= 1; x /= 2) m = fmaxf(m, __shfl_xor(m, x));
+    const float off = m == -INFINITY ? 0.f : m;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+#pragma unroll 4
+    for (int i = wave + 4 * par; i < mg.pieces; i += 4 * kPar) {
+      if (par < kPar) {
+        const float2 x = ml[at + i * step];
+        const f32x4 p = *reinterpret_cast<const f32x4*>(po + (at + i * step) * DP + col * 4);
+        const float f = x.x == m ? 1.f : exp2_hw(x.x - off);
+        l += f * x.y;
+        o += f * p;
+      }
+    }
+    // the pieces of one wave, then of the four, in fixed order
+#pragma unroll
+    for (int j = 1; j < kPar; ++j) {
+      const int from = (lane + j * kLanes) & 63;
+      const float ol = __shfl(l, from);
+      f32x4 oo;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) oo[t] = __shfl(o[t], from);
+      if (par == 0) {
+        l += ol;
+        o += oo;
+      }
+    }
+    __syncthreads();
+    if (par == 0) {
+      so[wave][col] = o;
+      if (col == 0) sml[wave] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (wave != 0 || par != 0) continue;
+    float mm = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mm = fmaxf(mm, sml[i].x);
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = sml[i].x == mm ? 1.f : exp2_hw(sml[i].x - mm);
+      l += f * sml[i].y;
+      o += f * so[i][col];
+    }
+    const bool some = l > 0.f || l != l;
+    const float inv = some ? 1.f / l : 0.f;
+    const int tok = row / sh.group, qh = hk * sh.group + row - tok * sh.group;
+    T* op = static_cast<T*>(a.out) + (mg.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim + col * 4;
+    if (col * 4 < a.cache.head_dim) store4(op, o * inv);
+    if (a.lse && col == 0)
+      a.lse[static_cast<long>(mg.row0 + tok) * a.n_heads + qh] = some ? (mm + log2f(l)) * kLn2 : -INFINITY;
+  }
+}
+
+constexpr long kMergeGrid = 2048;
 
 template <typename T, int DP>
 hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
@@ -400,11 +674,14 @@ hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
   const int part_rows = static_cast<int>(sh.max_parts() * hkv * sh.tile_rows);
   if (sh.tile_rows == 32) {
     constexpr size_t lds = 2 * (16 * (DP / 32) + 2) * 64 * sizeof(float);
-    attention_kernel<T, DP, 1, 4><<<items, 256, lds, s>>>(a, sh, part_rows);
+    attention_rows_kernel<T, DP, 4><<<items, 256, lds, s>>>(a, sh, part_rows);
   } else {
-    attention_kernel<T, DP, 4, 1><<<items, 256, 0, s>>>(a, sh, part_rows);
+    attention_block_kernel<T, DP><<<items, 256, 0, s>>>(a, sh, part_rows);
   }
-  attention_merge_kernel<T, DP><<<dim3(static_cast<unsigned>(sh.split_items * hkv), sh.tile_rows / 4), 256, 0, s>>>(a, sh, part_rows);
+  // no sequence is long enough to be split: nothing to join
+  if (static_cast<long>(a.cache.max_pages) * a.cache.page_tokens <= static_cast<long>(sh.min_tiles) * kTileTokens) return hipGetLastError();
+  const long units = sh.split_items * hkv * sh.tile_rows;
+  attention_merge_kernel<T, DP><<<static_cast<unsigned>(units < kMergeGrid ? units : kMergeGrid), 256, 0, s>>>(a, sh, part_rows);
   return hipGetLastError();
 }
 

@@ -87,6 +87,7 @@ static_assert(sizeof(AttnItem) == 48 && sizeof(AttnMerge) == 32 && sizeof(AttnPl
 struct AttnShape {
   int group;       // query heads of a kv head
   int tile_rows;   // rows of an item
+  int min_tiles;   // key tiles of an item at least, where rows are split
   long max_tiles;  // row tiles of the batch at most
   long split_items;  // items that splitting along the keys may add, and merges, at most
   __host__ __device__ long max_items() const { return max_tiles + split_items; }

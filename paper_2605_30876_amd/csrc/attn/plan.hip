@@ -8,8 +8,11 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kMaxSeqs = 4096;
-constexpr int kSplitWorkgroups = 512;  // items that splitting aims at, all kv heads together: two per CU
-constexpr int kMinTiles = 4;           // key tiles of an item at least: one per wave
+// Items that splitting aims at, all kv heads together.
+constexpr int kSplitRows = 2048;   // items of 32 rows
+constexpr int kSplitBlock = 512;   // items of 128 rows
+constexpr int kMinRows = 8;        // key tiles of an item at least
+constexpr int kMinBlock = 4;
 
 // Exclusive prefix sums over the workgroup's threads; *total is their sum.
 template <typename V>
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   long all;
   scan_exclusive(keys, lwaves, &all);
   const long split = sh.split_items;
-  const int chunk = static_cast<int>(max(static_cast<long>(kMinTiles), (all + split - 1) / split));
+  const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + split - 1) / split));
 
   AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
   AttnItem* out = reinterpret_cast<AttnItem*>(head + 1);
@@ -148,7 +151,9 @@ AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads
   const long by_seq = n_seqs * ((most + s.tile_rows - 1) / s.tile_rows);
   const long by_rows = static_cast<long>(T) * s.group / s.tile_rows + n_seqs;
   s.max_tiles = by_seq < by_rows ? by_seq : by_rows;
-  s.split_items = kSplitWorkgroups / n_kv_heads > 1 ? kSplitWorkgroups / n_kv_heads : 1;
+  const int aim = (s.tile_rows == 32 ? kSplitRows : kSplitBlock) / n_kv_heads;
+  s.split_items = aim > 1 ? aim : 1;
+  s.min_tiles = s.tile_rows == 32 ? kMinRows : kMinBlock;
   return s;
 }
 
