@@ -270,6 +270,17 @@ struct TileMap {
   }
 };
 
+// The plan's item and whether there is one, in one round trip to memory (the
+// array is as long as the grid).
+__device__ __forceinline__ bool load_item(const AttnArgs& a, int i, AttnItem& it) {
+  typedef int i32x16 __attribute__((ext_vector_type(16)));
+  const auto* p = (const __attribute__((address_space(4))) int32_t*)a.plan;
+  const int n = p[0];
+  const i32x16 w = *(const __attribute__((address_space(4))) i32x16*)(p + sizeof(AttnPlanHead) / 4 + static_cast<long>(i) * 16);
+  it = AttnItem{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], {w[9], w[10], w[11], w[12]}, {0, 0, 0}};
+  return i < n;
+}
+
 // The item's rows of this wave: row index, head and what they see; queries loaded.
 template <typename T, int DP>
 struct RowPlace {
@@ -305,12 +316,12 @@ struct RowPlace {
     if (!live) return;
     if (it.part >= 0) {
       const long at = (static_cast<long>(it.part) * a.cache.n_kv_heads + hk) * sh.tile_rows + (row - it.first);
-      float* po = static_cast<float*>(a.workspace) + at * DP;
+      float* po = static_cast<float*>(a.workspace) + (at - (row - it.first)) * DP + partial_at(DP, row - it.first, 4 * half);
 #pragma unroll
       for (int b = 0; b < kB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<f32x4*>(po + 32 * b + tile_key(i, half)) = f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
+          store4(po + partial_at(DP, 0, 32 * b + tile_key(i, 0)), f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
       if (half == 0)
         *reinterpret_cast<float2*>(static_cast<float*>(a.workspace) + static_cast<long>(part_rows) * DP + at * 2) = make_float2(w.m, w.l);
       return;
@@ -342,10 +353,9 @@ __global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_row
   constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS;
   extern __shared__ float lds[];
   const int hkv = a.cache.n_kv_heads;
-  const AttnPlanHead* head = reinterpret_cast<const AttnPlanHead*>(a.plan);
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
-  if (item_i >= head->n_items) return;
-  const AttnItem it = plan_items(a.plan)[item_i];
+  AttnItem it;
+  if (!load_item(a, item_i, it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Rows w;
@@ -357,17 +367,19 @@ __global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_row
   Frag k[kK], v[kB][kS];
   auto load_k = [&](const T* p) {
 #pragma unroll
-    for (int j = 0; j < kK; ++j) k[j] = *reinterpret_cast<const Frag*>(p + j * 64 * c + lane * c);
+    for (int j = 0; j < kK; ++j) k[j] = __builtin_nontemporal_load(reinterpret_cast<const Frag*>(p + j * 64 * c + lane * c));
   };
   auto load_v = [&](const T* p) {
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
-      for (int s = 0; s < kS; ++s) v[b][s] = *reinterpret_cast<const Frag*>(p + (b * kS + s) * 64 * c + lane * c);
+      for (int s = 0; s < kS; ++s) v[b][s] = __builtin_nontemporal_load(reinterpret_cast<const Frag*>(p + (b * kS + s) * 64 * c + lane * c));
   };
   // page ids are known two of this wave's tiles ahead, its keys and values one
   int kt = it.kt0 + wk;
-  int page = map.page(kt, kt1), page1 = map.page(kt + kWK, kt1);
+  static_assert(kWK == 4);
+  int page = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
+  int page1 = map.page(kt + kWK, kt1);
   if (map.holds(page)) {
     load_k(map.k + map.at(kt, page));
     load_v(map.v + map.at(kt, page));
@@ -461,10 +473,9 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
   constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS, kTS = Stage::kTS;
   __shared__ Stage s0, s1;  // apart, so that reads of one do not wait for loads into the other
   const int hkv = a.cache.n_kv_heads;
-  const AttnPlanHead* head = reinterpret_cast<const AttnPlanHead*>(a.plan);
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
-  if (item_i >= head->n_items) return;
-  const AttnItem it = plan_items(a.plan)[item_i];
+  AttnItem it;
+  if (!load_item(a, item_i, it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Rows w;
@@ -552,7 +563,12 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
   // are waited for by the wave that issued them, then by all: the barrier also
   // tells that the other buffer has been read.
   int kt = it.kt0;
-  Ids pg = pages(kt), pg1 = pages(kt + kTS);
+  Ids pg, pg1;
+#pragma unroll
+  for (int n = 0; n < kTS; ++n) {
+    pg.id[n] = it.page[n];
+    pg1.id[n] = it.page[kTS + n];
+  }
   load(kt, pg, s0);
   __builtin_amdgcn_sched_barrier(0);
   auto turn = [&](auto masked, Stage& cur, Stage& fill) {
@@ -583,89 +599,107 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
   rows.store(w, a, sh, it, hk, half, part_rows);
 }
 
-// Partial results of a row tile joined: a workgroup per row, its waves on
-// every fourth piece, a wave's lanes over the head dimension and, where it is
-// short, over several pieces.
+// Partial results of a row tile joined, pieces in fixed order.  A workgroup
+// takes 8 rows, which lie side by side in every KiB of the partial sums: a
+// wave reads 128 bytes of each, lane = (16-byte piece of the KiB, row), and the
+// waves share the pieces.
+constexpr int kMergeWaves = 8, kMergeRows = 8;
+
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, AttnShape sh, int part_rows) {
-  constexpr int kLanes = DP / 4, kPar = 64 / kLanes;  // lanes of a row, pieces at once
-  __shared__ f32x4 so[4][kLanes];
-  __shared__ float2 sml[4];
+__global__ __launch_bounds__(64 * kMergeWaves) void attention_merge_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+  constexpr int kV = DP / 32;  // f32x4 of a lane: 8 lanes of a row cover 32 elements
+  __shared__ f32x4 so[kMergeWaves - 1][kV][64];
+  __shared__ float2 sml[kMergeWaves][kMergeRows];
   const int hkv = a.cache.n_kv_heads;
-  const AttnPlanHead* head = reinterpret_cast<const AttnPlanHead*>(a.plan);
+  const AttnPlanHead head = *reinterpret_cast<const AttnPlanHead*>(a.plan);
   const AttnMerge* merges = reinterpret_cast<const AttnMerge*>(plan_items(a.plan) + sh.max_items());
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane % kLanes, par = lane / kLanes;
+  const int r = lane % kMergeRows, col = lane / kMergeRows;  // row; piece of 4 elements of every 32
   const float* po = static_cast<const float*>(a.workspace);
   const float2* ml = reinterpret_cast<const float2*>(po + static_cast<long>(part_rows) * DP);
   const long step = static_cast<long>(hkv) * sh.tile_rows;
-  const int units = head->n_merges * hkv * sh.tile_rows;
+  const int groups = (head.most_rows + kMergeRows - 1) / kMergeRows;
+  const int units = head.n_merges * hkv * groups;
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
-    const int r = u % sh.tile_rows, hk = u / sh.tile_rows % hkv;
-    const AttnMerge mg = merges[u / sh.tile_rows / hkv];
-    const int row = mg.first + r;
-    if (row >= mg.rows) continue;
-    const long at = (static_cast<long>(mg.part) * hkv + hk) * sh.tile_rows + r;
-    // pieces wave, wave + 4, ...: their maximum, then their sums relative to it
-    float m = -INFINITY;
-    for (int i = wave + 4 * lane; i < mg.pieces; i += 256) m = fmaxf(m, ml[at + i * step].x);
+    const int row0 = u % groups * kMergeRows, hk = u / groups % hkv;
+    const AttnMerge mg = merges[u / groups / hkv];
+    if (mg.first + row0 >= mg.rows) continue;
+    const int row = mg.first + row0 + r;
+    const bool live = row < mg.rows;
+    const long tile = (static_cast<long>(mg.part) * hkv + hk) * sh.tile_rows;
+    const float* pr = po + tile * DP + partial_at(DP, row0 + r, 4 * col);
+    const float2* mr = ml + tile + row0 + r;
+    // online over this wave's pieces: all their loads are in flight together
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[kV];
 #pragma unroll
-    for (int x = 32; x >= 1; x /= 2) m = fmaxf(m, __shfl_xor(m, x));
-    const float off = m == -INFINITY ? 0.f : m;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-#pragma unroll 4
-    for (int i = wave + 4 * par; i < mg.pieces; i += 4 * kPar) {
-      if (par < kPar) {
-        const float2 x = ml[at + i * step];
-        const f32x4 p = *reinterpret_cast<const f32x4*>(po + (at + i * step) * DP + col * 4);
-        const float f = x.x == m ? 1.f : exp2_hw(x.x - off);
-        l += f * x.y;
-        o += f * p;
+    for (int j = 0; j < kV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int kBatch = kV <= 4 ? 4 : 2;
+    for (int i0 = wave; i0 < mg.pieces; i0 += kMergeWaves * kBatch) {
+      float2 x[kBatch];
+      f32x4 p[kBatch][kV];
+      float nm = m;
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        const int i = i0 + y * kMergeWaves;
+        x[y] = make_float2(-INFINITY, 0.f);
+        if (live && i < mg.pieces) {
+          x[y] = mr[i * step];
+#pragma unroll
+          for (int j = 0; j < kV; ++j) p[y][j] = *reinterpret_cast<const f32x4*>(pr + i * step * DP + partial_at(DP, 0, 32 * j));
+        } else {
+#pragma unroll
+          for (int j = 0; j < kV; ++j) p[y][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) nm = fmaxf(nm, x[y].x);
+      const float f0 = m == nm ? 1.f : exp2_hw(m - nm);
+      m = nm;
+      l *= f0;
+#pragma unroll
+      for (int j = 0; j < kV; ++j) o[j] *= f0;
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        const float f = x[y].x == m ? 1.f : exp2_hw(x[y].x - m);
+        l += f * x[y].y;
+#pragma unroll
+        for (int j = 0; j < kV; ++j) o[j] += f * p[y][j];
       }
     }
-    // the pieces of one wave, then of the four, in fixed order
+    __syncthreads();  // the previous unit's sums have been read
+    if (col == 0) sml[wave][r] = make_float2(m, l);
+    if (wave > 0) {
 #pragma unroll
-    for (int j = 1; j < kPar; ++j) {
-      const int from = (lane + j * kLanes) & 63;
-      const float ol = __shfl(l, from);
-      f32x4 oo;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) oo[t] = __shfl(o[t], from);
-      if (par == 0) {
-        l += ol;
-        o += oo;
-      }
+      for (int j = 0; j < kV; ++j) so[wave - 1][j][lane] = o[j];
     }
     __syncthreads();
-    if (par == 0) {
-      so[wave][col] = o;
-      if (col == 0) sml[wave] = make_float2(m, l);
-    }
-    __syncthreads();
-    if (wave != 0 || par != 0) continue;
+    if (wave != 0 || !live) continue;
     float mm = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mm = fmaxf(mm, sml[i].x);
-    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < kMergeWaves; ++i) mm = fmaxf(mm, sml[i][r].x);
     l = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float f = sml[i].x == mm ? 1.f : exp2_hw(sml[i].x - mm);
-      l += f * sml[i].y;
-      o += f * so[i][col];
+    for (int i = 0; i < kMergeWaves; ++i) {
+      const float2 x = sml[i][r];
+      const float f = x.x == mm ? 1.f : exp2_hw(x.x - mm);
+      l += f * x.y;
+#pragma unroll
+      for (int j = 0; j < kV; ++j) o[j] = i == 0 ? f * o[j] : o[j] + f * so[i > 0 ? i - 1 : 0][j][lane];
     }
     const bool some = l > 0.f || l != l;
     const float inv = some ? 1.f / l : 0.f;
     const int tok = row / sh.group, qh = hk * sh.group + row - tok * sh.group;
     T* op = static_cast<T*>(a.out) + (mg.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim + col * 4;
-    if (col * 4 < a.cache.head_dim) store4(op, o * inv);
+#pragma unroll
+    for (int j = 0; j < kV; ++j)
+      if (32 * j + col * 4 < a.cache.head_dim) store4(op + 32 * j, o[j] * inv);
     if (a.lse && col == 0)
       a.lse[static_cast<long>(mg.row0 + tok) * a.n_heads + qh] = some ? (mm + log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
-constexpr long kMergeGrid = 2048;
+constexpr long kMergeGrid = 1024;
 
 template <typename T, int DP>
 hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
@@ -680,8 +714,8 @@ hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
   }
   // no sequence is long enough to be split: nothing to join
   if (static_cast<long>(a.cache.max_pages) * a.cache.page_tokens <= static_cast<long>(sh.min_tiles) * kTileTokens) return hipGetLastError();
-  const long units = sh.split_items * hkv * sh.tile_rows;
-  attention_merge_kernel<T, DP><<<static_cast<unsigned>(units < kMergeGrid ? units : kMergeGrid), 256, 0, s>>>(a, sh, part_rows);
+  const long units = sh.split_items * hkv * (sh.tile_rows / kMergeRows);
+  attention_merge_kernel<T, DP><<<static_cast<unsigned>(units < kMergeGrid ? units : kMergeGrid), 64 * kMergeWaves, 0, s>>>(a, sh, part_rows);
   return hipGetLastError();
 }
 

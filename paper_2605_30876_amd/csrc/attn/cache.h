@@ -70,6 +70,7 @@ struct AttnItem {
   int first, rows;            // first row of the tile, rows of the sequence
   int kt0, kt1;               // key tiles of 32 tokens
   int part;                   // partial result, or -1: the only item of its rows
+  int page[4];                // pages of the first key tiles (-1: none), known before the table could be
   int pad[3];
 };
 struct AttnMerge {
@@ -78,9 +79,10 @@ struct AttnMerge {
   int pad[3];
 };
 struct AttnPlanHead {
-  int n_items, n_merges, pad[2];
+  int n_items, n_merges;
+  int most_pieces, most_rows;  // of the row tiles to merge
 };
-static_assert(sizeof(AttnItem) == 48 && sizeof(AttnMerge) == 32 && sizeof(AttnPlanHead) == 16);
+static_assert(sizeof(AttnItem) == 64 && sizeof(AttnMerge) == 32 && sizeof(AttnPlanHead) == 16);
 
 // What the host knows of a plan: the kernel's row tile and the bounds that
 // size its arrays and grids.
@@ -103,9 +105,17 @@ __host__ __device__ inline const AttnItem* plan_items(const int32_t* plan) {
   return reinterpret_cast<const AttnItem*>(plan + sizeof(AttnPlanHead) / sizeof(int));
 }
 // Partial results of max_parts row tiles of every kv head: [part][kv head] of
-// tile_rows x dp sums, then as many (maximum, sum) pairs.
+// tile_rows x dp sums in the order in which the lanes hold them (partial_at),
+// then as many (maximum, sum) pairs.
 inline size_t attn_workspace_bytes(const AttnShape& s, int n_kv_heads, int dp) {
   return static_cast<size_t>(s.max_parts()) * n_kv_heads * s.tile_rows * (dp + 2) * sizeof(float);
+}
+
+// Floats from the start of a row tile's sums to the four of row r, elements
+// d .. d+3: the waves' 32 rows one after another, each stored as it lies in
+// the registers, 16 bytes a lane, so that a store is one contiguous KiB.
+__host__ __device__ constexpr int partial_at(int dp, int r, int d) {
+  return r / 32 * (32 * dp) + (d / 8 * 64 + d / 4 % 2 * 32 + r % 32) * 4;
 }
 
 struct AttnArgs {

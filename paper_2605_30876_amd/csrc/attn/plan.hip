@@ -6,12 +6,13 @@ namespace dmoe {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 256;
 constexpr int kMaxSeqs = 4096;
-// Items that splitting aims at, all kv heads together.
-constexpr int kSplitRows = 2048;   // items of 32 rows
-constexpr int kSplitBlock = 512;   // items of 128 rows
-constexpr int kMinRows = 8;        // key tiles of an item at least
+constexpr int kKeptSeqs = 512;  // sequences kept in LDS; further ones are read again
+// Items that splitting aims at, all kv heads together, and their key tiles at least.
+constexpr int kSplitRows = 1024;  // items of 32 rows
+constexpr int kSplitBlock = 512;  // items of 128 rows: as many workgroups as the device holds at once
+constexpr int kMinRows = 8;
 constexpr int kMinBlock = 4;
 
 // Exclusive prefix sums over the workgroup's threads; *total is their sum.
@@ -27,6 +28,7 @@ __device__ __forceinline__ V scan_exclusive(V v, V* waves, V* total) {
   if (lane == 63) waves[wave] = x;
   __syncthreads();
   V base = 0, sum = 0;
+#pragma unroll
   for (int i = 0; i < kThreads / 64; ++i) {
     base += i < wave ? waves[i] : 0;
     sum += waves[i];
@@ -55,31 +57,26 @@ struct Tile {
   int first, rows, kt;
 };
 
-__device__ __forceinline__ Tile load_tile(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
-                                          const int* tiles, int t) {
-  Tile r;
-  const int i = find(tiles, b.n_seqs, t);
-  r.q = load_seq(c, b, i);
-  r.rows = r.q.n * sh.group;
-  r.first = (t - tiles[i]) * sh.tile_rows;
-  const int last = min(r.first + sh.tile_rows, r.rows) - 1;
-  r.kt = (visible_end(r.q.pos0 + last / sh.group, r.q.len, mask_block) + kTileTokens - 1) / kTileTokens;
-  return r;
-}
-
 __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch b, AttnShape sh, int mask_block, int32_t* plan) {
   __shared__ int tiles[kMaxSeqs + 1];  // row tiles before each sequence
+  __shared__ Seq seqs[kKeptSeqs];
+  __shared__ Tile tile[kThreads];
   __shared__ int items[kThreads + 1];  // items before each row tile of a pass
   __shared__ int parts[kThreads];
-  __shared__ Tile tile[kThreads];
   __shared__ int iwaves[kThreads / 64];
   __shared__ long lwaves[kThreads / 64];
+  __shared__ int most[2];  // of the split row tiles: pieces, rows
   const int tid = threadIdx.x;
+  if (tid < 2) most[tid] = 0;
   int n_tiles = 0;
   for (int i0 = 0; i0 < b.n_seqs; i0 += kThreads) {
     const int i = i0 + tid;
     int n = 0;
-    if (i < b.n_seqs) n = static_cast<int>((static_cast<long>(load_seq(c, b, i).n) * sh.group + sh.tile_rows - 1) / sh.tile_rows);
+    if (i < b.n_seqs) {
+      const Seq q = load_seq(c, b, i);
+      if (i < kKeptSeqs) seqs[i] = q;
+      n = static_cast<int>((static_cast<long>(q.n) * sh.group + sh.tile_rows - 1) / sh.tile_rows);
+    }
     int total;
     const int at = scan_exclusive(n, iwaves, &total);
     if (i < b.n_seqs) tiles[i] = n_tiles + at;
@@ -89,55 +86,80 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   n_tiles = min(n_tiles, static_cast<int>(sh.max_tiles));
   if (tid == 0) tiles[b.n_seqs] = n_tiles;
   __syncthreads();
-
-  long keys = 0;
-  for (int t = tid; t < n_tiles; t += kThreads) keys += load_tile(c, b, sh, mask_block, tiles, t).kt;
+  // longest rows first under a causal mask: the last tiles see the most keys
+  auto load_tile = [&](int t) {
+    Tile r{};
+    if (t >= n_tiles) return r;
+    t = n_tiles - 1 - t;
+    const int i = find(tiles, b.n_seqs, t);
+    r.q = i < kKeptSeqs ? seqs[i] : load_seq(c, b, i);
+    r.rows = r.q.n * sh.group;
+    r.first = (t - tiles[i]) * sh.tile_rows;
+    const int last = min(r.first + sh.tile_rows, r.rows) - 1;
+    r.kt = (visible_end(r.q.pos0 + last / sh.group, r.q.len, mask_block) + kTileTokens - 1) / kTileTokens;
+    return r;
+  };
+  Tile r = load_tile(tid);
+  long keys = r.kt;
+  for (int t = tid + kThreads; t < n_tiles; t += kThreads) keys += load_tile(t).kt;
   long all;
   scan_exclusive(keys, lwaves, &all);
+  // Pieces of `chunk` key tiles: sum ceil(kt / chunk) <= n_tiles + all / chunk
+  // fills the aim but does not pass it.  With row tiles of about one length
+  // that are more than half of the aim nothing is split: one round of
+  // workgroups either way, and no partial results.  At least all / split: the arrays' size.
   const long split = sh.split_items;
-  const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + split - 1) / split));
+  const long room = max(max(split - n_tiles, split / 2), 1l);
+  const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + room - 1) / room));
 
   AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
   AttnItem* out = reinterpret_cast<AttnItem*>(head + 1);
   AttnMerge* merges = reinterpret_cast<AttnMerge*>(out + sh.max_items());
   int n_items = 0, n_parts = 0, n_merges = 0;
-  // longest rows first under a causal mask: the last tiles see the most keys
   for (int t0 = 0; t0 < n_tiles; t0 += kThreads) {
-    const int t = n_tiles - 1 - (t0 + tid);
-    int pieces = 0;
-    if (t >= 0) {
-      tile[tid] = load_tile(c, b, sh, mask_block, tiles, t);
-      pieces = max(1, (tile[tid].kt + chunk - 1) / chunk);
-    }
-    int total, ptotal, mtotal;
-    const int at = scan_exclusive(pieces, iwaves, &total);
-    const int pat = scan_exclusive(pieces > 1 ? pieces : 0, iwaves, &ptotal);
-    const int mat = scan_exclusive(pieces > 1 ? 1 : 0, iwaves, &mtotal);
-    items[tid] = at;
-    parts[tid] = pieces > 1 ? n_parts + pat : -1;
+    if (t0 > 0) r = load_tile(t0 + tid);
+    const int pieces = t0 + tid < n_tiles ? max(1, (r.kt + chunk - 1) / chunk) : 0;
+    tile[tid] = r;
+    // three sums at once, 21 bits each: a pass has at most kThreads + split items
+    const long mine = pieces | (pieces > 1 ? static_cast<long>(pieces) << 21 | 1l << 42 : 0);
+    long sum;
+    const long at = scan_exclusive(mine, lwaves, &sum);
+    constexpr long kBits = (1 << 21) - 1;
+    const int total = static_cast<int>(sum & kBits);
+    const int part = n_parts + static_cast<int>(at >> 21 & kBits);
+    items[tid] = static_cast<int>(at & kBits);
+    parts[tid] = pieces > 1 ? part : -1;
     if (pieces > 1) {
-      const Tile& r = tile[tid];
-      merges[n_merges + mat] = AttnMerge{r.q.row0, r.first, r.rows, n_parts + pat, pieces, {0, 0, 0}};
+      merges[n_merges + (at >> 42)] = AttnMerge{r.q.row0, r.first, r.rows, part, pieces, {0, 0, 0}};
+      atomicMax(&most[0], pieces);
+      atomicMax(&most[1], min(sh.tile_rows, r.rows - r.first));
     }
     if (tid == 0) items[kThreads] = total;
     __syncthreads();
     for (int x = tid; x < total; x += kThreads) {
       const int j = find(items, kThreads, x);
-      const Tile& r = tile[j];
-      const int p = x - items[j], n = max(1, (r.kt + chunk - 1) / chunk);
-      AttnItem it{r.q.slot, r.q.row0, r.q.n, r.q.len, r.first, r.rows, 0, 0, parts[j] < 0 ? -1 : parts[j] + p, {0, 0, 0}};
-      it.kt0 = static_cast<int>(static_cast<long>(r.kt) * p / n);
-      it.kt1 = static_cast<int>(static_cast<long>(r.kt) * (p + 1) / n);
+      const Tile& u = tile[j];
+      const int p = x - items[j], n = max(1, (u.kt + chunk - 1) / chunk);
+      AttnItem it{u.q.slot, u.q.row0, u.q.n, u.q.len, u.first, u.rows, 0, 0, parts[j] < 0 ? -1 : parts[j] + p, {}, {0, 0, 0}};
+      it.kt0 = static_cast<int>(static_cast<long>(u.kt) * p / n);
+      it.kt1 = static_cast<int>(static_cast<long>(u.kt) * (p + 1) / n);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        it.page[i] = it.kt0 + i < it.kt1
+                         ? c.table[static_cast<long>(u.q.slot) * c.max_pages + (it.kt0 + i) * kTileTokens / c.page_tokens]
+                         : -1;
       out[n_items + x] = it;
     }
     n_items += total;
-    n_parts += ptotal;
-    n_merges += mtotal;
+    n_parts += static_cast<int>(sum >> 21 & kBits);
+    n_merges += static_cast<int>(sum >> 42);
     __syncthreads();
   }
   if (tid == 0) {
     head->n_items = n_items;
     head->n_merges = n_merges;
+    head->most_pieces = most[0];
+    head->most_rows = most[1];
   }
 }
 
