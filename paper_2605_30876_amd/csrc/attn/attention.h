@@ -164,8 +164,9 @@ struct WaveRows {
 
   // For a tile in which some row does not see every key: values that no row
   // of the wave sees are not the sequence's, or a later token's, and become 0,
-  // whatever they are.  True if the rest is finite; a value that some rows see
-  // and others do not must not reach the others through 0 * value.
+  // whatever they are.  True if the rest is finite: a value that some rows see
+  // and others do not must not reach the others through 0 * value, so a tile
+  // with one that is not is left to add_by_key.
   __device__ __forceinline__ bool cut(Frag (&v)[kB][kS], int key0, int half) const {
     const int seen = hi - key0;
     uint32_t top = 0;
@@ -200,8 +201,42 @@ struct WaveRows {
     return __builtin_bit_cast(Frag, make_uint4(u.x & (word == 0 ? bits : 0), u.y & (word == 1 ? bits : 0), u.z & (word == 2 ? bits : 0),
                                                u.w & (word == 3 ? bits : 0)));
   }
-  // Such a tile key by key: a key's products are added to the rows that see it.
-  __device__ __forceinline__ void add_by_key(const f32x16& p, const Frag (&v)[kB][kS], int key0, int half) {
+  // Such tiles among kt, kt + step, ..., once the running maximum is the last
+  // one: a key's products are added to the rows that see it.
+  template <typename Map>
+  __device__ __forceinline__ void add_by_key(const Map& map, int kt, int kt1, int step, float scale2, int half) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (; kt < kt1; kt += step) {
+      const int page = map.page(kt, kt1), key0 = kt * kTileTokens;
+      if (!map.holds(page) || key0 >= hi) continue;
+      const long at = map.at(kt, page);
+      Frag v[kB][kS];
+      load(v, map.v + at, lane);
+      if (cut(v, key0, half)) continue;
+      f32x16 s;
+      {
+        Frag k[kK];
+        load(k, map.k + at, lane);
+        s = scores(k);
+      }
+      const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = tile_key(i, half) < end - key0 ? exp2_hw(__builtin_fmaf(s[i], scale2, -off)) : 0.f;
+      add_keys(s, v, key0, half);
+    }
+  }
+  static __device__ __forceinline__ void load(Frag (&k)[kK], const T* p, int lane) {
+#pragma unroll
+    for (int j = 0; j < kK; ++j) k[j] = *reinterpret_cast<const Frag*>(p + j * 64 * c + lane * c);
+  }
+  static __device__ __forceinline__ void load(Frag (&v)[kB][kS], const T* p, int lane) {
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int s = 0; s < kS; ++s) v[b][s] = *reinterpret_cast<const Frag*>(p + (b * kS + s) * 64 * c + lane * c);
+  }
+  __device__ __forceinline__ void add_keys(const f32x16& p, const Frag (&v)[kB][kS], int key0, int half) {
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       const Frag f = Ty::probs(p, s);
@@ -237,10 +272,9 @@ struct WaveRows {
   }
 };
 
-// Waves a SIMD holds: two where the sums, the queries and a tile fit half of its registers.
 template <typename T>
 constexpr int waves_per_simd(int dp) {
-  return dp * sizeof(T) <= 256 ? 2 : 1;
+  return two_per_cu(sizeof(T) == 4 ? DMOE_F32 : DMOE_BF16, dp) ? 2 : 1;
 }
 
 // Where a sequence's tiles of one kv head lie.
@@ -384,6 +418,7 @@ __global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_row
     load_k(map.k + map.at(kt, page));
     load_v(map.v + map.at(kt, page));
   }
+  bool left = false;  // tiles for add_by_key
   auto turn = [&](auto masked) {
     const int page2 = map.page(kt + 2 * kWK, kt1);
     const bool here = map.holds(page), more = map.holds(page1);
@@ -394,10 +429,10 @@ __global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_row
     if (here) {
       const int key0 = kt * kTileTokens;
       w.template softmax<1>(s, scale2, key0, masked, half);
-      if (masked && !w.cut(v, key0, half))
-        w.add_by_key(s[0], v, key0, half);
-      else
+      if (!masked || w.cut(v, key0, half))
         w.add(s[0], v);
+      else
+        left = true;
     }
     if (more) load_v(map.v + at1);
     kt += kWK;
@@ -407,7 +442,9 @@ __global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_row
   // tiles that every row sees whole, then the others
   const int whole = min(kt1, w.lo / kTileTokens);
   while (kt < whole) turn(std::false_type());
+  const int first_masked = kt;
   while (kt < kt1) turn(std::true_type());
+  if (left) w.add_by_key(map, first_masked, kt1, kWK, scale2, half);
   w.l = other_half_sum(w.l);
 
   // join the waves two by two: the upper ones hand their sums to the lower
@@ -507,20 +544,19 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
 #pragma unroll
     for (int j = 0; j < kShare; ++j) dma16(p + (j0 + j) * 64 * c, &st.f[n][kv][j0 + j][0]);
   };
-  auto compute = [&](auto masked, int kt, const Ids& pg, const Stage& st) {
+  // A stage that every row sees whole; its tiles may still lie on no page, or
+  // behind the item's last.
+  auto compute = [&](std::false_type, int kt, const Ids& pg, const Stage& st) {
     if (!rows.any) return;
-    // tiles that are there, and that some row of the wave sees
     bool on[kTS];
     bool all = true, none = true;
 #pragma unroll
     for (int n = 0; n < kTS; ++n) {
       on[n] = map.holds(pg.id[n]);
-      if (masked) on[n] = on[n] && (kt + n) * kTileTokens < w.hi;
       all = all && on[n];
       none = none && !on[n];
     }
     if (none) return;
-    const int key0 = kt * kTileTokens;
     f32x16 s[kTS];
 #pragma unroll
     for (int n = 0; n < kTS; ++n) {
@@ -535,28 +571,42 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[n][i] = on[n] ? s[n][i] : -INFINITY;
     }
-    w.template softmax<kTS>(s, scale2, key0, masked, half);
+    w.template softmax<kTS>(s, scale2, kt * kTileTokens, false, half);
 #pragma unroll
     for (int n = 0; n < kTS; ++n) {
       if (!on[n]) continue;
-      if constexpr (masked) {
-        Frag v[kB][kS];
 #pragma unroll
-        for (int b = 0; b < kB; ++b)
+      for (int x = 0; x < kS; ++x) {
+        const Frag f = Types<T>::probs(s[n], x);
 #pragma unroll
-          for (int x = 0; x < kS; ++x) v[b][x] = st.f[n][1][b * kS + x][lane];
-        if (w.cut(v, key0 + n * kTileTokens, half))
-          w.add(s[n], v);
-        else
-          w.add_by_key(s[n], v, key0 + n * kTileTokens, half);
-      } else {
-#pragma unroll
-        for (int x = 0; x < kS; ++x) {
-          const Frag f = Types<T>::probs(s[n], x);
-#pragma unroll
-          for (int b = 0; b < kB; ++b) Types<T>::mma(w.o[b], st.f[n][1][b * kS + x][lane], f);
-        }
+        for (int b = 0; b < kB; ++b) Types<T>::mma(w.o[b], st.f[n][1][b * kS + x][lane], f);
       }
+    }
+  };
+  // Any stage, tile by tile (registers are short where values are cut).
+  bool left = false;  // tiles for add_by_key
+  auto compute_masked = [&](int kt, const Ids& pg, const Stage& st) {
+#pragma unroll
+    for (int n = 0; n < kTS; ++n) {
+      const int key0 = (kt + n) * kTileTokens;
+      if (!map.holds(pg.id[n]) || key0 >= w.hi) continue;
+      f32x16 s[1];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kK; ++j) Types<T>::mma(s[0], st.f[n][0][j][lane], w.q[j]);
+      w.template softmax<1>(s, scale2, key0, true, half);
+      __builtin_amdgcn_sched_barrier(0);
+      Frag v[kB][kS];
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int x = 0; x < kS; ++x) v[b][x] = st.f[n][1][b * kS + x][lane];
+      if (w.cut(v, key0, half))
+        w.add(s[0], v);
+      else
+        left = true;
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   // page ids are known two stages ahead, keys and values one.  A stage's loads
@@ -578,23 +628,31 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
     load(kt + kTS, pg1, fill);
     const Ids pg2 = pages(kt + 2 * kTS);
     __builtin_amdgcn_sched_barrier(0);
-    compute(masked, kt, pg, cur);
+    if constexpr (masked)
+      compute_masked(kt, pg, cur);
+    else
+      compute(masked, kt, pg, cur);
     __builtin_amdgcn_sched_barrier(0);
     kt += kTS;
     pg = pg1;
     pg1 = pg2;
   };
-  // pairs of stages whose keys every row of the workgroup sees, then the others
-  const int whole = min(it.kt1, visible_end(it.len - it.n + it.first / sh.group, it.len, a.mask_block) / kTileTokens);
-  while (kt + 2 * kTS <= whole) {
+  // stages whose keys every row of the workgroup sees, then the others
+  const int whole = visible_end(it.len - it.n + it.first / sh.group, it.len, a.mask_block) / kTileTokens;
+  int stages = whole >= it.kt1 ? (it.kt1 - kt + kTS - 1) / kTS : max(whole - kt, 0) / kTS;
+  const int first_masked = kt + stages * kTS;
+  for (; stages >= 2; stages -= 2) {
     turn(std::false_type(), s0, s1);
     turn(std::false_type(), s1, s0);
   }
-  while (kt < it.kt1) {
-    turn(std::true_type(), s0, s1);
-    if (kt >= it.kt1) break;
-    turn(std::true_type(), s1, s0);
+  if (stages) turn(std::false_type(), s0, s1);
+  for (bool odd = stages; kt < it.kt1; odd = !odd) {
+    if (odd)
+      turn(std::true_type(), s1, s0);
+    else
+      turn(std::true_type(), s0, s1);
   }
+  if (left) w.add_by_key(map, first_masked, it.kt1, 1, scale2, half);
   w.l = other_half_sum(w.l);
   rows.store(w, a, sh, it, hk, half, part_rows);
 }

@@ -92,9 +92,12 @@ struct AttnShape {
   int min_tiles;   // key tiles of an item at least, where rows are split
   long max_tiles;  // row tiles of the batch at most
   long split_items;  // items that splitting along the keys may add, and merges, at most
+  int aim;           // items that splitting aims at: at most split_items
   __host__ __device__ long max_items() const { return max_tiles + split_items; }
   __host__ __device__ long max_parts() const { return 2 * split_items; }
 };
+// Two workgroups of the block kernel fit a CU where a wave's registers fit half of a SIMD's.
+constexpr bool two_per_cu(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) <= 256; }
 AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
 
 inline size_t plan_ints(const AttnShape& s) {

@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   // fills the aim but does not pass it.  With row tiles of about one length
   // that are more than half of the aim nothing is split: one round of
   // workgroups either way, and no partial results.  At least all / split: the arrays' size.
-  const long split = sh.split_items;
+  const long split = sh.aim;
   const long room = max(max(split - n_tiles, split / 2), 1l);
   const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + room - 1) / room));
 
@@ -174,13 +174,16 @@ AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads
   const long by_rows = static_cast<long>(T) * s.group / s.tile_rows + n_seqs;
   s.max_tiles = by_seq < by_rows ? by_seq : by_rows;
   const int aim = (s.tile_rows == 32 ? kSplitRows : kSplitBlock) / n_kv_heads;
-  s.split_items = aim > 1 ? aim : 1;
+  s.aim = aim > 1 ? aim : 1;
+  s.split_items = s.aim;
   s.min_tiles = s.tile_rows == 32 ? kMinRows : kMinBlock;
   return s;
 }
 
-hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
+hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& shape, int mask_block,
                                  int32_t* plan, hipStream_t s) {
+  AttnShape sh = shape;
+  if (sh.tile_rows > 32 && !two_per_cu(c.dt, padded_dim(c.head_dim))) sh.aim = sh.aim > 1 ? sh.aim / 2 : 1;
   plan_kernel<<<1, kThreads, 0, s>>>(c, b, sh, mask_block, plan);
   return hipGetLastError();
 }
