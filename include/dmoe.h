@@ -595,7 +595,7 @@ dmoe_status dmoe_rope_turns(int rot_dim, double base, dmoe_rope_scaling scaling,
  * same stride, else they must not overlap.  inverse: turned the other way
  * (a -> -a, the same scale): the gradient with respect to x of a forward call,
  * given the gradient of its output.
- * Limits: T, n_heads >= 1; head_dim a multiple of 8 in [8, 256].
+ * Limits: T >= 1; 1 <= n_heads <= 65535; head_dim a multiple of 8 in [8, 256].
  */
 dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, dmoe_dtype dt, int T, int n_heads,
                       int head_dim, const int32_t* positions, dmoe_rotary rope, int inverse, void* stream);
@@ -668,7 +668,7 @@ typedef struct dmoe_batch {
  * denoised over several steps) overwrites them.  Strides in elements between
  * rows, multiples of 16 bytes.  Two sequences of a batch must not be the same
  * slot.
- * Limits: n_heads a multiple of n_kv_heads up to 1024 * n_kv_heads if q is set.
+ * Limits: n_heads a multiple of n_kv_heads, up to 1024 * n_kv_heads and 8192, if q is set.
  */
 dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch batch, const void* k, long k_stride,
                               const void* v, long v_stride, const void* q, long q_stride, void* q_out,

@@ -146,7 +146,7 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
   REQUIRE(valid_head_dim(head_dim), "head_dim=%d must be a multiple of 8 in [8, 256]", head_dim);
   const long width = static_cast<long>(n_heads) * head_dim;
   REQUIRE(width <= kIntLimit, "n_heads*head_dim must fit in int32");
-  SUPPORT(n_heads <= 65536, "n_heads=%d must be at most 65536", n_heads);
+  SUPPORT(n_heads <= 65535, "n_heads=%d must be at most 65535", n_heads);
   FORWARD(check_rope(__func__, rope, head_dim));
   ROWS(x, x_stride, width, dt);
   ROWS(out, out_stride, width, dt);
@@ -181,6 +181,7 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
   if (q) {
     FORWARD(check_heads(__func__, batch.T, n_heads, cache->n_kv_heads));
     const long width = static_cast<long>(n_heads) * cache->head_dim;
+    SUPPORT(n_heads <= 8192, "n_heads=%d must be at most 8192", n_heads);
     ROWS(q, q_stride, width, cache->dt);
     ROWS(q_out, q_out_stride, width, cache->dt);
     REQUIRE((q == q_out && q_stride == q_out_stride) ||

@@ -103,11 +103,11 @@ def test_refused_calls_change_nothing(gpu_lib):
     assert int(b.c.status[0]) == -1 and torch.equal(b.c.refs, refs) and int(b.c.lens[0]) == 60
 
 
-@pytest.mark.parametrize("seed", range(4))
+@pytest.mark.parametrize("seed", range(6))
 def test_random_calls(gpu_lib, seed):
     r = random.Random(seed)
     slots, max_pages, page = r.choice([(5, 6, 32), (40, 5, 64), (9, 20, 32)])
-    b = Both(r.choice([25, 60, 130]), page, slots, max_pages, layers=r.choice([1, 3]), dtype=r.choice([torch.bfloat16, torch.float32]))
+    b = Both(r.choice([25, 60, 130]) if seed < 4 else 13000, page, slots, max_pages, layers=r.choice([1, 3]), dtype=r.choice([torch.bfloat16, torch.float32]))
     for _ in range(25):
         n = r.randint(1, slots)
         dst = r.sample(range(slots), n)
@@ -122,9 +122,10 @@ def test_random_calls(gpu_lib, seed):
             b.update(dst, [min(max_pages * page, k + r.randint(0, 40)) for k in keep], src, keep)
 
 
-def test_many_entries_and_pages(gpu_lib):
-    """More entries than threads, and more pages than a thread each."""
-    b = Both(9000, 32, 1500, 6, layers=1)
+@pytest.mark.parametrize("pages", [9000, 20000])
+def test_many_entries_and_pages(gpu_lib, pages):
+    """More entries than threads, and pools whose counts fit LDS and do not."""
+    b = Both(pages, 32, 1500, 6, layers=1)
     r = random.Random(1)
     b.update(list(range(1500)), [r.randint(0, 150) for _ in range(1500)])
     src = [r.randrange(1500) for _ in range(1400)]
