@@ -1,9 +1,10 @@
 // Rotary positions, and the store of a step's keys and values into the paged
 // cache with the rotation fused in.
 //
-// A workgroup takes 8 tokens of a few heads: it forms cos and sin of (token,
-// pair) once in LDS and uses them for all of its heads, a 16-byte chunk per
-// thread and row, the loads of several rows in flight together.  The work is
+// A thread takes the same two 16-byte chunks (a row's pairs lie in chunks that
+// belong together) of one token in one head after another, so that a pair's
+// cos and sin are formed once, in registers, for all of its heads; no two
+// lanes load the same bytes and nothing passes through LDS.  The work is
 // bytes: every element is read and written once.
 #include "cache.h"
 
@@ -12,29 +13,14 @@ namespace dmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 8;      // of a workgroup that rotates
-constexpr int kInFlight = 4;    // rows a thread loads before it stores
+constexpr int kTokens = 8;    // of a workgroup that rotates: 128 bytes of a page's keys
+constexpr int kInFlight = 2;  // heads a thread loads before it stores (4: 67 against 59 us for 8000 prompt tokens)
 
 template <typename T>
 struct alignas(16) Chunk {
   static constexpr int c = 16 / sizeof(T);
   T v[c];
 };
-
-// cos and sin, times the scale, of every pair of `n` tokens; pos(i): position
-// of token i.
-template <typename Pos>
-__device__ __forceinline__ void form_angles(float2* cs, const dmoe_rotary& r, int n, bool inverse, Pos pos) {
-  const int pairs = r.rot_dim / 2;
-  for (int x = threadIdx.x; x < n * pairs; x += kThreads) {
-    const int i = x / pairs, f = x - i * pairs;
-    double turn = static_cast<double>(pos(i)) * r.turns[f];
-    turn -= rint(turn);  // [-1/2, 1/2]: the float32 below is off by 2^-26 turns at most
-    float s, co;
-    sincospif(2.f * static_cast<float>(turn), &s, &co);
-    cs[x] = make_float2(co * r.scale, (inverse ? -s : s) * r.scale);
-  }
-}
 
 // A chunk's values in float32, and rounded back (to nearest even, by the
 // conversion instruction).
@@ -54,91 +40,146 @@ __device__ __forceinline__ Chunk<bf16_t> narrow(const float (&f)[8]) {
   return __builtin_bit_cast(Chunk<bf16_t>, v);
 }
 
-// One chunk of a head, elements d0 .. d0 + c-1, rotated: `x` holds the head.
-// Everything is loaded before the caller stores, so x may be the output.
-template <typename T>
-__device__ __forceinline__ Chunk<T> rotated(const T* x, int d0, const float2* cs, int rot, bool interleaved) {
-  constexpr int c = Chunk<T>::c;
-  const Chunk<T> a = *reinterpret_cast<const Chunk<T>*>(x + d0);
-  if (d0 >= rot) return a;
-  float u[c];
-  widen(a, u);
-  if (interleaved) {
-#pragma unroll
-    for (int e = 0; e < c; e += 2) {
-      const bool in = d0 + e < rot;  // rot is even: a pair is in or out
-      const float2 t = cs[in ? (d0 + e) / 2 : 0];
-      const float x1 = u[e], x2 = u[e + 1];
-      u[e] = in ? x1 * t.x - x2 * t.y : x1;
-      u[e + 1] = in ? x2 * t.x + x1 * t.y : x2;
-    }
-    return narrow(u);
-  }
-  const int hr = rot / 2;
-  float w[c];
-  if (hr % c == 0) {
-    // a chunk lies in one half, its partner is a chunk
-    const bool low = d0 < hr;
-    widen(*reinterpret_cast<const Chunk<T>*>(x + (low ? d0 + hr : d0 - hr)), w);
-    const float2* t = cs + (low ? d0 : d0 - hr);
-#pragma unroll
-    for (int e = 0; e < c; ++e) u[e] = u[e] * t[e].x + (low ? -w[e] : w[e]) * t[e].y;
-    return narrow(u);
-  }
-#pragma unroll
-  for (int e = 0; e < c; ++e) {
-    const int d = d0 + e;
-    if (d < rot) {
-      const float2 t = cs[d < hr ? d : d - hr];
-      w[e] = load_as_f32<T>(x + (d < hr ? d + hr : d - hr));
-      u[e] = u[e] * t.x + (d < hr ? -w[e] : w[e]) * t.y;
-    }
-  }
-  return narrow(u);
-}
+// A thread's share of a row: two chunks and what their elements are turned by.
+// kAligned: interleaved pairs, or halves of whole chunks: element e of the one
+// chunk pairs with element e of the other (interleaved: 2c consecutive
+// elements, pairs within).  Otherwise the halves' border lies within a chunk,
+// and an element's partner is read by itself.
+template <typename T, bool kAligned>
+struct Unit {
+  static constexpr int c = Chunk<T>::c;
+  static constexpr int kPairs = kAligned ? c : 2 * c;  // cos and sin kept: per pair, or per element
+  int c0, c1;       // chunks of the row
+  bool turned;      // some element of them is rotated
+  float co[kPairs], si[kPairs];
 
-// n tokens of `heads` heads through the rotation; in(i, h) and out(i, h, j):
-// a head's elements, and where its chunk j goes (nullptr: nowhere).  A row's
+  __device__ __forceinline__ Unit(int u, const dmoe_rotary& r) {
+    const int hr = r.rot_dim / 2, n = hr / c;
+    const bool halves = kAligned && !r.interleaved;
+    c0 = halves && u < n ? u : 2 * u;
+    c1 = halves && u < n ? u + n : 2 * u + 1;
+    turned = r.turns && (halves ? u < n : 2 * c * u < r.rot_dim);
+  }
+  // pair (aligned) or element (otherwise) e's frequency; -1: not rotated
+  __device__ __forceinline__ int pair_of(int e, const dmoe_rotary& r) const {
+    const int hr = r.rot_dim / 2;
+    if constexpr (kAligned) return r.interleaved ? (c * (c0 / 2) + e < hr ? c * (c0 / 2) + e : -1) : c * c0 + e;
+    const int d = c * c0 + e;
+    return d < hr ? d : d < 2 * hr ? d - hr : -1;
+  }
+  __device__ __forceinline__ void form(int position, const dmoe_rotary& r, bool inverse) {
+    if (!turned) return;
+    double f[kPairs];  // all on their way together
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) f[e] = r.turns[max(pair_of(e, r), 0)];
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) {
+      double turn = static_cast<double>(position) * f[e];
+      turn -= rint(turn);  // [-1/2, 1/2]: the float32 below is off by 2^-26 turns at most
+      float s, q;
+      sincospif(2.f * static_cast<float>(turn), &s, &q);
+      co[e] = q * r.scale;
+      si[e] = (inverse ? -s : s) * r.scale;
+    }
+  }
+  struct Loaded {
+    Chunk<T> a, b;
+    T partner[kAligned ? 1 : 2 * c];
+  };
+  __device__ __forceinline__ Loaded load(const T* x, int chunks, const dmoe_rotary& r) const {
+    Loaded l;
+    l.a = c0 < chunks ? *reinterpret_cast<const Chunk<T>*>(x + c0 * c) : Chunk<T>{};
+    l.b = c1 < chunks ? *reinterpret_cast<const Chunk<T>*>(x + c1 * c) : Chunk<T>{};
+    if constexpr (!kAligned) {
+      const int hr = r.rot_dim / 2;
+#pragma unroll
+      for (int e = 0; e < 2 * c; ++e) {
+        const int d = c * c0 + e;
+        l.partner[e] = T(0);
+        if (turned && d < 2 * hr) l.partner[e] = x[d < hr ? d + hr : d - hr];
+      }
+    }
+    return l;
+  }
+  __device__ __forceinline__ void turn(Loaded& l, const dmoe_rotary& r) const {
+    if (!turned) return;
+    float x[c], y[c];
+    widen(l.a, x);
+    widen(l.b, y);
+    if constexpr (!kAligned) {
+      const int hr = r.rot_dim / 2;
+#pragma unroll
+      for (int e = 0; e < 2 * c; ++e) {
+        const int d = c * c0 + e;
+        const float p = load_as_f32<T>(&l.partner[e]);
+        float& v = e < c ? x[e] : y[e - c];
+        v = d < 2 * hr ? v * co[e] + (d < hr ? -p : p) * si[e] : v;
+      }
+    } else if (r.interleaved) {
+#pragma unroll
+      for (int e = 0; e < c; ++e) {
+        float* v = e < c / 2 ? x + 2 * e : y + 2 * e - c;
+        const float v1 = v[0], v2 = v[1];
+        const bool in = pair_of(e, r) >= 0;
+        v[0] = in ? v1 * co[e] - v2 * si[e] : v1;
+        v[1] = in ? v2 * co[e] + v1 * si[e] : v2;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < c; ++e) {
+        const float v1 = x[e], v2 = y[e];
+        x[e] = v1 * co[e] - v2 * si[e];
+        y[e] = v2 * co[e] + v1 * si[e];
+      }
+    }
+    l.a = narrow(x);
+    l.b = narrow(y);
+  }
+};
+
+bool aligned_pairs(const dmoe_rotary& r, int c) { return r.interleaved || !r.turns || r.rot_dim / 2 % c == 0; }
+
+// n tokens of `heads` heads through the rotation; in(i, h) and out(i, h, j): a
+// head's elements, and where its chunk j goes (nullptr: nowhere).  A row's
 // chunks lie in one wave, whose loads of them are done when it stores: in
 // place is safe.  Chunks from dim on, up to `padded`, are 0.
-template <typename T, typename In, typename Out>
-__device__ __forceinline__ void rotate_rows(int n, int heads, int dim, int padded, const float2* cs, const dmoe_rotary& r, In in, Out out) {
+template <typename T, bool kAligned, typename Pos, typename In, typename Out>
+__device__ __forceinline__ void rotate_rows(int n, int heads, int dim, int padded, const dmoe_rotary& r, bool inverse, Pos pos, In in, Out out) {
   constexpr int c = Chunk<T>::c;
-  const int chunks = padded / c, pairs = r.rot_dim / 2;
-  const int log = chunks > 1 ? 32 - __builtin_clz(chunks - 1) : 0;  // lanes of a row: 2^log, at most 64
-  const int j = threadIdx.x & ((1 << log) - 1), step = kThreads >> log, rows = n * heads;
-  for (int x0 = threadIdx.x >> log; x0 < rows; x0 += step * kInFlight) {
-    Chunk<T> y[kInFlight];
+  const int chunks = padded / c, units = (chunks + 1) / 2;
+  const int log = units > 1 ? 32 - __builtin_clz(units - 1) : 0;  // lanes of a row: 2^log, at most 32
+  const int row = threadIdx.x >> log, i = row % kTokens, step = (kThreads >> log) / kTokens;
+  Unit<T, kAligned> u(threadIdx.x & ((1 << log) - 1), r);
+  if (i >= n || u.c0 >= chunks) return;
+  for (int h0 = row / kTokens; h0 < heads; h0 += step * kInFlight) {
+    typename Unit<T, kAligned>::Loaded l[kInFlight];
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      const int x = x0 + u * step;
-      y[u] = Chunk<T>{};
-      if (x < rows && j * c < dim) {
-        const int h = x / n, i = x - h * n;
-        y[u] = rotated<T>(in(i, h), j * c, cs + i * pairs, r.turns ? r.rot_dim : 0, r.interleaved);
-      }
+    for (int y = 0; y < kInFlight; ++y) {
+      const int h = h0 + y * step;
+      if (h < heads) l[y] = u.load(in(i, h), dim / c, r);
     }
+    if (h0 == row / kTokens) u.form(pos(i), r, inverse);  // while the first heads are on their way
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      const int x = x0 + u * step;
-      if (x < rows && j < chunks) {
-        const int h = x / n, i = x - h * n;
-        if (T* to = out(i, h, j)) *reinterpret_cast<Chunk<T>*>(to) = y[u];
+    for (int y = 0; y < kInFlight; ++y) {
+      const int h = h0 + y * step;
+      if (h < heads) {
+        u.turn(l[y], r);
+        if (T* to = out(i, h, u.c0)) *reinterpret_cast<Chunk<T>*>(to) = l[y].a;
+        if (u.c1 < chunks)
+          if (T* to = out(i, h, u.c1)) *reinterpret_cast<Chunk<T>*>(to) = l[y].b;
       }
     }
   }
 }
 
-template <typename T>
+template <typename T, bool kAligned>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const T* x, long x_stride, T* out, long out_stride, int T_, int n_heads,
                                                         int heads, int dim, const int32_t* positions, dmoe_rotary r, bool inverse) {
-  extern __shared__ float2 cs[];
   const int t0 = blockIdx.x * kTokens, n = min(kTokens, T_ - t0);
   const int h0 = blockIdx.y * heads;
-  form_angles(cs, r, n, inverse, [&](int i) { return positions[t0 + i]; });
-  __syncthreads();
-  rotate_rows<T>(
-      n, min(heads, n_heads - h0), dim, dim, cs, r, [&](int i, int h) { return x + (t0 + i) * x_stride + (h0 + h) * dim; },
+  rotate_rows<T, kAligned>(
+      n, min(heads, n_heads - h0), dim, dim, r, inverse, [&](int i) { return positions[t0 + i]; },
+      [&](int i, int h) { return x + (t0 + i) * x_stride + (h0 + h) * dim; },
       [&](int i, int h, int j) { return out + (t0 + i) * out_stride + (h0 + h) * dim + j * Chunk<T>::c; });
 }
 
@@ -177,10 +218,10 @@ __device__ __forceinline__ Seq find_tile(const AppendArgs& a, int x, int tiles, 
 
 // blockIdx.x: tile of 32 positions.  blockIdx.y: the values of one
 // kv head each, then (8 tokens, group of `heads` heads) of the queries and keys.
-template <typename T>
+template <typename T, bool kAligned>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tiles, int heads, int groups) {
   constexpr int c = Chunk<T>::c;
-  extern __shared__ float2 cs[];
+  extern __shared__ float4 lds[];
   const int hkv = a.cache.n_kv_heads, dim = a.cache.head_dim;
   int tile0;
   const Seq q = find_tile(a, blockIdx.x, tiles, tile0);
@@ -197,10 +238,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tile
   const long at = ((static_cast<long>(a.layer) * a.cache.n_pages + page) * hkv * pt + p0 % pt / kTileTokens * kTileTokens) * dp;
   if (y >= 0) {
     const int nq = a.q ? a.n_heads : 0, h0 = y % groups * heads;
-    if (a.rope.turns) form_angles(cs, a.rope, n, false, [&](int i) { return p0 + i; });
-    __syncthreads();
-    rotate_rows<T>(
-        n, min(heads, nq + hkv - h0), dim, dp, cs, a.rope,
+    rotate_rows<T, kAligned>(
+        n, min(heads, nq + hkv - h0), dim, dp, a.rope, false, [&](int i) { return p0 + i; },
         [&](int i, int h) {
           h += h0;
           return h < nq ? static_cast<const T*>(a.q) + (t0 + i) * a.q_stride + h * dim
@@ -217,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tile
   if (!held) return;
   // values: a chunk holds c tokens of one element, so the tile is turned in LDS
   const int hk = blockIdx.y, r0 = p0 % kTileTokens;
-  T* tile = reinterpret_cast<T*>(cs);
+  T* tile = reinterpret_cast<T*>(lds);
   const T* vin = static_cast<const T*>(a.v) + t0 * a.v_stride + static_cast<long>(hk) * dim;
   for (int x = threadIdx.x; x < n * (dim / c); x += kThreads) {
     const int i = x / (dim / c), j = x - i * (dim / c);
@@ -250,8 +289,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tile
 }
 
 // Heads of a workgroup that rotates: as many as keep kGroups workgroups, so
-// that their angles are formed for as many heads as possible.
-constexpr long kGroups = 2048;
+// that angles are formed for as many heads as possible.
+constexpr long kGroups = 1024;
 int heads_of_workgroup(long token_groups, int n_heads) {
   int heads = 1;
   while (heads < n_heads && token_groups * ((n_heads + 2 * heads - 1) / (2 * heads)) >= kGroups) heads *= 2;
@@ -266,12 +305,14 @@ hipError_t append(const AppendArgs& a, hipStream_t s) {
   const int turned = a.cache.n_kv_heads + (a.q ? a.n_heads : 0), dp = padded_dim(a.cache.head_dim);
   const int heads = heads_of_workgroup((a.batch.T + kTokens - 1) / kTokens, turned);
   const int groups = (turned + heads - 1) / heads;
-  const size_t angles = a.rope.turns ? static_cast<size_t>(kTokens) * (a.rope.rot_dim / 2) * sizeof(float2) : 0;
-  const size_t turn = static_cast<size_t>(kTileTokens) * dp * sizeof(T);
+  const size_t lds = static_cast<size_t>(kTileTokens) * dp * sizeof(T);
   // n tokens lie in at most n / 32 + 2 tiles
   const long each = static_cast<long>(a.batch.n_seqs) * tiles, counted = a.batch.T / kTileTokens + 2l * a.batch.n_seqs;
-  append_kernel<T><<<dim3(static_cast<unsigned>(each < counted ? each : counted), a.cache.n_kv_heads + kSub * groups), kThreads,
-                     angles > turn ? angles : turn, s>>>(a, each <= counted ? tiles : 0, heads, groups);
+  const dim3 grid(static_cast<unsigned>(each < counted ? each : counted), a.cache.n_kv_heads + kSub * groups);
+  if (aligned_pairs(a.rope, Chunk<T>::c))
+    append_kernel<T, true><<<grid, kThreads, lds, s>>>(a, each <= counted ? tiles : 0, heads, groups);
+  else
+    append_kernel<T, false><<<grid, kThreads, lds, s>>>(a, each <= counted ? tiles : 0, heads, groups);
   return hipGetLastError();
 }
 
@@ -280,9 +321,15 @@ hipError_t rope(const void* x, long x_stride, void* out, long out_stride, int T_
                 const dmoe_rotary& r, bool inverse, hipStream_t s) {
   const int groups = (T_ + kTokens - 1) / kTokens;
   const int heads = heads_of_workgroup(groups, n_heads);
-  const size_t lds = static_cast<size_t>(kTokens) * (r.rot_dim / 2) * sizeof(float2);
-  rope_kernel<T><<<dim3(groups, (n_heads + heads - 1) / heads), kThreads, lds, s>>>(
-      static_cast<const T*>(x), x_stride, static_cast<T*>(out), out_stride, T_, n_heads, heads, dim, positions, r, inverse);
+  const dim3 grid(groups, (n_heads + heads - 1) / heads);
+  auto run = [&](auto kernel) {
+    kernel<<<grid, kThreads, 0, s>>>(static_cast<const T*>(x), x_stride, static_cast<T*>(out), out_stride, T_, n_heads, heads, dim, positions,
+                                     r, inverse);
+  };
+  if (aligned_pairs(r, Chunk<T>::c))
+    run(rope_kernel<T, true>);
+  else
+    run(rope_kernel<T, false>);
   return hipGetLastError();
 }
 
