@@ -39,7 +39,7 @@ class _On:
         self.device = device
 
     def __enter__(self):
-        self.back = torch.cuda.current_device()
+        self.back = torch._C._cuda_getDevice()
         if self.device.index is not None and self.device.index != self.back:
             torch.cuda.set_device(self.device)
 

@@ -661,7 +661,7 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
 // takes 8 rows, which lie side by side in every KiB of the partial sums: a
 // wave reads 128 bytes of each, lane = (16-byte piece of the KiB, row), and the
 // waves share the pieces.
-constexpr int kMergeWaves = 8, kMergeRows = 8;
+constexpr int kMergeWaves = 4, kMergeRows = 8;
 
 template <typename T, int DP>
 __global__ __launch_bounds__(64 * kMergeWaves) void attention_merge_kernel(AttnArgs a, AttnShape sh, int part_rows) {
@@ -669,18 +669,23 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attention_merge_kernel(AttnA
   __shared__ f32x4 so[kMergeWaves - 1][kV][64];
   __shared__ float2 sml[kMergeWaves][kMergeRows];
   const int hkv = a.cache.n_kv_heads;
-  const AttnPlanHead head = *reinterpret_cast<const AttnPlanHead*>(a.plan);
-  const AttnMerge* merges = reinterpret_cast<const AttnMerge*>(plan_items(a.plan) + sh.max_items());
+  const int groups = sh.tile_rows / kMergeRows;
+  // the number of merges and the first one are loaded together: the grid is within their array
+  const auto* plan = (const __attribute__((address_space(4))) int32_t*)a.plan;
+  const int units = plan[1] * hkv * groups;
+  const long merges = (sizeof(AttnPlanHead) + sh.max_items() * sizeof(AttnItem)) / sizeof(int);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane % kMergeRows, col = lane / kMergeRows;  // row; piece of 4 elements of every 32
   const float* po = static_cast<const float*>(a.workspace);
   const float2* ml = reinterpret_cast<const float2*>(po + static_cast<long>(part_rows) * DP);
   const long step = static_cast<long>(hkv) * sh.tile_rows;
-  const int groups = (head.most_rows + kMergeRows - 1) / kMergeRows;
-  const int units = head.n_merges * hkv * groups;
-  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+  int u = blockIdx.x;
+  do {
+    typedef int i32x8 __attribute__((ext_vector_type(8)));
     const int row0 = u % groups * kMergeRows, hk = u / groups % hkv;
-    const AttnMerge mg = merges[u / groups / hkv];
+    const i32x8 mw = *(const __attribute__((address_space(4))) i32x8*)(plan + merges + u / groups / hkv * 8l);
+    const AttnMerge mg{mw[0], mw[1], mw[2], mw[3], mw[4], {0, 0, 0}};
+    if (u >= units) return;
     if (mg.first + row0 >= mg.rows) continue;
     const int row = mg.first + row0 + r;
     const bool live = row < mg.rows;
@@ -754,7 +759,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attention_merge_kernel(AttnA
       if (32 * j + col * 4 < a.cache.head_dim) store4(op + 32 * j, o[j] * inv);
     if (a.lse && col == 0)
       a.lse[static_cast<long>(mg.row0 + tok) * a.n_heads + qh] = some ? (mm + log2f(l)) * kLn2 : -INFINITY;
-  }
+  } while ((u += gridDim.x) < units);
 }
 
 constexpr long kMergeGrid = 1024;

@@ -79,8 +79,7 @@ struct AttnMerge {
   int pad[3];
 };
 struct AttnPlanHead {
-  int n_items, n_merges;
-  int most_pieces, most_rows;  // of the row tiles to merge
+  int n_items, n_merges, pad[2];
 };
 static_assert(sizeof(AttnItem) == 64 && sizeof(AttnMerge) == 32 && sizeof(AttnPlanHead) == 16);
 

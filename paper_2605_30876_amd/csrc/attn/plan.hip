@@ -10,7 +10,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxSeqs = 4096;
 constexpr int kKeptSeqs = 512;  // sequences kept in LDS; further ones are read again
 // Items that splitting aims at, all kv heads together, and their key tiles at least.
-constexpr int kSplitRows = 1024;  // items of 32 rows
+constexpr int kSplitRows = 512;   // items of 32 rows
 constexpr int kSplitBlock = 512;  // items of 128 rows: as many workgroups as the device holds at once
 constexpr int kMinRows = 8;
 constexpr int kMinBlock = 4;
@@ -65,9 +65,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   __shared__ int parts[kThreads];
   __shared__ int iwaves[kThreads / 64];
   __shared__ long lwaves[kThreads / 64];
-  __shared__ int most[2];  // of the split row tiles: pieces, rows
   const int tid = threadIdx.x;
-  if (tid < 2) most[tid] = 0;
   int n_tiles = 0;
   for (int i0 = 0; i0 < b.n_seqs; i0 += kThreads) {
     const int i = i0 + tid;
@@ -104,12 +102,14 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   for (int t = tid + kThreads; t < n_tiles; t += kThreads) keys += load_tile(t).kt;
   long all;
   scan_exclusive(keys, lwaves, &all);
-  // Pieces of `chunk` key tiles: sum ceil(kt / chunk) <= n_tiles + all / chunk
-  // fills the aim but does not pass it.  With row tiles of about one length
-  // that are more than half of the aim nothing is split: one round of
-  // workgroups either way, and no partial results.  At least all / split: the arrays' size.
+  // Pieces of `chunk` key tiles: sum ceil(kt / chunk) <= n_tiles + all / chunk,
+  // and all / chunk <= room <= aim, which the arrays' sizes count on.  Items of
+  // 128 rows leave partial results of 64 KiB: they fill one round of workgroups
+  // but do not pass it, and with row tiles of about one length that are more
+  // than half of the aim nothing is split.  Those of 32 rows are cheap to join:
+  // pieces of the average length even the sequences out.
   const long split = sh.aim;
-  const long room = max(max(split - n_tiles, split / 2), 1l);
+  const long room = sh.tile_rows == 32 ? split : max(max(split - n_tiles, split / 2), 1l);
   const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + room - 1) / room));
 
   AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
@@ -129,11 +129,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
     const int part = n_parts + static_cast<int>(at >> 21 & kBits);
     items[tid] = static_cast<int>(at & kBits);
     parts[tid] = pieces > 1 ? part : -1;
-    if (pieces > 1) {
-      merges[n_merges + (at >> 42)] = AttnMerge{r.q.row0, r.first, r.rows, part, pieces, {0, 0, 0}};
-      atomicMax(&most[0], pieces);
-      atomicMax(&most[1], min(sh.tile_rows, r.rows - r.first));
-    }
+    if (pieces > 1) merges[n_merges + (at >> 42)] = AttnMerge{r.q.row0, r.first, r.rows, part, pieces, {0, 0, 0}};
     if (tid == 0) items[kThreads] = total;
     __syncthreads();
     for (int x = tid; x < total; x += kThreads) {
@@ -158,8 +154,6 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   if (tid == 0) {
     head->n_items = n_items;
     head->n_merges = n_merges;
-    head->most_pieces = most[0];
-    head->most_rows = most[1];
   }
 }
 

