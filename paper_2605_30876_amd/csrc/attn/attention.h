@@ -311,7 +311,7 @@ __device__ __forceinline__ bool load_item(const AttnArgs& a, int i, AttnItem& it
   const auto* p = (const __attribute__((address_space(4))) int32_t*)a.plan;
   const int n = p[0];
   const i32x16 w = *(const __attribute__((address_space(4))) i32x16*)(p + sizeof(AttnPlanHead) / 4 + static_cast<long>(i) * 16);
-  it = AttnItem{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], {w[9], w[10], w[11], w[12]}, {0, 0, 0}};
+  it = AttnItem{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], {w[9], w[10], w[11], w[12], w[13], w[14]}, 0};
   return i < n;
 }
 
@@ -498,36 +498,45 @@ __device__ __forceinline__ void dma16(const T* src, Frag* dst) {
 template <typename T, int DP>
 struct BlockStage {
   static constexpr int kTileFrags = DP / (2 * Types<T>::c);           // operands of a tile's keys, or of its values
-  static constexpr int kTS = DP * sizeof(T) * kTileTokens <= 8192 ? 2 : 1;  // tiles of a stage: up to 32 KiB, or one
+  static constexpr int kTS = stage_tiles(sizeof(T) == 4 ? DMOE_F32 : DMOE_BF16, DP);
   typename Types<T>::Frag f[kTS][2][kTileFrags][64];                  // [tile][keys, values][operand][lane]
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+//
+// kWK = 2: eight waves, each four on one half of the item's keys, joined
+// through LDS: half the partial results of two such workgroups, which matters
+// where few row tiles are cut into many items.
+template <typename T, int DP, int kWK>
+__global__ __launch_bounds__(256 * kWK, waves_per_simd<T>(DP)) void attention_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef WaveRows<T, DP> Rows;
   typedef typename Rows::Frag Frag;
   typedef BlockStage<T, DP> Stage;
   constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS, kTS = Stage::kTS;
-  __shared__ Stage s0, s1;  // apart, so that reads of one do not wait for loads into the other
+  __shared__ Stage s0s[kWK], s1s[kWK];  // apart, so that reads of one do not wait for loads into the other
   const int hkv = a.cache.n_kv_heads;
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
   AttnItem it;
   if (!load_item(a, item_i, it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wk = kWK > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
+  Stage &s0 = s0s[wk], &s1 = s1s[wk];
   Rows w;
   w.clear();
   const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wave, lane);
   const float scale2 = a.scale * kLog2e;
   const TileMap<T, DP> map(a, it.slot, hk);
-
+  // this wave's keys; the first half has at least as many stages
+  const int mid = kWK > 1 ? item_middle(it.kt0, it.kt1) : it.kt1;
+  const int kt0 = wk ? mid : it.kt0, kt1 = wk ? it.kt1 : mid;
+  const int turns = (mid - it.kt0 + kTS - 1) / kTS;
   struct Ids {
     int id[kTS];
   };
   auto pages = [&](int kt) {
     Ids p;
 #pragma unroll
-    for (int n = 0; n < kTS; ++n) p.id[n] = map.page(kt + n, it.kt1);
+    for (int n = 0; n < kTS; ++n) p.id[n] = map.page(kt + n, kt1);
     return p;
   };
   // a wave's share of a stage: with two tiles the keys or the values of one,
@@ -612,13 +621,14 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
   // page ids are known two stages ahead, keys and values one.  A stage's loads
   // are waited for by the wave that issued them, then by all: the barrier also
   // tells that the other buffer has been read.
-  int kt = it.kt0;
+  int kt = kt0;
   Ids pg, pg1;
 #pragma unroll
   for (int n = 0; n < kTS; ++n) {
-    pg.id[n] = it.page[n];
-    pg1.id[n] = it.page[kTS + n];
+    pg.id[n] = wk ? it.page[4 + n] : kt + n < kt1 ? it.page[n] : -1;
+    pg1.id[n] = wk || (kWK > 1 && kt + kTS + n >= kt1) ? -1 : it.page[kTS + n];
   }
+  if (wk) pg1 = pages(kt + kTS);
   load(kt, pg, s0);
   __builtin_amdgcn_sched_barrier(0);
   auto turn = [&](auto masked, Stage& cur, Stage& fill) {
@@ -637,23 +647,58 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_block_ke
     pg = pg1;
     pg1 = pg2;
   };
-  // stages whose keys every row of the workgroup sees, then the others
+  // stages whose keys every row of the workgroup sees, then the others; every
+  // wave takes all turns, for their barriers
   const int whole = visible_end(it.len - it.n + it.first / sh.group, it.len, a.mask_block) / kTileTokens;
-  int stages = whole >= it.kt1 ? (it.kt1 - kt + kTS - 1) / kTS : max(whole - kt, 0) / kTS;
+  const int stages = whole >= kt1 ? max(kt1 - kt + kTS - 1, 0) / kTS : max(whole - kt, 0) / kTS;
   const int first_masked = kt + stages * kTS;
-  for (; stages >= 2; stages -= 2) {
+  int done = 0;
+  for (; done + 2 <= stages; done += 2) {
     turn(std::false_type(), s0, s1);
     turn(std::false_type(), s1, s0);
   }
-  if (stages) turn(std::false_type(), s0, s1);
-  for (bool odd = stages; kt < it.kt1; odd = !odd) {
-    if (odd)
+  if (done < stages) {
+    turn(std::false_type(), s0, s1);
+    ++done;
+  }
+  for (; done < turns; ++done) {
+    if (done & 1)
       turn(std::true_type(), s1, s0);
     else
       turn(std::true_type(), s0, s1);
   }
-  if (left) w.add_by_key(map, first_masked, it.kt1, 1, scale2, half);
+  if (left) w.add_by_key(map, first_masked, kt1, 1, scale2, half);
   w.l = other_half_sum(w.l);
+  if constexpr (kWK > 1) {
+    // the second half's sums to the first's waves; the stages are done with
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(wave < 2 ? s0s : s1s) + (wave & 1) * (16 * kB * 64);
+    static_assert(sizeof(s0s) >= 2 * 16 * kB * 64 * sizeof(float));
+    __shared__ float2 stats[4][64];
+    if (wk) {
+      stats[wave][lane] = make_float2(w.m, w.l);
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) store4(sums + (4 * b + i / 4) * 256 + lane * 4, f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
+    }
+    __syncthreads();
+    if (wk) return;
+    const float2 other = stats[wave][lane];
+    const float nm = fmaxf(w.m, other.x);
+    const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = other.x == nm ? 1.f : exp2_hw(other.x - nm);
+    w.scale(fa);
+    w.m = nm;
+    w.l += fb * other.y;
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(sums + (4 * b + i / 4) * 256 + lane * 4);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
+      }
+  }
   rows.store(w, a, sh, it, hk, half, part_rows);
 }
 
@@ -773,7 +818,14 @@ hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
     constexpr size_t lds = 2 * (16 * (DP / 32) + 2) * 64 * sizeof(float);
     attention_rows_kernel<T, DP, 4><<<items, 256, lds, s>>>(a, sh, part_rows);
   } else {
-    attention_block_kernel<T, DP><<<items, 256, 0, s>>>(a, sh, part_rows);
+    if constexpr (waves_per_simd<T>(DP) == 2) {
+      if (sh.wide)
+        attention_block_kernel<T, DP, 2><<<items, 512, 0, s>>>(a, sh, part_rows);
+      else
+        attention_block_kernel<T, DP, 1><<<items, 256, 0, s>>>(a, sh, part_rows);
+    } else {
+      attention_block_kernel<T, DP, 1><<<items, 256, 0, s>>>(a, sh, part_rows);
+    }
   }
   // no sequence is long enough to be split: nothing to join
   if (static_cast<long>(a.cache.max_pages) * a.cache.page_tokens <= static_cast<long>(sh.min_tiles) * kTileTokens) return hipGetLastError();

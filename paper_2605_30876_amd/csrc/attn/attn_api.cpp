@@ -211,7 +211,7 @@ dmoe_status dmoe_attention_plan(const dmoe_cache* cache, dmoe_batch batch, int n
   REQUIRE(plan, "plan must not be NULL");
   ALIGNED(plan);
   REQUIRE(mask_block >= 0, "mask_block=%d must be >= 0", mask_block);
-  const dmoe::AttnShape sh = dmoe::attn_shape(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads);
+  const dmoe::AttnShape sh = dmoe::attn_shape(*cache, batch, n_heads);
   REQUIRE(plan_ints >= dmoe::plan_ints(sh), "a plan of %zu ints is smaller than the %zu needed", plan_ints, dmoe::plan_ints(sh));
   return hip_status(dmoe::launch_attention_plan(*cache, batch, sh, mask_block, plan, static_cast<hipStream_t>(stream)), __func__);
 }
@@ -234,7 +234,7 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   ALIGNED(plan);
   ALIGNED(workspace);
   ALIGNED_TO(lse, 4);
-  const dmoe::AttnShape sh = dmoe::attn_shape(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads);
+  const dmoe::AttnShape sh = dmoe::attn_shape(*cache, batch, n_heads);
   REQUIRE(plan_ints >= dmoe::plan_ints(sh), "a plan of %zu ints is smaller than the %zu needed", plan_ints, dmoe::plan_ints(sh));
   const size_t need = dmoe::attn_workspace_bytes(sh, cache->n_kv_heads, dmoe::padded_dim(cache->head_dim));
   REQUIRE(ws_bytes >= need, "workspace of %zu bytes is smaller than the %zu bytes needed", ws_bytes, need);

@@ -70,9 +70,14 @@ struct AttnItem {
   int first, rows;            // first row of the tile, rows of the sequence
   int kt0, kt1;               // key tiles of 32 tokens
   int part;                   // partial result, or -1: the only item of its rows
-  int page[4];                // pages of the first key tiles (-1: none), known before the table could be
-  int pad[3];
+  // pages of the first four key tiles and of two from item_middle on (-1:
+  // none), known before the table could be
+  int page[6];
+  int pad;
 };
+// Where the second half of an item's key tiles starts: the first has as many pairs of tiles, or one more.
+__host__ __device__ constexpr int item_middle(int kt0, int kt1) { return kt0 + ((kt1 - kt0 + 1) / 2 + 1) / 2 * 2 < kt1 ? kt0 + ((kt1 - kt0 + 1) / 2 + 1) / 2 * 2 : kt1; }
+
 struct AttnMerge {
   int row0, first, rows;      // as above
   int part, pieces;           // partial results part .. part + pieces-1
@@ -92,12 +97,18 @@ struct AttnShape {
   long max_tiles;  // row tiles of the batch at most
   long split_items;  // items that splitting along the keys may add, and merges, at most
   int aim;           // items that splitting aims at: at most split_items
+  bool wide;         // block kernel: two halves of an item's keys per workgroup
+  int unit;          // key tiles that an item's range is a multiple of (stage_tiles)
   __host__ __device__ long max_items() const { return max_tiles + split_items; }
   __host__ __device__ long max_parts() const { return 2 * split_items; }
 };
+// Key tiles of a stage of the block kernel: up to 16 KiB of keys, or one tile.
+constexpr int stage_tiles(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) * kTileTokens <= 8192 ? 2 : 1; }
 // Two workgroups of the block kernel fit a CU where a wave's registers fit half of a SIMD's.
 constexpr bool two_per_cu(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) <= 256; }
 AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
+// The same for a cache of this type: the block kernel's form, and what it aims at.
+AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads);
 
 inline size_t plan_ints(const AttnShape& s) {
   return (sizeof(AttnPlanHead) + static_cast<size_t>(s.max_items()) * sizeof(AttnItem) +

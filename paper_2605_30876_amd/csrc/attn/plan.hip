@@ -14,6 +14,7 @@ constexpr int kSplitRows = 512;   // items of 32 rows
 constexpr int kSplitBlock = 512;  // items of 128 rows: as many workgroups as the device holds at once
 constexpr int kMinRows = 8;
 constexpr int kMinBlock = 4;
+constexpr int kMinWide = 8;
 
 // Exclusive prefix sums over the workgroup's threads; *total is their sum.
 template <typename V>
@@ -136,14 +137,16 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
       const int j = find(items, kThreads, x);
       const Tile& u = tile[j];
       const int p = x - items[j], n = max(1, (u.kt + chunk - 1) / chunk);
-      AttnItem it{u.q.slot, u.q.row0, u.q.n, u.q.len, u.first, u.rows, 0, 0, parts[j] < 0 ? -1 : parts[j] + p, {}, {0, 0, 0}};
-      it.kt0 = static_cast<int>(static_cast<long>(u.kt) * p / n);
-      it.kt1 = static_cast<int>(static_cast<long>(u.kt) * (p + 1) / n);
+      AttnItem it{u.q.slot, u.q.row0, u.q.n, u.q.len, u.first, u.rows, 0, 0, parts[j] < 0 ? -1 : parts[j] + p, {}, 0};
+      const long units = (u.kt + sh.unit - 1) / sh.unit;
+      it.kt0 = static_cast<int>(units * p / n) * sh.unit;
+      it.kt1 = min(static_cast<int>(units * (p + 1) / n) * sh.unit, u.kt);
+      const int mid = item_middle(it.kt0, it.kt1);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        it.page[i] = it.kt0 + i < it.kt1
-                         ? c.table[static_cast<long>(u.q.slot) * c.max_pages + (it.kt0 + i) * kTileTokens / c.page_tokens]
-                         : -1;
+      for (int i = 0; i < 6; ++i) {
+        const int kt = i < 4 ? it.kt0 + i : mid + i - 4;
+        it.page[i] = kt < it.kt1 ? c.table[static_cast<long>(u.q.slot) * c.max_pages + kt * kTileTokens / c.page_tokens] : -1;
+      }
       out[n_items + x] = it;
     }
     n_items += total;
@@ -171,13 +174,28 @@ AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads
   s.aim = aim > 1 ? aim : 1;
   s.split_items = s.aim;
   s.min_tiles = s.tile_rows == 32 ? kMinRows : kMinBlock;
+  s.wide = false;
+  s.unit = 1;
   return s;
 }
 
-hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& shape, int mask_block,
+AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
+  AttnShape s = attn_shape(b.n_seqs, b.T, b.max_new, n_heads, c.n_kv_heads);
+  if (s.tile_rows > 32) {
+    // one workgroup a CU: where a wave needs more than half of a SIMD's
+    // registers, and where eight waves work on an item, which they do if the
+    // batch's row tiles alone do not fill the device
+    const bool two = two_per_cu(c.dt, padded_dim(c.head_dim));
+    s.wide = two && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
+    if (!two || s.wide) s.aim = s.aim > 1 ? s.aim / 2 : 1;
+    if (s.wide) s.min_tiles = kMinWide;
+    s.unit = stage_tiles(c.dt, padded_dim(c.head_dim));
+  }
+  return s;
+}
+
+hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
                                  int32_t* plan, hipStream_t s) {
-  AttnShape sh = shape;
-  if (sh.tile_rows > 32 && !two_per_cu(c.dt, padded_dim(c.head_dim))) sh.aim = sh.aim > 1 ? sh.aim / 2 : 1;
   plan_kernel<<<1, kThreads, 0, s>>>(c, b, sh, mask_block, plan);
   return hipGetLastError();
 }
