@@ -376,42 +376,46 @@ struct RowPlace {
   }
 };
 
-// Few rows (one token a sequence, a small block): 32 of one kv head per
-// workgroup, its kWK waves on every kWK-th key tile, joined through LDS.  The
-// cache is read once, straight into registers; the next tile's keys are
-// issued when this one's are used up, its values likewise.
-template <typename T, int DP, int kWK>
-__global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+// Few rows (one token a sequence, a small block): 32 kWR of one kv head per
+// workgroup, 4 / kWR waves to 32 of them, each on every (4 / kWR)-th key tile,
+// joined through LDS.  The cache goes straight into registers, past the caches
+// where one wave alone reads a tile; the next tile's keys are issued when this
+// one's are used up, its values likewise.
+template <typename T, int DP, int kWR>
+__global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef WaveRows<T, DP> Rows;
   typedef typename Rows::Frag Frag;
-  constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS;
+  constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS, kWK = 4 / kWR;
   extern __shared__ float lds[];
   const int hkv = a.cache.n_kv_heads;
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
   AttnItem it;
   if (!load_item(a, item_i, it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % kWK, wr = wave / kWK;
   Rows w;
   w.clear();
-  const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first, lane);
+  const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wr, lane);
   const float scale2 = a.scale * kLog2e;
   const TileMap<T, DP> map(a, it.slot, hk);
   const int kt1 = min(it.kt1, (w.hi + kTileTokens - 1) / kTileTokens);
   Frag k[kK], v[kB][kS];
+  auto load1 = [&](const T* p) {
+    const Frag* f = reinterpret_cast<const Frag*>(p + lane * c);
+    return kWR == 1 ? __builtin_nontemporal_load(f) : *f;
+  };
   auto load_k = [&](const T* p) {
 #pragma unroll
-    for (int j = 0; j < kK; ++j) k[j] = __builtin_nontemporal_load(reinterpret_cast<const Frag*>(p + j * 64 * c + lane * c));
+    for (int j = 0; j < kK; ++j) k[j] = load1(p + j * 64 * c);
   };
   auto load_v = [&](const T* p) {
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
-      for (int s = 0; s < kS; ++s) v[b][s] = __builtin_nontemporal_load(reinterpret_cast<const Frag*>(p + (b * kS + s) * 64 * c + lane * c));
+      for (int s = 0; s < kS; ++s) v[b][s] = load1(p + (b * kS + s) * 64 * c);
   };
   // page ids are known two of this wave's tiles ahead, its keys and values one
   int kt = it.kt0 + wk;
-  static_assert(kWK == 4);
   int page = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
   int page1 = map.page(kt + kWK, kt1);
   if (map.holds(page)) {
@@ -452,7 +456,7 @@ __global__ __launch_bounds__(64 * kWK, waves_per_simd<T>(DP)) void attention_row
   constexpr int kLen = (16 * kB + 2) * 64;
 #pragma unroll
   for (int n = kWK / 2; n >= 1; n /= 2) {
-    float* buf = lds + (wk % n) * kLen;
+    float* buf = lds + (wr * (kWK / 2) + wk % n) * kLen;
     if (wk >= n && wk < 2 * n) {
       buf[lane] = w.m;
       buf[64 + lane] = w.l;
@@ -814,9 +818,12 @@ hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
   const int hkv = a.cache.n_kv_heads;
   const unsigned items = static_cast<unsigned>(sh.max_items() * hkv);
   const int part_rows = static_cast<int>(sh.max_parts() * hkv * sh.tile_rows);
-  if (sh.tile_rows == 32) {
+  if (sh.tile_rows <= 64) {
     constexpr size_t lds = 2 * (16 * (DP / 32) + 2) * 64 * sizeof(float);
-    attention_rows_kernel<T, DP, 4><<<items, 256, lds, s>>>(a, sh, part_rows);
+    if (sh.tile_rows == 32)
+      attention_rows_kernel<T, DP, 1><<<items, 256, lds, s>>>(a, sh, part_rows);
+    else
+      attention_rows_kernel<T, DP, 2><<<items, 256, lds, s>>>(a, sh, part_rows);
   } else {
     if constexpr (waves_per_simd<T>(DP) == 2) {
       if (sh.wide)

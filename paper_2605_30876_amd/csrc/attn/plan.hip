@@ -12,8 +12,8 @@ constexpr int kKeptSeqs = 512;  // sequences kept in LDS; further ones are read 
 // Items that splitting aims at, all kv heads together, and their key tiles at least.
 constexpr int kSplitRows = 512;   // items of 32 rows
 constexpr int kSplitBlock = 512;  // items of 128 rows: as many workgroups as the device holds at once
-constexpr int kMinRows = 8;
-constexpr int kMinBlock = 4;
+constexpr int kMinRows = 8;   // two a wave
+constexpr int kMinBlock = 4;  // two a wave of the 64-row form, two stages of the block kernel
 constexpr int kMinWide = 8;
 
 // Exclusive prefix sums over the workgroup's threads; *total is their sum.
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   // than half of the aim nothing is split.  Those of 32 rows are cheap to join:
   // pieces of the average length even the sequences out.
   const long split = sh.aim;
-  const long room = sh.tile_rows == 32 ? split : max(max(split - n_tiles, split / 2), 1l);
+  const long room = sh.tile_rows <= 64 ? split : max(max(split - n_tiles, split / 2), 1l);
   const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + room - 1) / room));
 
   AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
@@ -166,11 +166,11 @@ AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads
   AttnShape s;
   s.group = n_heads / n_kv_heads;
   const long most = static_cast<long>(max_new < T ? max_new : T) * s.group;
-  s.tile_rows = most <= 32 ? 32 : 128;
+  s.tile_rows = most <= 32 ? 32 : most <= 64 ? 64 : 128;
   const long by_seq = n_seqs * ((most + s.tile_rows - 1) / s.tile_rows);
   const long by_rows = static_cast<long>(T) * s.group / s.tile_rows + n_seqs;
   s.max_tiles = by_seq < by_rows ? by_seq : by_rows;
-  const int aim = (s.tile_rows == 32 ? kSplitRows : kSplitBlock) / n_kv_heads;
+  const int aim = (s.tile_rows <= 64 ? kSplitRows : kSplitBlock) / n_kv_heads;
   s.aim = aim > 1 ? aim : 1;
   s.split_items = s.aim;
   s.min_tiles = s.tile_rows == 32 ? kMinRows : kMinBlock;
@@ -181,7 +181,7 @@ AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads
 
 AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   AttnShape s = attn_shape(b.n_seqs, b.T, b.max_new, n_heads, c.n_kv_heads);
-  if (s.tile_rows > 32) {
+  if (s.tile_rows > 64) {
     // one workgroup a CU: where a wave needs more than half of a SIMD's
     // registers, and where eight waves work on an item, which they do if the
     // batch's row tiles alone do not fill the device
