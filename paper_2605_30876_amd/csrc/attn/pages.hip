@@ -12,10 +12,11 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kMaxSlots = 65536;
-// Pools of up to this many pages have their counts in LDS while an update
-// changes them: an atomic there takes no trip to L2 (32 sequences over 700
-// pages: 20.0 us with the counts in memory, kInLds us there).
-constexpr int kLdsPages = 12288;
+// Updates of up to this many entries over pools of up to this many pages keep
+// entries and counts in LDS: an atomic there takes no trip to L2 (32 sequences
+// over 700 pages: 20 us with both in memory, 8 to 11 us so).
+constexpr int kLdsPages = 8192;
+constexpr int kLdsEntries = 256;
 
 template <typename V>
 __device__ __forceinline__ V scan_exclusive(V v, V* waves, V* total) {
@@ -48,9 +49,16 @@ struct Counts {
     return __hip_atomic_load(at + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __device__ __forceinline__ void add(int p, int d) const { atomicAdd(at + p, d); }
+  __device__ __forceinline__ void set(int p, int v) const {
+    if constexpr (kLds)
+      at[p] = v;
+    else
+      __hip_atomic_store(at + p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ void lower(int p, int v) const { atomicMin(at + p, v); }
   // what all threads did before is seen by all after
   __device__ __forceinline__ static void sync() {
-    if constexpr (!kLds) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the atomics have acted
+    if constexpr (!kLds) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): stores and atomics have acted
     __syncthreads();
   }
 };
@@ -76,9 +84,11 @@ struct Entry {
 template <bool kLds>
 __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const int32_t* dst, const int32_t* src, const int32_t* keep,
                                                           const int32_t* new_lens, int n, int32_t* status, int32_t* n_pairs,
-                                                          Entry* entries, int32_t* from, int32_t* to, int32_t* rows,
-                                                          int32_t* owner, int32_t* free_list) {
+                                                          Entry* entries_ws, int32_t* from, int32_t* to, int32_t* rows,
+                                                          int32_t* free_list) {
   extern __shared__ int32_t lds_counts[];
+  __shared__ Entry lds_entries[kLds ? kLdsEntries : 1];
+  Entry* const entries = kLds ? lds_entries : entries_ws;
   __shared__ uint32_t seen[kMaxSlots / 32];
   __shared__ int waves[kThreads / 64];
   __shared__ int bad;
@@ -154,29 +164,28 @@ __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const in
   count_shared(1);
   for (int i = tid; i < n; i += kThreads) {
     Entry& e = entries[i];
-    if (e.keep % pt) {
-      e.part = rows[static_cast<long>(i) * mp + e.full];
-      owner[e.part] = n;
-    }
+    if (e.keep % pt) e.part = rows[static_cast<uint32_t>(i) * mp + e.full];
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): owner's stores and atomics have acted
   counts.sync();
-  // a part that nobody holds any more stays with the first entry that had it
-  for (int i = tid; i < n; i += kThreads) {
-    const Entry& e = entries[i];
-    if (e.part >= 0 && e.src == e.dst && counts.get(e.part) == 0) atomicMin(&owner[e.part], i);
-  }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): owner's stores and atomics have acted
-  counts.sync();
-  // parts that stay are held by their entry, the others until they are copied
+  // a part that nobody holds any more stays with the first entry that had it:
+  // the entries that may keep it lower its count to their number less n
   for (int i = tid; i < n; i += kThreads) {
     Entry& e = entries[i];
-    if (e.part >= 0) {
-      e.mine = __hip_atomic_load(&owner[e.part], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
-      counts.add(e.part, 1);
-    }
+    e.mine = e.part >= 0 && e.src == e.dst && counts.get(e.part) <= 0;
+    if (e.mine) counts.lower(e.part, i - n);
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): owner's stores and atomics have acted
+  counts.sync();
+  for (int i = tid; i < n; i += kThreads) {
+    Entry& e = entries[i];
+    if (e.mine) e.mine = counts.get(e.part) == i - n;
+  }
+  counts.sync();
+  for (int i = tid; i < n; i += kThreads)
+    if (entries[i].mine) counts.set(entries[i].part, 0);
+  counts.sync();
+  // parts that stay are held by their entry, the others until they are copied
+  for (int i = tid; i < n; i += kThreads)
+    if (entries[i].part >= 0) counts.add(entries[i].part, 1);
   counts.sync();
   int need = 0, copies = 0;
   for (int i0 = 0; i0 < n; i0 += kThreads) {
@@ -342,10 +351,10 @@ size_t align16(size_t b) { return (b + 15) & ~static_cast<size_t>(15); }
 
 }  // namespace
 
-// Workspace: pairs' number | entries | from | to | rows | owner | free list.
+// Workspace: pairs' number | entries | from | to | rows | free list.
 size_t update_workspace_bytes(long n, long max_pages, long n_pages) {
   const long most = n * max_pages < n_pages ? n * max_pages : n_pages;  // pages handed out
-  return 16 + align16(n * sizeof(Entry)) + 2 * align16(n * 4) + align16(n * max_pages * 4) + align16(n_pages * 4) + align16(most * 4);
+  return 16 + align16(n * sizeof(Entry)) + 2 * align16(n * 4) + align16(n * max_pages * 4) + align16(most * 4);
 }
 
 hipError_t launch_update(const dmoe_cache& c, const int32_t* dst, const int32_t* src, const int32_t* keep,
@@ -361,12 +370,11 @@ hipError_t launch_update(const dmoe_cache& c, const int32_t* dst, const int32_t*
   int32_t* from = take(n * 4l);
   int32_t* to = take(n * 4l);
   int32_t* rows = take(static_cast<long>(n) * c.max_pages * 4);
-  int32_t* owner = take(c.n_pages * 4l);
   int32_t* free_list = take(0);
-  if (c.n_pages <= kLdsPages)
-    update_kernel<true><<<1, kThreads, c.n_pages * 4l, s>>>(c, dst, src, keep, new_lens, n, status, n_pairs, entries, from, to, rows, owner, free_list);
+  if (c.n_pages <= kLdsPages && n <= kLdsEntries)
+    update_kernel<true><<<1, kThreads, c.n_pages * 4l, s>>>(c, dst, src, keep, new_lens, n, status, n_pairs, entries, from, to, rows, free_list);
   else
-    update_kernel<false><<<1, kThreads, 0, s>>>(c, dst, src, keep, new_lens, n, status, n_pairs, entries, from, to, rows, owner, free_list);
+    update_kernel<false><<<1, kThreads, 0, s>>>(c, dst, src, keep, new_lens, n, status, n_pairs, entries, from, to, rows, free_list);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   return copy_pages(c, PairList{n_pairs, from, to, 1, n}, nullptr, nullptr, s);
