@@ -302,11 +302,14 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(dmoe_cache c, int32_t
 
 constexpr int kCopyThreads = 256;
 constexpr int kUnroll = 4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr long kUnit = kCopyThreads * kUnroll;  // 16-byte pieces of a unit: 16 KiB
 constexpr unsigned kCopyGrid = 4096;
 
 // Units of 16 KiB: (pair, layer, keys or values, part of the page).  With
-// `moved`, the table is rewritten too.
+// `moved`, the table is rewritten too.  Non-temporal both ways: 586 MB of a
+// compaction in 122 us against 130 through the caches (4.8 TB/s, the rate of a
+// large copy).
 __global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairList l, long page_len, const int32_t* moved,
                                                             int32_t* table_out) {
   const long gtid = static_cast<long>(blockIdx.x) * kCopyThreads + threadIdx.x;
@@ -326,16 +329,16 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairLi
     const int a = l.from[static_cast<long>(i) * l.step], b = l.to[static_cast<long>(i) * l.step];
     if (a < 0 || a >= c.n_pages || b < 0 || b >= c.n_pages) continue;
     uint4* pool = static_cast<uint4*>(kv ? c.v : c.k) + static_cast<long>(layer) * c.n_pages * page_len;
-    const uint4* s = pool + a * page_len + part * kUnit;
-    uint4* d = pool + b * page_len + part * kUnit;
+    const u32x4* s = (const u32x4*)pool + a * page_len + part * kUnit;
+    u32x4* d = (u32x4*)pool + b * page_len + part * kUnit;
     const long len = min(kUnit, page_len - part * kUnit);
-    uint4 x[kUnroll];
+    u32x4 x[kUnroll];
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j)
-      if (threadIdx.x + j * kCopyThreads < len) x[j] = s[threadIdx.x + j * kCopyThreads];
+      if (threadIdx.x + j * kCopyThreads < len) x[j] = __builtin_nontemporal_load(s + threadIdx.x + j * kCopyThreads);
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j)
-      if (threadIdx.x + j * kCopyThreads < len) d[threadIdx.x + j * kCopyThreads] = x[j];
+      if (threadIdx.x + j * kCopyThreads < len) __builtin_nontemporal_store(x[j], d + threadIdx.x + j * kCopyThreads);
   }
 }
 
