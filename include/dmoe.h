@@ -697,7 +697,7 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
  *   workspace  dmoe_attention_workspace_size bytes; holds the partial results
  *              of one dmoe_attention call at a time: calls that share it must
  *              not overlap in time
- * batch, n_heads and mask_block of dmoe_attention must be those of its plan.
+ * cache, batch, n_heads and mask_block of dmoe_attention must be those of its plan.
  * q, out: [T][n_heads][head_dim] of the cache's type, rows q_stride and
  * out_stride elements apart (multiples of 16 bytes); out must not overlap q.
  * lse: [T][n_heads].

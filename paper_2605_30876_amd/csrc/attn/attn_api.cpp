@@ -194,13 +194,13 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
 
 size_t dmoe_attention_plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
   if (!valid_shape(n_seqs, T, max_new, n_heads, n_kv_heads)) return 0;
-  return dmoe::plan_ints(dmoe::attn_shape(n_seqs, T, max_new, n_heads, n_kv_heads));
+  return dmoe::plan_ints(n_seqs, T, max_new, n_heads, n_kv_heads);
 }
 
 size_t dmoe_attention_workspace_size(dmoe_dtype dt, int n_seqs, int T, int max_new, int n_heads, int n_kv_heads,
                                      int head_dim) {
   if (!valid_dtype(dt) || !valid_shape(n_seqs, T, max_new, n_heads, n_kv_heads) || !valid_head_dim(head_dim)) return 0;
-  return dmoe::attn_workspace_bytes(dmoe::attn_shape(n_seqs, T, max_new, n_heads, n_kv_heads), n_kv_heads, dmoe::padded_dim(head_dim));
+  return dmoe::attn_workspace_bytes(n_seqs, T, max_new, n_heads, n_kv_heads, dmoe::padded_dim(head_dim));
 }
 
 dmoe_status dmoe_attention_plan(const dmoe_cache* cache, dmoe_batch batch, int n_heads, int mask_block, int32_t* plan,
@@ -212,7 +212,8 @@ dmoe_status dmoe_attention_plan(const dmoe_cache* cache, dmoe_batch batch, int n
   ALIGNED(plan);
   REQUIRE(mask_block >= 0, "mask_block=%d must be >= 0", mask_block);
   const dmoe::AttnShape sh = dmoe::attn_shape(*cache, batch, n_heads);
-  REQUIRE(plan_ints >= dmoe::plan_ints(sh), "a plan of %zu ints is smaller than the %zu needed", plan_ints, dmoe::plan_ints(sh));
+  const size_t ints = dmoe::plan_ints(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads);
+  REQUIRE(plan_ints >= ints, "a plan of %zu ints is smaller than the %zu needed", plan_ints, ints);
   return hip_status(dmoe::launch_attention_plan(*cache, batch, sh, mask_block, plan, static_cast<hipStream_t>(stream)), __func__);
 }
 
@@ -235,8 +236,10 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   ALIGNED(workspace);
   ALIGNED_TO(lse, 4);
   const dmoe::AttnShape sh = dmoe::attn_shape(*cache, batch, n_heads);
-  REQUIRE(plan_ints >= dmoe::plan_ints(sh), "a plan of %zu ints is smaller than the %zu needed", plan_ints, dmoe::plan_ints(sh));
-  const size_t need = dmoe::attn_workspace_bytes(sh, cache->n_kv_heads, dmoe::padded_dim(cache->head_dim));
+  const size_t ints = dmoe::plan_ints(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads);
+  REQUIRE(plan_ints >= ints, "a plan of %zu ints is smaller than the %zu needed", plan_ints, ints);
+  const size_t need = dmoe::attn_workspace_bytes(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads,
+                                                 dmoe::padded_dim(cache->head_dim));
   REQUIRE(ws_bytes >= need, "workspace of %zu bytes is smaller than the %zu bytes needed", ws_bytes, need);
   dmoe::AttnArgs a{*cache, layer, batch, n_heads, mask_block, q, q_stride, scale, plan, out, out_stride, lse, workspace};
   const hipStream_t s = static_cast<hipStream_t>(stream);

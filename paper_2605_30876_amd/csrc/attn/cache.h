@@ -104,10 +104,11 @@ struct AttnShape {
 };
 // Key tiles of a stage of the block kernel: up to 16 KiB of keys, or one tile.
 constexpr int stage_tiles(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) * kTileTokens <= 8192 ? 2 : 1; }
+// What any cache needs for these sizes.
+size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
+size_t attn_workspace_bytes(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads, int dp);
 // Two workgroups of the block kernel fit a CU where a wave's registers fit half of a SIMD's.
 constexpr bool two_per_cu(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) <= 256; }
-AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
-// The same for a cache of this type: the block kernel's form, and what it aims at.
 AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads);
 
 inline size_t plan_ints(const AttnShape& s) {

@@ -13,8 +13,10 @@ constexpr int kKeptSeqs = 512;  // sequences kept in LDS; further ones are read 
 constexpr int kSplitRows = 512;   // items of 32 rows
 constexpr int kSplitBlock = 512;  // items of 128 rows: as many workgroups as the device holds at once
 constexpr int kMinRows = 8;   // two a wave
-constexpr int kMinBlock = 4;  // two a wave of the 64-row form, two stages of the block kernel
+constexpr int kMinTwo = 6;    // 64 rows: three a wave
+constexpr int kMinBlock = 4;
 constexpr int kMinWide = 8;
+constexpr long kFewTiles = 16, kFewKeys = 2048;
 
 // Exclusive prefix sums over the workgroup's threads; *total is their sum.
 template <typename V>
@@ -162,36 +164,66 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
 
 }  // namespace
 
-AttnShape attn_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
+namespace {
+
+long most_rows(int T, int max_new, int group) { return static_cast<long>(max_new < T ? max_new : T) * group; }
+
+AttnShape shape_of(int tile_rows, int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
   AttnShape s;
   s.group = n_heads / n_kv_heads;
-  const long most = static_cast<long>(max_new < T ? max_new : T) * s.group;
-  s.tile_rows = most <= 32 ? 32 : most <= 64 ? 64 : 128;
-  const long by_seq = n_seqs * ((most + s.tile_rows - 1) / s.tile_rows);
-  const long by_rows = static_cast<long>(T) * s.group / s.tile_rows + n_seqs;
+  s.tile_rows = tile_rows;
+  const long by_seq = n_seqs * ((most_rows(T, max_new, s.group) + tile_rows - 1) / tile_rows);
+  const long by_rows = static_cast<long>(T) * s.group / tile_rows + n_seqs;
   s.max_tiles = by_seq < by_rows ? by_seq : by_rows;
-  const int aim = (s.tile_rows <= 64 ? kSplitRows : kSplitBlock) / n_kv_heads;
+  const int aim = (tile_rows <= 64 ? kSplitRows : kSplitBlock) / n_kv_heads;
   s.aim = aim > 1 ? aim : 1;
   s.split_items = s.aim;
-  s.min_tiles = s.tile_rows == 32 ? kMinRows : kMinBlock;
+  s.min_tiles = tile_rows == 32 ? kMinRows : tile_rows == 64 ? kMinTwo : kMinBlock;
   s.wide = false;
   s.unit = 1;
   return s;
 }
 
+}  // namespace
+
 AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
-  AttnShape s = attn_shape(b.n_seqs, b.T, b.max_new, n_heads, c.n_kv_heads);
-  if (s.tile_rows > 64) {
-    // one workgroup a CU: where a wave needs more than half of a SIMD's
-    // registers, and where eight waves work on an item, which they do if the
-    // batch's row tiles alone do not fill the device
-    const bool two = two_per_cu(c.dt, padded_dim(c.head_dim));
-    s.wide = two && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
-    if (!two || s.wide) s.aim = s.aim > 1 ? s.aim / 2 : 1;
-    if (s.wide) s.min_tiles = kMinWide;
-    s.unit = stage_tiles(c.dt, padded_dim(c.head_dim));
-  }
+  const long most = most_rows(b.T, b.max_new, n_heads / c.n_kv_heads);
+  auto shape = [&](int rows) { return shape_of(rows, b.n_seqs, b.T, b.max_new, n_heads, c.n_kv_heads); };
+  if (most <= 32) return shape(32);
+  // More than 64 rows a sequence: 128 to a workgroup read the cache once where
+  // 64 read it twice, but a workgroup of 64 starts sooner and there are twice as
+  // many.  64 where little is read: under kFewTiles row tiles of all kv heads, or kFewKeys
+  // (row tile, key tile) pairs at the sequences' longest.  A step of one sequence,
+  // 128 rows of four kv heads: 12.5 against 16.7 us a layer at 400 tokens, 17.1 against 18.9 at 4096, 26.7
+  // against 25.3 at 16000; of eight: 16.4 against 19.1 at 400, 31.8 against 30.2 at 4096.
+  const AttnShape two = shape(64);
+  const long tiles = two.max_tiles * c.n_kv_heads, keys = static_cast<long>(c.max_pages) * c.page_tokens / kTileTokens;
+  if (most <= 64 || tiles <= kFewTiles || tiles * keys <= kFewKeys) return two;
+  AttnShape s = shape(128);
+  // one workgroup a CU: where a wave needs more than half of a SIMD's
+  // registers, and where eight waves work on an item, which they do if the
+  // batch's row tiles alone do not fill the device
+  const bool half = two_per_cu(c.dt, padded_dim(c.head_dim));
+  s.wide = half && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
+  if (!half || s.wide) s.aim = s.aim > 1 ? s.aim / 2 : 1;
+  if (s.wide) s.min_tiles = kMinWide;
+  s.unit = stage_tiles(c.dt, padded_dim(c.head_dim));
   return s;
+}
+
+size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
+  size_t n = 0;
+  for (int rows : {32, 64, 128}) {
+    const size_t m = plan_ints(shape_of(rows, n_seqs, T, max_new, n_heads, n_kv_heads));
+    n = m > n && (rows > 32 || most_rows(T, max_new, n_heads / n_kv_heads) <= 32) ? m : n;
+  }
+  return n;
+}
+
+size_t attn_workspace_bytes(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads, int dp) {
+  const long most = most_rows(T, max_new, n_heads / n_kv_heads);
+  const int rows = most <= 32 ? 32 : most <= 64 ? 64 : 128;
+  return attn_workspace_bytes(shape_of(rows, n_seqs, T, max_new, n_heads, n_kv_heads), n_kv_heads, dp);
 }
 
 hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
