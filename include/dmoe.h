@@ -595,7 +595,7 @@ dmoe_status dmoe_rope_turns(int rot_dim, double base, dmoe_rope_scaling scaling,
  * same stride, else they must not overlap.  inverse: turned the other way
  * (a -> -a, the same scale): the gradient with respect to x of a forward call,
  * given the gradient of its output.
- * Limits: T >= 1; 1 <= n_heads <= 65535; head_dim a multiple of 8 in [8, 256].
+ * Limits: 1 <= T <= 2^26; 1 <= n_heads <= 65535; head_dim a multiple of 8 in [8, 256].
  */
 dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, dmoe_dtype dt, int T, int n_heads,
                       int head_dim, const int32_t* positions, dmoe_rotary rope, int inverse, void* stream);
@@ -650,7 +650,7 @@ size_t dmoe_cache_page_bytes(dmoe_dtype dt, int page_tokens, int n_kv_heads, int
  * slots out of range are cut to the range (rows outside [0, T) are never
  * touched, a sequence of a slot outside the table has no tokens).  max_new: an
  * upper bound of every sequence's new tokens (more are ignored).
- * Limits: 1 <= n_seqs <= 4096, n_slots if slots is NULL; T, max_new >= 1.
+ * Limits: 1 <= n_seqs <= 4096, n_slots if slots is NULL; 1 <= T <= 2^26; max_new >= 1.
  */
 typedef struct dmoe_batch {
   const int32_t* q_offsets;
@@ -684,7 +684,7 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
  * before them, as block diffusion does), and none if p < 0:
  *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j]) v[j],
  *   lse[t][h] = log sum_j exp(scale * q[t][h] . k[j])      (float32, optional).
- * A row that sees no key is 0 with lse -inf.  What a row does not see does not
+ * A row that sees no key, or only keys of score -inf, is 0 with lse -inf.  What a row does not see does not
  * reach it, whatever it holds (NaN and infinities included).  Scores, softmax statistics and
  * sums are float32; with DMOE_BF16 the probabilities are rounded to bf16
  * (relative 2^-8, the matrix operand's type), their sum is not.
@@ -702,7 +702,7 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
  * out_stride elements apart (multiples of 16 bytes); out must not overlap q.
  * lse: [T][n_heads].
  * Limits: n_heads a multiple of n_kv_heads, n_heads / n_kv_heads <= 1024;
- * scale > 0 and finite; T * n_heads < 2^31.
+ * scale > 0 and finite; T * n_heads <= 2^30.
  */
 size_t dmoe_attention_plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
 size_t dmoe_attention_workspace_size(dmoe_dtype dt, int n_seqs, int T, int max_new, int n_heads, int n_kv_heads,

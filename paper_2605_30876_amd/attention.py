@@ -13,8 +13,8 @@ plan and workspace of one batch shape.  A step is
 :func:`.layer.decode_step` calls between its MoE layers.
 
 Everything is enqueued on the current stream (or ``stream``); nothing is read
-back and nothing is allocated after construction where the outputs are given, so a step
-can be captured in a HIP graph.  An object's calls share its workspace: calls
+back, and calls whose outputs are given allocate nothing (but for a cache's
+workspace beyond 64 MB), so a step can be captured in a HIP graph.  An object's calls share its workspace: calls
 on one object must not overlap in time.
 """
 from __future__ import annotations
@@ -26,9 +26,10 @@ import torch
 from . import lib
 
 
-def _i32(t: torch.Tensor, name: str, n: int | None = None) -> torch.Tensor:
-    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() < n):
-        raise ValueError(f"{name} must be a contiguous int32 tensor" + (f" of at least {n} values" if n is not None else ""))
+def _i32(t: torch.Tensor, name: str, device, n: int = 0) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor on {device} of at least {n} values, "
+                         f"not {t.dtype} {list(t.shape)} on {t.device}")
     return t
 
 
@@ -39,6 +40,8 @@ class _On:
         self.device = device
 
     def __enter__(self):
+        if self.device.type != "cuda":
+            raise ValueError(f"the tensors are on {self.device}: the kernels need a GPU's")
         self.back = torch._C._cuda_getDevice()
         if self.device.index is not None and self.device.index != self.back:
             torch.cuda.set_device(self.device)
@@ -84,7 +87,7 @@ class Rope:
         out = x if out is None else _heads(out, "out", T, heads, dim, x.dtype, x.device)
         if T == 0:
             return out
-        _i32(positions, "positions", T)
+        _i32(positions, "positions", x.device, T)
         with _On(x.device):
             lib.dmoe_rope(x, out, T, heads, dim, positions, self.c, inverse, stream)
         return out
@@ -121,9 +124,11 @@ class PagedCache:
                 return torch.full(shape, fill, dtype=torch.int32, device=device)
             if tuple(t.shape) != shape:
                 raise ValueError(f"{name} must be int32 {list(shape)}")
-            return _i32(t, name)
+            return _i32(t, name, self.k.device)
 
         self.k, self.v = pool(k, "k"), pool(v, "v")
+        if self.v.device != self.k.device:
+            raise ValueError(f"k is on {self.k.device}, v on {self.v.device}")
         self.table = ints(table, "table", (n_slots, max_pages), -1)
         self.lens = ints(lens, "lens", (n_slots,), 0)
         self.refs = ints(refs, "refs", (n_pages,), 0)
@@ -131,16 +136,18 @@ class PagedCache:
         self.status = torch.zeros((1,), dtype=torch.int32, device=device)
         self.c = lib.dmoe_cache(lib.ptr(self.k), lib.ptr(self.v), lib.ptr(self.table), lib.ptr(self.lens), lib.ptr(self.refs),
                                 dt, n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages)
-        self._ws = None
+        # for calls on every slot, where that is not much; larger calls add one of their own
+        nbytes = max(lib.dmoe_cache_update_workspace_size(min(n_slots, 4096), max_pages, n_pages),
+                     lib.dmoe_cache_compact_workspace_size(n_pages))
+        self._ws = [torch.empty((min(nbytes, 64 << 20),), dtype=torch.uint8, device=device)]
 
     def _workspace(self, nbytes: int) -> torch.Tensor:
-        """Grown outside graph capture only: a captured call keeps the workspace it was captured with."""
-        if self._ws is None or self._ws.numel() < nbytes:
-            if self._ws is not None and torch.cuda.is_current_stream_capturing():
+        """The last workspace, or a larger one outside graph capture (a captured call keeps the one it was captured with)."""
+        if self._ws[-1].numel() < nbytes:
+            if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("the cache's workspace is too small for this call: run it once before capturing it")
-            self._kept = getattr(self, "_kept", []) + ([self._ws] if self._ws is not None else [])
-            self._ws = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
-        return self._ws
+            self._ws.append(torch.empty((nbytes,), dtype=torch.uint8, device=self.device))
+        return self._ws[-1]
 
     def update(self, dst: torch.Tensor, new_lens: torch.Tensor, src: torch.Tensor | None = None,
                keep: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
@@ -150,14 +157,15 @@ class PagedCache:
         n = dst.numel()
         if n == 0:
             return
-        _i32(dst, "dst"), _i32(new_lens, "new_lens", n)
+        d = self.device
+        _i32(dst, "dst", d), _i32(new_lens, "new_lens", d, n)
         for t, name in ((src, "src"), (keep, "keep")):
             if t is not None:
-                _i32(t, name, n)
+                _i32(t, name, d, n)
+        status = self.status if status is None else _i32(status, "status", d, 1)
         with _On(self.device):
             ws = self._workspace(lib.dmoe_cache_update_workspace_size(n, self.max_pages, self.n_pages))
-            lib.dmoe_cache_update(self.c, dst, src, keep, new_lens, n, self.status if status is None else _i32(status, "status", 1), ws,
-                                  stream)
+            lib.dmoe_cache_update(self.c, dst, src, keep, new_lens, n, status, ws, stream)
 
     def resize(self, slots: torch.Tensor, new_lens: torch.Tensor, stream=None):
         """Grows or truncates sequences to new_lens tokens."""
@@ -176,10 +184,10 @@ class PagedCache:
                 counts: torch.Tensor | None = None, stream=None):
         """Moves the live pages together at the pool's start.  table_out, refs_out: where the new table and counts
         go (default: in place); counts [2]: live pages, pages moved."""
-        table_out = self.table if table_out is None else _i32(table_out, "table_out", self.table.numel())
-        refs_out = self.refs if refs_out is None else _i32(refs_out, "refs_out", self.refs.numel())
+        table_out = self.table if table_out is None else _i32(table_out, "table_out", self.device, self.table.numel())
+        refs_out = self.refs if refs_out is None else _i32(refs_out, "refs_out", self.device, self.refs.numel())
         if counts is not None:
-            _i32(counts, "counts", 2)
+            _i32(counts, "counts", self.device, 2)
         with _On(self.device):
             ws = self._workspace(lib.dmoe_cache_compact_workspace_size(self.n_pages))
             lib.dmoe_cache_compact(self.c, table_out, refs_out, counts, ws, stream)
@@ -190,7 +198,7 @@ class PagedCache:
             return
         if pairs.dim() != 2 or pairs.shape[1] != 2:
             raise ValueError(f"pairs must be [n, 2], not {list(pairs.shape)}")
-        _i32(pairs, "pairs")
+        _i32(pairs, "pairs", self.device)
         with _On(self.device):
             lib.dmoe_cache_copy_pages(self.c, pairs, pairs.shape[0], stream)
 
@@ -213,8 +221,9 @@ class BlockAttention:
         if ints == 0:
             raise ValueError(f"no such batch: n_seqs={n_seqs}, T={T}, max_new={max_new}, n_heads={n_heads}, "
                              f"n_kv_heads={cache.n_kv_heads}")
-        if rope is not None and rope.rot_dim > cache.head_dim:
-            raise ValueError(f"rot_dim={rope.rot_dim} exceeds head_dim={cache.head_dim}")
+        if rope is not None and (rope.rot_dim > cache.head_dim or rope.turns.device != cache.device):
+            raise ValueError(f"a rotation of {rope.rot_dim} elements on {rope.turns.device} does not fit head_dim={cache.head_dim} on "
+                             f"{cache.device}")
         self._plan = torch.zeros((ints,), dtype=torch.int32, device=cache.device)
         nbytes = lib.dmoe_attention_workspace_size(cache.c.dt, n_seqs, T, max_new, n_heads, cache.n_kv_heads, cache.head_dim)
         self.workspace = torch.empty((nbytes,), dtype=torch.uint8, device=cache.device)
@@ -223,9 +232,9 @@ class BlockAttention:
     def begin(self, q_offsets: torch.Tensor, slots: torch.Tensor | None = None):
         """The step's batch: sequence i is rows q_offsets[i] .. q_offsets[i+1] of its tensors and slot slots[i]
         (default i) of the cache.  int32 device tensors, read by the calls that follow."""
-        _i32(q_offsets, "q_offsets", self.n_seqs + 1)
+        _i32(q_offsets, "q_offsets", self.cache.device, self.n_seqs + 1)
         if slots is not None:
-            _i32(slots, "slots", self.n_seqs)
+            _i32(slots, "slots", self.cache.device, self.n_seqs)
         self._kept = (q_offsets, slots)
         self.batch = lib.dmoe_batch(lib.ptr(q_offsets), lib.ptr(slots), self.n_seqs, self.T, self.max_new)
 
@@ -262,8 +271,9 @@ class BlockAttention:
         c = self.cache
         _heads(q, "q", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
         out = torch.empty_like(q) if out is None else _heads(out, "out", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < self.T * self.n_heads):
-            raise ValueError(f"lse must be contiguous float32 [{self.T}, {self.n_heads}]")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < self.T * self.n_heads
+                                or lse.device != c.device):
+            raise ValueError(f"lse must be contiguous float32 [{self.T}, {self.n_heads}] on {c.device}")
         with _On(c.device):
             lib.dmoe_attention(c.c, layer, self._started(), self.n_heads, self.mask_block, q, self.scale, self._plan, out, lse,
                                self.workspace, stream)
@@ -296,7 +306,9 @@ class AttentionLayer:
     def __call__(self, x: torch.Tensor, stream=None) -> torch.Tensor:
         """x [T, H] plus its attention (a buffer of this object)."""
         a, c, w = self.att, self.att.cache, self.w
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(c.device)):
+        if tuple(x.shape) != (a.T, self.H) or x.dtype != c.dtype or x.device != c.device:
+            raise ValueError(f"x must be {c.dtype} [{a.T}, {self.H}] on {c.device}, not {x.dtype} {list(x.shape)} on {x.device}")
+        with torch.no_grad(), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(c.device)):
             torch.mm(x, w["wq"].t(), out=self.q)
             torch.mm(x, w["wk"].t(), out=self.k)
             torch.mm(x, w["wv"].t(), out=self.v)

@@ -15,6 +15,8 @@ constexpr int kMaxKvHeads = 256;
 constexpr int kMaxGroup = 1024;
 constexpr int kMaxPageTokens = 1024;
 constexpr int kMaxEntries = 4096;
+constexpr int kMaxRows = 1 << 26;    // rows of a step's tensors: grids stay below 2^32 threads
+constexpr long kMaxHeadRows = 1 << 30;  // (row, head) pairs: a tile beyond the last still fits int32
 
 bool valid_head_dim(int d) { return d >= 8 && d <= 256 && d % 8 == 0; }
 bool valid_page(int page_tokens, int n_kv_heads, int head_dim) {
@@ -64,6 +66,7 @@ dmoe_status check_batch(const char* fn, const dmoe_cache* c, const dmoe_batch& b
   REQUIRE(b.n_seqs >= 1 && b.T >= 1 && b.max_new >= 1, "n_seqs=%d, T=%d and max_new=%d must be >= 1", b.n_seqs, b.T, b.max_new);
   REQUIRE(b.slots || b.n_seqs <= c->n_slots, "without slots n_seqs=%d must be at most n_slots=%d", b.n_seqs, c->n_slots);
   SUPPORT(b.n_seqs <= kMaxSeqs, "n_seqs=%d must be at most %d", b.n_seqs, kMaxSeqs);
+  SUPPORT(b.T <= kMaxRows, "T=%d must be at most %d", b.T, kMaxRows);
   ALIGNED_TO(b.q_offsets, 4);
   ALIGNED_TO(b.slots, 4);
   return DMOE_OK;
@@ -72,7 +75,7 @@ dmoe_status check_batch(const char* fn, const dmoe_cache* c, const dmoe_batch& b
 dmoe_status check_heads(const char* fn, int T, int n_heads, int n_kv_heads) {
   REQUIRE(n_heads >= 1 && n_heads % n_kv_heads == 0, "n_heads=%d must be a multiple of n_kv_heads=%d", n_heads, n_kv_heads);
   SUPPORT(n_heads / n_kv_heads <= kMaxGroup, "n_heads / n_kv_heads = %d must be at most %d", n_heads / n_kv_heads, kMaxGroup);
-  REQUIRE(static_cast<long>(T) * n_heads <= kIntLimit, "T*n_heads must fit in int32");
+  SUPPORT(static_cast<long>(T) * n_heads <= kMaxHeadRows, "T*n_heads must be at most %ld", kMaxHeadRows);
   return DMOE_OK;
 }
 
@@ -98,9 +101,9 @@ size_t span(long rows, long stride, long width, dmoe_dtype dt) {
 }
 
 bool valid_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
-  return n_seqs >= 1 && n_seqs <= kMaxSeqs && T >= 1 && max_new >= 1 && n_kv_heads >= 1 && n_kv_heads <= kMaxKvHeads &&
+  return n_seqs >= 1 && n_seqs <= kMaxSeqs && T >= 1 && T <= kMaxRows && max_new >= 1 && n_kv_heads >= 1 && n_kv_heads <= kMaxKvHeads &&
          n_heads >= 1 && n_heads % n_kv_heads == 0 && n_heads / n_kv_heads <= kMaxGroup &&
-         static_cast<long>(T) * n_heads <= kIntLimit;
+         static_cast<long>(T) * n_heads <= kMaxHeadRows;
 }
 
 }  // namespace
@@ -147,6 +150,7 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
   const long width = static_cast<long>(n_heads) * head_dim;
   REQUIRE(width <= kIntLimit, "n_heads*head_dim must fit in int32");
   SUPPORT(n_heads <= 65535, "n_heads=%d must be at most 65535", n_heads);
+  SUPPORT(T <= kMaxRows, "T=%d must be at most %d", T, kMaxRows);
   FORWARD(check_rope(__func__, rope, head_dim));
   ROWS(x, x_stride, width, dt);
   ROWS(out, out_stride, width, dt);

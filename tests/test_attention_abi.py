@@ -9,7 +9,7 @@ import torch
 
 import attention_ref as R
 from paper_2605_30876_amd import lib
-from paper_2605_30876_amd.attention import PagedCache
+from paper_2605_30876_amd.attention import BlockAttention, PagedCache
 
 # These calls pass host addresses as "device" pointers; validation must reject
 # them before any launch.  Never run them where a GPU could execute a launch.
@@ -82,6 +82,8 @@ def test_caches_and_batches(L, p, name):
     for over in BAD_BATCHES:
         assert status(L, name, *f(cache(p), batch(p, **over))) == BAD, over
     assert status(L, name, *f(cache(p), batch(p, slots=p, n_seqs=5000))) == NO
+    assert status(L, name, *f(cache(p), batch(p, T=(1 << 26) + 1))) == NO
+    assert status(L, name, *f(cache(p), batch(p, T=1 << 26), heads=32, qs=2048, os=2048)) == NO
     assert status(L, name, *f(cache(p), batch(p), heads=3)) == BAD
     assert status(L, name, *f(cache(p), batch(p), heads=0)) == BAD
     assert status(L, name, *f(cache(p), batch(p), heads=2 * 1025, qs=2 * 1025 * 64, os=2 * 1025 * 64)) == NO
@@ -119,6 +121,7 @@ def test_rope_refusals(L, p):
                  dict(dim=60), dict(dim=512), dict(xs=128), dict(xs=257), dict(os=512), dict(out=p + 32), dict(x=p + 8), dict(pos=p + 1),
                  dict(rope=lib.dmoe_rotary(p, 128, 0, 1.0)), dict(rope=lib.dmoe_rotary(p, 5, 0, 1.0))):
         assert call(**over) == BAD, over
+    assert call(T=(1 << 26) + 1) == NO and call(heads=65536, xs=1 << 23, os=1 << 23) == NO
 
 
 def test_page_refusals(L, p):
@@ -191,6 +194,14 @@ def test_cache_object_refuses_wrong_arrays():
     with pytest.raises(ValueError):
         PagedCache(1, 2, 32, 1, 64, 1, 1, device="cpu", table=torch.zeros(1, 1, dtype=torch.int64))
     c = PagedCache(1, 2, 32, 1, 64, 1, 1, device="cpu")
+    one = torch.zeros(1, dtype=torch.int32)
+    for call in (lambda: c.resize(one, one), c.compact, lambda: c.copy_pages(one.expand(1, 2).contiguous())):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    att = BlockAttention(c, 2, 1, 1, 1)
+    att.begin(torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError, match="GPU"):
+        att.plan()
     assert c.c.n_pages == 2 and c.table.tolist() == [[-1]] and c.k.shape == (1, 2, 32 * 64)
 
 

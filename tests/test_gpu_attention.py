@@ -19,7 +19,8 @@ BF16, F32 = torch.bfloat16, torch.float32
 class Setup:
     """A batch over a cache whose unused places hold NaN, pages in random order."""
 
-    def __init__(self, dtype, heads, kv_heads, dim, page, lens, new, mask, seed=0, layers=1, extra_rows=2, slack=3, scale=None):
+    def __init__(self, dtype, heads, kv_heads, dim, page, lens, new, mask, seed=0, layers=1, extra_rows=2, slack=3, scale=None,
+                 capacity=0):
         g = torch.Generator().manual_seed(seed)
         self.dtype, self.dim, self.lens, self.new, self.mask = dtype, dim, lens, new, mask
         n = len(lens)
@@ -27,7 +28,7 @@ class Setup:
         pages = sum(held) + slack
         ids = torch.randperm(pages, generator=g).tolist()
         slots = torch.randperm(n + 2, generator=g)[:n].tolist()
-        width = max(held + [0]) + 1
+        width = max(max(held + [0]) + 1, capacity // page)  # capacity: tokens that a slot has table entries for
         table = torch.full((n + 2, width), -1, dtype=torch.int32)
         all_lens = torch.full((n + 2,), 3, dtype=torch.int32)  # other slots: of no concern
         at = 0
@@ -72,8 +73,10 @@ class Setup:
         torch.cuda.synchronize()
         return out.cpu(), lse.cpu()
 
-    def check(self, out, lse, layer=0, see=None):
+    def check(self, out, lse, layer=0, see=None, skip=None):
         for i, (m, n) in enumerate(zip(self.lens, self.new)):
+            if i == skip:
+                continue
             rows = slice(self.off[i], self.off[i + 1])
             end = R.ends(range(m - n, m), m, self.mask) if see is None else see(i)
             ref = R.attention(self.q[layer, rows], self.k[i][layer], self.v[i][layer], end, self.scale)
@@ -111,6 +114,51 @@ def test_lengths(gpu_lib, lens, new, mask):
     s.check(*s.run())
     s = Setup(F32, 2, 1, 32, 64, lens, new, mask, seed=sum(lens) + mask, extra_rows=0)
     s.check(*s.run())
+
+
+# Batches for each form of the kernel: over 64 rows a sequence, many sequences
+# or a long table: 128 rows a workgroup, two halves of the keys each where the
+# row tiles of all kv heads are under 256; else 64 rows.
+FORMS = {"two_halves": (BF16, 8, 2, 128, 32, 9, 40000), "two_halves_64": (BF16, 6, 2, 64, 64, 10, 40000), "two_halves_f32": (F32, 6, 2, 64, 32, 9, 40000),
+         "one_80": (BF16, 64, 32, 80, 32, 9, 40000), "one_128": (BF16, 64, 32, 128, 64, 9, 40000), "one_32": (BF16, 96, 32, 24, 32, 9, 40000),
+         "one_wide_heads": (BF16, 6, 2, 192, 32, 9, 40000), "one_256": (BF16, 6, 2, 256, 32, 9, 40000), "one_f32": (F32, 6, 2, 128, 32, 9, 40000),
+         "one_f32_256": (F32, 6, 2, 200, 32, 9, 40000), "sixty_four": (BF16, 8, 2, 128, 32, 4, 0), "sixty_four_f32": (F32, 6, 2, 96, 32, 4, 0)}
+
+
+def _form(name, mask, seed=1, **kw):
+    dtype, heads, kv, dim, page, n, capacity = FORMS[name]
+    lens, new = [333, 64, 0, 900, 33, 128, 5, 0, 97, 41][:n], [40, 33, 0, 21, 1, 40, 9, 2, 0, 4][:n]
+    return Setup(dtype, heads, kv, dim, page, lens, new, mask, seed=seed, capacity=capacity, **kw)
+
+
+@pytest.mark.parametrize("mask", [0, 1, 24, 64])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_forms(gpu_lib, form, mask):
+    s = _form(form, mask)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_forms_with_poison_and_holes(gpu_lib, form):
+    """Values that are not finite behind a causal row, and pages missing in front of it."""
+    s = _form(form, 1)
+    i, m, n = 3, s.lens[3], s.new[3]
+    first = m - n + n // 2
+    _poison(s, i, list(range(first, m)), float("nan"), "v")
+    _poison(s, i, [first + 1], float("inf"), "k")
+    holes = (0, 4) if s.page == 32 else (1, 2)
+    for j in holes:
+        s.cache.table[s.slots[i], j] = -1
+    out, lse = s.run()
+    keep = [p for p in range(m) if p // s.page not in holes]
+    k, v = s.k[i][0][keep], s.v[i][0][keep]
+    rows = slice(s.off[i], s.off[i] + n // 2)
+    end = torch.tensor([sum(p <= q for p in keep) for q in range(m - n, first)])
+    ref = R.attention(s.q[0, rows], k, v, end, s.scale)
+    tol, ltol = R.bounds(s.dtype, s.dim, m, *ref)
+    assert bool(((out[rows].double() - ref[0]).abs() <= tol).all()) and bool(((lse[rows].double() - ref[1]).abs() <= ltol).all())
+    assert not torch.isfinite(out[s.off[i] + n // 2:s.off[i + 1]]).any()
+    s.check(out, lse, skip=i)  # the other sequences are what they were
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -299,3 +347,11 @@ def test_wrong_tensors_are_refused(gpu_lib):
         s.att.attend(1, q)
     with pytest.raises(RuntimeError):
         BlockAttention(s.cache, 4, 1, 6, 8).plan()
+    with pytest.raises(ValueError):
+        s.att.begin(s.offd.cpu())
+    with pytest.raises(ValueError):
+        s.att.begin(s.offd, s.slotsd.long())
+    with pytest.raises(ValueError):
+        s.cache.resize(s.slotsd.cpu(), s.slotsd)
+    with pytest.raises(ValueError):
+        s.att.attend(0, q, lse=torch.zeros(8, 4))
