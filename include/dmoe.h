@@ -622,7 +622,7 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
  * nothing is stored there and no key is seen there.
  * Limits: n_layers, n_pages, n_slots, max_pages >= 1; page_tokens a multiple
  * of 32 up to 1024; n_kv_heads in [1, 256]; head_dim a multiple of 8 in [8, 256];
- * n_slots <= 65536; max_pages * page_tokens < 2^31.
+ * n_slots <= 65536; max_pages * page_tokens <= 2^30.
  */
 typedef struct dmoe_cache {
   void* k;

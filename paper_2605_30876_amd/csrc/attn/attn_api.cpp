@@ -15,6 +15,7 @@ constexpr int kMaxKvHeads = 256;
 constexpr int kMaxGroup = 1024;
 constexpr int kMaxPageTokens = 1024;
 constexpr int kMaxEntries = 4096;
+constexpr long kMaxTokens = 1 << 30;  // of a sequence: a tile beyond the last still fits int32
 constexpr int kMaxRows = 1 << 26;    // rows of a step's tensors: grids stay below 2^32 threads
 constexpr long kMaxHeadRows = 1 << 30;  // (row, head) pairs: a tile beyond the last still fits int32
 
@@ -53,7 +54,7 @@ dmoe_status check_cache(const char* fn, const dmoe_cache* c, bool refs) {
   REQUIRE(valid_page(c->page_tokens, c->n_kv_heads, c->head_dim),
           "page_tokens=%d must be a multiple of 32 up to %d, n_kv_heads=%d in [1, %d], head_dim=%d a multiple of 8 in [8, 256]",
           c->page_tokens, kMaxPageTokens, c->n_kv_heads, kMaxKvHeads, c->head_dim);
-  REQUIRE(static_cast<long>(c->max_pages) * c->page_tokens <= kIntLimit, "max_pages*page_tokens must fit in int32");
+  REQUIRE(static_cast<long>(c->max_pages) * c->page_tokens <= kMaxTokens, "max_pages*page_tokens must be at most %ld", kMaxTokens);
   SUPPORT(c->n_slots <= kMaxSlots, "n_slots=%d must be at most %d", c->n_slots, kMaxSlots);
   REQUIRE(!misaligned(c->k) && !misaligned(c->v), "the cache's k and v must be 16-byte aligned");
   REQUIRE(!misaligned_to(c->table, 4) && !misaligned_to(c->lens, 4) && !misaligned_to(c->refs, 4),
