@@ -24,6 +24,9 @@
  *                              the routing of the same forward)
  *   dmoe_combine               y_t = sum_j w[t,j] * FFN_{e_tj}(x_t) + FFN_s(x_t)
  *
+ * The attention that precedes the MoE layer in a model (rotary positions, a
+ * paged key/value cache, attention over it) is the section at the end.
+ *
  * dmoe_route_block / dmoe_route_token / dmoe_route_topp run the routing steps
  * and the schedule of one routing mode as one call with fewer kernel
  * launches; and two layout conversions for the expert FFN's operands:

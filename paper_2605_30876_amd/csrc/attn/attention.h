@@ -26,15 +26,16 @@ constexpr float kLazy = 8.f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// c: values of a 16-byte chunk; a matrix operand (1 KiB, one chunk per lane)
-// covers 2c elements of the head dimension (keys) or 2c tokens (values).
-template <typename T>
-struct Types;
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4);
 }
+
+// c: values of a 16-byte chunk; a matrix operand (1 KiB, one chunk per lane)
+// covers 2c elements of the head dimension (keys) or 2c tokens (values).
+template <typename T>
+struct Types;
 template <>
 struct Types<bf16_t> {
   typedef bf16x8 Frag;
@@ -285,8 +286,8 @@ struct TileMap {
   const __attribute__((address_space(4))) int32_t* table;
   long page_len, layer0;
   int hkv, n_pages, shift;  // tiles of a page: 1 << shift, or -shift of them
-  __device__ __forceinline__ TileMap(const AttnArgs& a, int slot, int hk)
-      : table((const __attribute__((address_space(4))) int32_t*)(a.cache.table + static_cast<long>(slot) * a.cache.max_pages)), hkv(a.cache.n_kv_heads), n_pages(a.cache.n_pages) {
+  __device__ __forceinline__ TileMap(const AttnArgs& a, int slot, int hk) : hkv(a.cache.n_kv_heads), n_pages(a.cache.n_pages) {
+    table = (const __attribute__((address_space(4))) int32_t*)(a.cache.table + static_cast<long>(slot) * a.cache.max_pages);
     const int tpp = a.cache.page_tokens / kTileTokens;
     shift = (tpp & (tpp - 1)) == 0 ? 31 - __builtin_clz(tpp) : -tpp;
     page_len = static_cast<long>(a.cache.page_tokens) * DP;
@@ -381,6 +382,15 @@ struct RowPlace {
 // joined through LDS.  The cache goes straight into registers, past the caches
 // where one wave alone reads a tile; the next tile's keys are issued when this
 // one's are used up, its values likewise.
+//
+// Bound by the cache's bytes: bf16, 32 query and 8 kv heads of 128, one token
+// over 131k: 537 MB in 85 us (6.3 TB/s); 64 of up to 16k: 1.08 GB in 181 us
+// (6.0 TB/s).  The matrix instructions mostly multiply rows that are not there
+// (4 of 32 here), which costs nothing: a CU's four could take 16 times the
+// bytes it gets.  With loads through the caches the first took 96 us.  Short
+// sequences are a chain of round trips: item and queries 1.6 us, keys and
+// values 0.6, a tile's arithmetic 0.5 (fp32, 64 elements: 2.3), the join 1.1, the
+// stores 0.5.
 template <typename T, int DP, int kWR>
 __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef WaveRows<T, DP> Rows;
@@ -507,9 +517,19 @@ struct BlockStage {
 };
 
 //
+// Bound by issue: bf16, 4096 tokens over 12k, 16 query and 4 kv heads of 128:
+// 490 to 550 us, 880 to 980 TFLOP/s of 1430 that a library product of 8192^3
+// reaches.  The matrix pipes are busy 52 % of the cycles and vector
+// instructions fill most of the rest (about 75 a tile and wave, 16 of them
+// exponentials at a quarter of the rate).  Measured and not kept: the next
+// tile's scores formed between the exponentials by scheduling groups (+5 %: the
+// accumulators are copied more), operands read four ahead (+3 %), wave priorities
+// around the matrix instructions (0 %).
+//
 // kWK = 2: eight waves, each four on one half of the item's keys, joined
 // through LDS: half the partial results of two such workgroups, which matters
-// where few row tiles are cut into many items.
+// where few row tiles are cut into many items (sixteen blocks of 32 tokens over up to
+// 8k: kernel and join 22.3 + 7.1 -> 22.1 + 4.9 us; 64 MB of keys and values).
 template <typename T, int DP, int kWK>
 __global__ __launch_bounds__(256 * kWK, waves_per_simd<T>(DP)) void attention_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef WaveRows<T, DP> Rows;
@@ -684,7 +704,8 @@ __global__ __launch_bounds__(256 * kWK, waves_per_simd<T>(DP)) void attention_bl
 #pragma unroll
       for (int b = 0; b < kB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) store4(sums + (4 * b + i / 4) * 256 + lane * 4, f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
+        for (int i = 0; i < 16; i += 4)
+          store4(sums + (4 * b + i / 4) * 256 + lane * 4, f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
     }
     __syncthreads();
     if (wk) return;
@@ -709,7 +730,10 @@ __global__ __launch_bounds__(256 * kWK, waves_per_simd<T>(DP)) void attention_bl
 // Partial results of a row tile joined, pieces in fixed order.  A workgroup
 // takes 8 rows, which lie side by side in every KiB of the partial sums: a
 // wave reads 128 bytes of each, lane = (16-byte piece of the KiB, row), and the
-// waves share the pieces.
+// waves share the pieces.  4.2 us for 17 pieces of 512 rows, 4.9 for 7 of 8192;
+// with the sums stored row by row and a workgroup per row 14 and 15.  Eight waves
+// were faster for one sequence's 127 pieces (8.3 against 11.4 us) and slower for
+// many rows (9.4 against 4.8).
 constexpr int kMergeWaves = 4, kMergeRows = 8;
 
 template <typename T, int DP>

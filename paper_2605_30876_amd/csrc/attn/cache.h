@@ -53,6 +53,30 @@ __device__ __forceinline__ Seq load_seq(const dmoe_cache& c, const dmoe_batch& b
   return s;
 }
 
+// Exclusive prefix sums over a workgroup's kThreads threads, waves[kThreads/64]
+// in LDS; *total is their sum.
+template <int kThreads, typename V>
+__device__ __forceinline__ V scan_exclusive(V v, V* waves, V* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  V x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const V y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  V base = 0, sum = 0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) {
+    base += i < wave ? waves[i] : 0;
+    sum += waves[i];
+  }
+  __syncthreads();
+  *total = sum;
+  return base + x - v;
+}
+
 // Keys that the token at position p sees (a prefix of the sequence).
 __host__ __device__ __forceinline__ int visible_end(int p, int len, int mask_block) {
   if (p < 0) return 0;
@@ -75,9 +99,12 @@ struct AttnItem {
   int page[6];
   int pad;
 };
-// Where the second half of an item's key tiles starts: the first has as many pairs of tiles, or one more.
-__host__ __device__ constexpr int item_middle(int kt0, int kt1) { return kt0 + ((kt1 - kt0 + 1) / 2 + 1) / 2 * 2 < kt1 ? kt0 + ((kt1 - kt0 + 1) / 2 + 1) / 2 * 2 : kt1; }
-
+// Where the second half of an item's key tiles starts: the first has as many
+// pairs of tiles, or one more.
+__host__ __device__ constexpr int item_middle(int kt0, int kt1) {
+  const int first = ((kt1 - kt0 + 1) / 2 + 1) / 2 * 2;
+  return first < kt1 - kt0 ? kt0 + first : kt1;
+}
 struct AttnMerge {
   int row0, first, rows;      // as above
   int part, pieces;           // partial results part .. part + pieces-1

@@ -1,5 +1,9 @@
 // The attention's work items, made on the device: a step's lengths never
-// visit the host, and every layer of the step uses the one plan.
+// visit the host, and every layer of the step uses the one plan.  One
+// workgroup: prefix sums over sequences and row tiles, then an item per thread.
+// 4.8 us for one sequence, 5.5 for 64: half of it the launch, the rest three
+// round trips (offsets and slots, lengths, page ids) and the barriers; 1024
+// threads took 7.5.
 #include "cache.h"
 
 namespace dmoe {
@@ -17,29 +21,6 @@ constexpr int kMinTwo = 6;    // 64 rows: three a wave
 constexpr int kMinBlock = 4;
 constexpr int kMinWide = 8;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
-
-// Exclusive prefix sums over the workgroup's threads; *total is their sum.
-template <typename V>
-__device__ __forceinline__ V scan_exclusive(V v, V* waves, V* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  V x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const V y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  if (lane == 63) waves[wave] = x;
-  __syncthreads();
-  V base = 0, sum = 0;
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) {
-    base += i < wave ? waves[i] : 0;
-    sum += waves[i];
-  }
-  __syncthreads();
-  *total = sum;
-  return base + x - v;
-}
 
 // Largest i with a[i] <= x, for a[0] = 0 <= x < a[n].
 __device__ __forceinline__ int find(const int* a, int n, int x) {
@@ -79,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
       n = static_cast<int>((static_cast<long>(q.n) * sh.group + sh.tile_rows - 1) / sh.tile_rows);
     }
     int total;
-    const int at = scan_exclusive(n, iwaves, &total);
+    const int at = scan_exclusive<kThreads>(n, iwaves, &total);
     if (i < b.n_seqs) tiles[i] = n_tiles + at;
     n_tiles += total;
   }
@@ -104,7 +85,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   long keys = r.kt;
   for (int t = tid + kThreads; t < n_tiles; t += kThreads) keys += load_tile(t).kt;
   long all;
-  scan_exclusive(keys, lwaves, &all);
+  scan_exclusive<kThreads>(keys, lwaves, &all);
   // Pieces of `chunk` key tiles: sum ceil(kt / chunk) <= n_tiles + all / chunk,
   // and all / chunk <= room <= split_items, which the arrays' sizes count on.
   // Items of 128 rows leave partial results of 64 KiB: they fill one round of
@@ -127,7 +108,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
     // three sums at once, 21 bits each: a pass has at most kThreads + split items
     const long mine = pieces | (pieces > 1 ? static_cast<long>(pieces) << 21 | 1l << 42 : 0);
     long sum;
-    const long at = scan_exclusive(mine, lwaves, &sum);
+    const long at = scan_exclusive<kThreads>(mine, lwaves, &sum);
     constexpr long kBits = (1 << 21) - 1;
     const int total = static_cast<int>(sum & kBits);
     const int part = n_parts + static_cast<int>(at >> 21 & kBits);

@@ -20,7 +20,7 @@ L, HEADS, KV, DIM, PAGE = 3, 8, 2, 64, 32
 
 
 class Model:
-    def __init__(self, name, routing, seqs=None):
+    def __init__(self, name, routing, seqs=None, heads=HEADS, kv=KV, dim=DIM):
         cfg = get_config(name)
         self.cfg = cfg = cfg if seqs is None else cfg.with_(name=f"{name}_{seqs}", NB=seqs)
         self.routing, self.n, self.bs, self.T = routing, cfg.NB, cfg.bs, cfg.NB * cfg.bs
@@ -29,12 +29,12 @@ class Model:
         dt = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
         self.m = [MoELayer(cfg.H, cfg.E, cfg.I, cfg.I_s, cfg.k, cfg.NB, cfg.bs, dtype=dt, device="cuda") for _ in range(L)]
         self.xs = [ds[0]["x"]] + [torch.empty_like(ds[0]["x"]) for _ in range(L - 1)]
-        self.cache = PagedCache(L, 12 * self.n, PAGE, KV, DIM, self.n + 1, 6, dtype=dt)
-        self.att = BlockAttention(self.cache, HEADS, self.n, self.bs, self.T, mask_block=self.bs, rope=Rope(DIM // 2))
+        self.cache = PagedCache(L, 12 * self.n, PAGE, kv, dim, self.n + 1, 6, dtype=dt)
+        self.att = BlockAttention(self.cache, heads, self.n, self.bs, self.T, mask_block=self.bs, rope=Rope(dim // 2))
         g = torch.Generator(device="cuda").manual_seed(5)
         new = lambda *s: torch.randn(*s, generator=g, device="cuda").mul_(1 / math.sqrt(s[1])).to(dt)  # noqa: E731
-        self.al = [AttentionLayer(self.att, l, {"wq": 3 * new(HEADS * DIM, cfg.H), "wk": new(KV * DIM, cfg.H), "wv": new(KV * DIM, cfg.H),
-                                                "wo": new(cfg.H, HEADS * DIM)}) for l in range(L)]
+        self.al = [AttentionLayer(self.att, l, {"wq": 3 * new(heads * dim, cfg.H), "wk": new(kv * dim, cfg.H), "wv": new(kv * dim, cfg.H),
+                                                "wo": new(cfg.H, heads * dim)}) for l in range(L)]
         i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
         self.slots, self.i32 = i32(list(range(self.n))), i32
         self.att.begin(i32([i * self.bs for i in range(self.n + 1)]), self.slots)
@@ -88,9 +88,11 @@ def test_generation(gpu_lib, name, routing, seqs):
     m.check_attention()
 
 
-def test_captured_step_equals_eager(gpu_lib):
-    m = Model("small_bf16", "block", 1)
-    e = Model("small_bf16", "block", 1)
+@pytest.mark.parametrize("name,heads,kv,dim", [("small_bf16", HEADS, KV, DIM), ("decode_b1", 16, 4, 128)])
+def test_captured_step_equals_eager(gpu_lib, name, heads, kv, dim):
+    """The projections are library products of these sizes: what they record in a graph is replayed here too."""
+    m = Model(name, "block", 1, heads, kv, dim)
+    e = Model(name, "block", 1, heads, kv, dim)
     for x in (m, e):
         x.cache.resize(x.slots, x.i32([x.bs] * x.n))
         x.step()
