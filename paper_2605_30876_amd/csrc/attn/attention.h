@@ -92,8 +92,18 @@ constexpr int waves_per_simd(int dp) {
   return two_per_cu(sizeof(T) == 4 ? DMOE_F32 : DMOE_BF16, dp) ? 2 : 1;
 }
 
+// Queries, keys, values and sums of a wave of the rows kernel pass its 512
+// registers: the queries stay in LDS, and keys and values take turns in
+// one set of registers.  fp32, 256 elements, 64 single tokens of 4096, 16 query
+// and 4 kv heads: 923 us with all in registers, and much of it in scratch; 802 with
+// the turns alone; 532 with both (2.1 GB of keys and values, 4.0 TB/s).
+template <typename T>
+constexpr bool rows_tight(int dp) {
+  return dp * sizeof(T) > 768;
+}
+
 // A wave's 32 rows against tiles of 32 keys.
-template <typename T, int DP>
+template <typename T, int DP, bool kQLds = false>
 struct WaveRows {
   typedef Types<T> Ty;
   typedef typename Ty::Frag Frag;
@@ -102,6 +112,7 @@ struct WaveRows {
   static constexpr int kB = DP / 32;       // 32-wide blocks of the output
   static constexpr int kS = 16 / c;        // operands of a tile's values per block
   Frag q[kK];
+  const Frag* ql;  // kQLds: the queries, read from here
   f32x16 o[kB];
   float m, l;  // l: of this half's keys
   int end;     // keys the row sees
@@ -133,7 +144,7 @@ struct WaveRows {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < kK; ++j) Ty::mma(s, k[j], q[j]);
+    for (int j = 0; j < kK; ++j) Ty::mma(s, k[j], kQLds ? ql[64 * j] : q[j]);
     return s;
   }
 
@@ -335,7 +346,8 @@ template <typename T, int DP>
 struct RowPlace {
   int row, tok, qh;
   bool live, any;
-  __device__ __forceinline__ RowPlace(WaveRows<T, DP>& w, const AttnArgs& a, const AttnItem& it, int g, int hk, int row_lo, int lane) {
+  template <typename Rows>
+  __device__ __forceinline__ RowPlace(Rows& w, const AttnArgs& a, const AttnItem& it, int g, int hk, int row_lo, int lane) {
     constexpr int c = Types<T>::c;
     typedef typename Types<T>::Frag Frag;
     const int row_hi = min(row_lo + 32, it.rows) - 1;
@@ -351,7 +363,7 @@ struct RowPlace {
     w.hi = any ? visible_end(pos0 + row_hi / g, it.len, a.mask_block) : 0;
     const T* qp = static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
 #pragma unroll
-    for (int j = 0; j < WaveRows<T, DP>::kK; ++j) {
+    for (int j = 0; j < Rows::kK; ++j) {
       const int d = (2 * j + (lane >> 5)) * c;
       Frag f{};
       if (live && d < a.cache.head_dim) f = *reinterpret_cast<const Frag*>(qp + d);
@@ -359,9 +371,10 @@ struct RowPlace {
     }
   }
   // The wave's sums: divided into out, or as they are into the workspace.
-  __device__ __forceinline__ void store(const WaveRows<T, DP>& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk,
+  template <typename Rows>
+  __device__ __forceinline__ void store(const Rows& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk,
                                         int half, int part_rows) const {
-    constexpr int kB = WaveRows<T, DP>::kB;
+    constexpr int kB = Rows::kB;
     if (!live) return;
     if (it.part >= 0) {
       const long at = (static_cast<long>(it.part) * a.cache.n_kv_heads + hk) * sh.tile_rows + (row - it.first);
@@ -407,7 +420,8 @@ struct RowPlace {
 // stores 0.5.
 template <typename T, int DP, int kWR>
 __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
-  typedef WaveRows<T, DP> Rows;
+  constexpr bool kTight = rows_tight<T>(DP);
+  typedef WaveRows<T, DP, kTight> Rows;
   typedef typename Rows::Frag Frag;
   constexpr int c = Rows::c, kK = Rows::kK, kB = Rows::kB, kS = Rows::kS, kWK = 4 / kWR;
   extern __shared__ float lds[];
@@ -420,6 +434,15 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
   Rows w;
   w.clear();
   const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wr, lane);
+  if constexpr (kTight) {
+    Frag* ql = reinterpret_cast<Frag*>(lds) + wr * (kK * 64) + lane;
+    if (wk == 0) {
+#pragma unroll
+      for (int j = 0; j < kK; ++j) ql[64 * j] = w.q[j];
+    }
+    w.ql = ql;
+    __syncthreads();
+  }
   const float scale2 = a.scale * kLog2e;
   const TileMap<T, DP> map(a, it.slot, hk);
   const int kt1 = min(it.kt1, (w.hi + kTileTokens - 1) / kTileTokens);
@@ -442,9 +465,10 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
   int kt = it.kt0 + wk;
   int page = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
   int page1 = map.page(kt + kWK, kt1);
+  long at = map.holds(page) ? map.at(kt, page) : 0;
   if (map.holds(page)) {
-    load_k(map.k + map.at(kt, page));
-    load_v(map.v + map.at(kt, page));
+    load_k(map.k + at);
+    if (!kTight) load_v(map.v + at);
   }
   bool left = false;  // tiles for add_by_key
   auto turn = [&](auto masked) {
@@ -454,7 +478,12 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
     const long at1 = more ? map.at(kt + kWK, page1) : 0;
     f32x16 s[1];
     if (here) s[0] = w.scores(k);
-    if (more) load_k(map.k + at1);
+    if (kTight) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (here) load_v(map.v + at);
+    } else if (more) {
+      load_k(map.k + at1);
+    }
     if (here) {
       const int key0 = kt * kTileTokens;
       w.template softmax<1>(s, scale2, key0, masked, half);
@@ -463,8 +492,10 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
       else
         left = true;
     }
-    if (more) load_v(map.v + at1);
+    if (kTight) __builtin_amdgcn_sched_barrier(0);
+    if (more) kTight ? load_k(map.k + at1) : load_v(map.v + at1);
     kt += kWK;
+    at = at1;
     page = page1;
     page1 = page2;
   };
@@ -483,7 +514,7 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
   constexpr int kLen = (16 * kB + 2) * 64;
 #pragma unroll
   for (int n = kWK / 2; n >= 1; n /= 2) {
-    float* buf = lds + (wr * (kWK / 2) + wk % n) * kLen;
+    float* buf = lds + (kTight ? kWR * kK * 256 : 0) + (wr * (kWK / 2) + wk % n) * kLen;
     if (wk >= n && wk < 2 * n) {
       buf[lane] = w.m;
       buf[64 + lane] = w.l;
@@ -861,7 +892,7 @@ hipError_t launch_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
   const unsigned items = static_cast<unsigned>(sh.max_items() * hkv);
   const int part_rows = static_cast<int>(sh.max_parts() * hkv * sh.tile_rows);
   if (sh.tile_rows <= 64) {
-    constexpr size_t lds = 2 * (16 * (DP / 32) + 2) * 64 * sizeof(float);
+    const size_t lds = 2 * (16 * (DP / 32) + 2) * 64 * sizeof(float) + (rows_tight<T>(DP) ? sh.tile_rows * DP * sizeof(T) : 0);
     if (sh.tile_rows == 32)
       attention_rows_kernel<T, DP, 1><<<items, 256, lds, s>>>(a, sh, part_rows);
     else

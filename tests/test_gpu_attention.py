@@ -118,16 +118,21 @@ def test_lengths(gpu_lib, lens, new, mask):
 
 # Batches for each form of the kernel: over 64 rows a sequence, many sequences
 # or a long table: 128 rows a workgroup, two halves of the keys each where the
-# row tiles of all kv heads are under 256; else 64 rows.
+# row tiles of all kv heads are under 256; else 64 rows, or 32 where a sequence
+# has no more.
 FORMS = {"two_halves": (BF16, 8, 2, 128, 32, 9, 40000), "two_halves_64": (BF16, 6, 2, 64, 64, 10, 40000), "two_halves_f32": (F32, 6, 2, 64, 32, 9, 40000),
          "one_80": (BF16, 64, 32, 80, 32, 9, 40000), "one_128": (BF16, 64, 32, 128, 64, 9, 40000), "one_32": (BF16, 96, 32, 24, 32, 9, 40000),
          "one_wide_heads": (BF16, 6, 2, 192, 32, 9, 40000), "one_256": (BF16, 6, 2, 256, 32, 9, 40000), "one_f32": (F32, 6, 2, 128, 32, 9, 40000),
-         "one_f32_256": (F32, 6, 2, 200, 32, 9, 40000), "sixty_four": (BF16, 8, 2, 128, 32, 4, 0), "sixty_four_f32": (F32, 6, 2, 96, 32, 4, 0)}
+         "one_f32_256": (F32, 6, 2, 200, 32, 9, 40000), "sixty_four": (BF16, 8, 2, 128, 32, 4, 0), "sixty_four_f32": (F32, 6, 2, 96, 32, 4, 0),
+         "sixty_four_f32_256": (F32, 6, 2, 200, 32, 4, 0), "sixty_four_256": (BF16, 6, 2, 256, 32, 4, 0),
+         "thirty_two": (BF16, 2, 2, 128, 64, 4, 0), "thirty_two_192": (BF16, 2, 2, 192, 32, 4, 0), "thirty_two_f32_256": (F32, 2, 2, 256, 32, 4, 0)}
 
 
 def _form(name, mask, seed=1, **kw):
     dtype, heads, kv, dim, page, n, capacity = FORMS[name]
     lens, new = [333, 64, 0, 900, 33, 128, 5, 0, 97, 41][:n], [40, 33, 0, 21, 1, 40, 9, 2, 0, 4][:n]
+    if name.startswith("thirty_two"):
+        new = [min(x, 32 * kv // heads) for x in new]
     return Setup(dtype, heads, kv, dim, page, lens, new, mask, seed=seed, capacity=capacity, **kw)
 
 
