@@ -124,6 +124,7 @@ struct AttnShape {
   long max_tiles;  // row tiles of the batch at most
   long split_items;  // items that splitting along the keys may add, and merges, at most
   int aim;           // items that splitting aims at: at most split_items
+  int even_tiles;    // 128 rows: key tiles of a piece at least, where pieces even out lengths
   bool wide;         // block kernel: two halves of an item's keys per workgroup
   int unit;          // key tiles that an item's range is a multiple of (stage_tiles)
   __host__ __device__ long max_items() const { return max_tiles + split_items; }

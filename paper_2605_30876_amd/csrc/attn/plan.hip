@@ -20,6 +20,9 @@ constexpr int kMinRows = 8;   // two a wave
 constexpr int kMinTwo = 6;    // 64 rows: three a wave
 constexpr int kMinBlock = 4;
 constexpr int kMinWide = 8;
+// Pieces that even out row tiles of 128, key tiles: long enough not to notice their partial results.
+constexpr int kEvenBf16 = 48;
+constexpr int kEvenF32 = 16;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
 
 // Largest i with a[i] <= x, for a[0] = 0 <= x < a[n].
@@ -49,7 +52,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   __shared__ int parts[kThreads];
   __shared__ int iwaves[kThreads / 64];
   __shared__ long lwaves[kThreads / 64];
+  __shared__ int longest;  // key tiles of a row tile at most
   const int tid = threadIdx.x;
+  if (tid == 0) longest = 0;
   int n_tiles = 0;
   for (int i0 = 0; i0 < b.n_seqs; i0 += kThreads) {
     const int i = i0 + tid;
@@ -83,19 +88,34 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   };
   Tile r = load_tile(tid);
   long keys = r.kt;
-  for (int t = tid + kThreads; t < n_tiles; t += kThreads) keys += load_tile(t).kt;
+  int most = r.kt;
+  for (int t = tid + kThreads; t < n_tiles; t += kThreads) {
+    const int kt = load_tile(t).kt;
+    keys += kt;
+    most = max(most, kt);
+  }
+  if (most > 0) atomicMax(&longest, most);
   long all;
   scan_exclusive<kThreads>(keys, lwaves, &all);
   // Pieces of `chunk` key tiles: sum ceil(kt / chunk) <= n_tiles + all / chunk,
-  // and all / chunk <= room <= split_items, which the arrays' sizes count on.
+  // and all / chunk <= split_items, which the arrays' sizes count on.
   // Items of 128 rows leave partial results of 64 KiB: they fill one round of
-  // workgroups but do not pass it, and with row tiles of about one length that
-  // are more than half of the aim nothing is split.  Those of 32 rows are cheap
-  // to join: pieces of the average length even the sequences out, of half of it
-  // where there are many sequences (64 of up to 16k tokens: 191 -> 181 us).
+  // workgroups but do not pass it, and row tiles of about one length that are more
+  // than half of the aim are not split.  Of uneven lengths they are, into two
+  // rounds, in pieces that are long beside their partial results: 60 blocks of up
+  // to 16k, 12 query and 3 kv heads of 32: 93 -> 69 us; 48 of up to 8k, 64 and 8 of 128: 285 -> 250;
+  // fp32, 73 of 24 tokens of up to 5k, 10 and 2 of 96: 240 -> 195.  With fewer row tiles it costs
+  // more than it evens out: 32 blocks of up to 16k, 16 and 4 of 128: 66 -> 74.
+  // Items of 32 rows are cheap to join: pieces of the average length even the
+  // sequences out, of half of it where there are many sequences (64 of up to 16k tokens:
+  // 191 -> 181 us).
   const long split = sh.aim;
-  const long room = sh.tile_rows <= 64 ? (n_tiles > split / 2 ? sh.split_items : split) : max(max(split - n_tiles, split / 2), 1l);
-  const int chunk = static_cast<int>(max(static_cast<long>(sh.min_tiles), (all + room - 1) / room));
+  const bool many = n_tiles > split / 2;
+  const long room = sh.tile_rows <= 64 ? (many && sh.tile_rows == 32 ? sh.split_items : split) : max(max(split - n_tiles, split / 2), 1l);
+  long len = max(static_cast<long>(sh.min_tiles), (all + room - 1) / room);
+  if (sh.tile_rows == 128 && many && 10l * longest * n_tiles > 13 * all)
+    len = min(len, max(static_cast<long>(sh.even_tiles), (all + 2 * split - 1) / (2 * split)));
+  const int chunk = static_cast<int>(len);
 
   AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
   AttnItem* out = reinterpret_cast<AttnItem*>(head + 1);
@@ -159,8 +179,10 @@ AttnShape shape_of(int tile_rows, int n_seqs, int T, int max_new, int n_heads, i
   s.max_tiles = by_seq < by_rows ? by_seq : by_rows;
   const int aim = (tile_rows <= 64 ? kSplitRows : kSplitBlock) / n_kv_heads;
   s.aim = aim > 1 ? aim : 1;
-  s.split_items = tile_rows == 32 ? 2 * s.aim : s.aim;
+  // twice the aim where the plan may go for it: always with 32 rows, with 128 where it may find many row tiles
+  s.split_items = tile_rows == 32 || (tile_rows == 128 && s.max_tiles > s.aim / 2) ? 2 * s.aim : s.aim;
   s.min_tiles = tile_rows == 32 ? kMinRows : tile_rows == 64 ? kMinTwo : kMinBlock;
+  s.even_tiles = 0;
   s.wide = false;
   s.unit = 1;
   return s;
@@ -189,6 +211,7 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   s.wide = half && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
   if (!half || s.wide) s.aim = s.aim > 1 ? s.aim / 2 : 1;
   if (s.wide) s.min_tiles = kMinWide;
+  s.even_tiles = c.dt == DMOE_F32 ? kEvenF32 : kEvenBf16;
   s.unit = stage_tiles(c.dt, padded_dim(c.head_dim));
   return s;
 }

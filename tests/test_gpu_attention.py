@@ -166,6 +166,15 @@ def test_forms_with_poison_and_holes(gpu_lib, form):
     s.check(out, lse, skip=i)  # the other sequences are what they were
 
 
+@pytest.mark.parametrize("dtype,dim,lens", [(BF16, 80, [60, 9000, 40, 40, 4000, 33, 40, 50, 64]), (F32, 96, [3200, 64, 50, 40, 40, 33, 90, 40]),
+                                            (BF16, 32, [6000, 64, 50, 1700, 40])])
+def test_uneven_row_tiles(gpu_lib, dtype, dim, lens):
+    """As many row tiles of 128 as the device takes at once, a few of them far longer: cut so that they even out."""
+    s = Setup(dtype, 64, 32, dim, 32, lens, [40 - i for i in range(len(lens))], 1, seed=dim, capacity=40000)
+    s.check(*s.run())
+    s.check(*s.run())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_many_sequences(gpu_lib, dtype):
     lens = [(7 * i * i) % 211 for i in range(150)]
