@@ -220,7 +220,8 @@ __device__ __forceinline__ Seq find_tile(const AppendArgs& a, int x, int tiles, 
 }
 
 // blockIdx.x: tile of 32 positions.  blockIdx.y: the values of one
-// kv head each, then (8 tokens, group of `heads` heads) of the queries and keys.
+// kv head each, then (8 of the tile's new tokens, group of `heads` heads) of the
+// queries and keys.
 template <typename T, bool kAligned>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tiles, int heads, int groups) {
   constexpr int c = Chunk<T>::c;
@@ -230,8 +231,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tile
   const Seq q = find_tile(a, blockIdx.x, tiles, tile0);
   const int start = max(q.pos0, 0);
   const int y = static_cast<int>(blockIdx.y) - hkv;
-  const int from = y < 0 ? tile0 : tile0 + y / groups * kTokens;
-  const int p0 = max(start, from), p1 = min(q.len, from + (y < 0 ? kTileTokens : kTokens)), n = p1 - p0;
+  const int end = min(q.len, tile0 + kTileTokens);
+  const int p0 = max(start, tile0) + (y < 0 ? 0 : y / groups * kTokens), p1 = y < 0 ? end : min(end, p0 + kTokens), n = p1 - p0;
   if (n <= 0) return;
   const long t0 = q.row0 + (p0 - q.pos0);
   const int dp = padded_dim(dim), pt = a.cache.page_tokens;
@@ -291,27 +292,34 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tile
   }
 }
 
-// Heads of a workgroup that rotates: as many as keep kGroups workgroups, so
-// that angles are formed for as many heads as possible.
-constexpr long kGroups = 1024;
-int heads_of_workgroup(long token_groups, int n_heads) {
+// Heads of a workgroup that rotates.  One where that leaves few workgroups (a
+// block of 32 tokens, 20 heads: 4.2 us against 4.5 with four); else as many as its lanes
+// take at once (64 single tokens: 8.1 us with one, 6.2 with four; 46 sequences of 2, 24 heads of
+// 32: 15.5 with one, 6.1), and as keep kGroups workgroups, so that angles are formed for
+// as many heads as possible.  launched: token groups of the grid, some empty.
+constexpr long kFill = 512, kGroups = 1024;
+int heads_of_workgroup(long launched, long token_groups, int n_heads, int chunks) {
+  int lanes = 1;  // of a row, as in rotate_rows
+  while (lanes < (chunks + 1) / 2) lanes *= 2;
   int heads = 1;
+  while (heads < n_heads && heads * lanes * kTokens < kThreads && launched * ((n_heads + heads - 1) / heads) > kFill) heads *= 2;
   while (heads < n_heads && token_groups * ((n_heads + 2 * heads - 1) / (2 * heads)) >= kGroups) heads *= 2;
   return heads < n_heads ? heads : n_heads;
 }
 
 template <typename T>
 hipError_t append(const AppendArgs& a, hipStream_t s) {
-  constexpr int kSub = kTileTokens / kTokens;
   const int most = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const int tiles = (most + kTileTokens - 2) / kTileTokens + 1;
   const int turned = a.cache.n_kv_heads + (a.q ? a.n_heads : 0), dp = padded_dim(a.cache.head_dim);
-  const int heads = heads_of_workgroup((a.batch.T + kTokens - 1) / kTokens, turned);
-  const int groups = (turned + heads - 1) / heads;
   const size_t lds = static_cast<size_t>(kTileTokens) * dp * sizeof(T);
-  // n tokens lie in at most n / 32 + 2 tiles
+  // n tokens lie in at most n / 32 + 2 tiles, and at most `most` of a tile's positions are new
   const long each = static_cast<long>(a.batch.n_seqs) * tiles, counted = a.batch.T / kTileTokens + 2l * a.batch.n_seqs;
-  const dim3 grid(static_cast<unsigned>(each < counted ? each : counted), a.cache.n_kv_heads + kSub * groups);
+  const long grid_tiles = each < counted ? each : counted;
+  const int sub = ((most < kTileTokens ? most : kTileTokens) + kTokens - 1) / kTokens;
+  const int heads = heads_of_workgroup(grid_tiles * sub, (a.batch.T + kTokens - 1) / kTokens, turned, dp / Chunk<T>::c);
+  const int groups = (turned + heads - 1) / heads;
+  const dim3 grid(static_cast<unsigned>(grid_tiles), a.cache.n_kv_heads + sub * groups);
   if (aligned_pairs(a.rope, Chunk<T>::c))
     append_kernel<T, true><<<grid, kThreads, lds, s>>>(a, each <= counted ? tiles : 0, heads, groups);
   else
@@ -323,7 +331,7 @@ template <typename T>
 hipError_t rope(const void* x, long x_stride, void* out, long out_stride, int T_, int n_heads, int dim, const int32_t* positions,
                 const dmoe_rotary& r, bool inverse, hipStream_t s) {
   const int groups = (T_ + kTokens - 1) / kTokens;
-  const int heads = heads_of_workgroup(groups, n_heads);
+  const int heads = heads_of_workgroup(groups, groups, n_heads, dim / Chunk<T>::c);
   const dim3 grid(groups, (n_heads + heads - 1) / heads);
   auto run = [&](auto kernel) {
     kernel<<<grid, kThreads, 0, s>>>(static_cast<const T*>(x), x_stride, static_cast<T*>(out), out_stride, T_, n_heads, heads, dim, positions,
