@@ -565,11 +565,12 @@ struct BlockStage {
 };
 
 //
-// Bound by issue: bf16, 4096 tokens over 12k, 16 query and 4 kv heads of 128:
-// 490 to 550 us, 880 to 980 TFLOP/s of 1430 that a library product of 8192^3
-// reaches.  The matrix pipes are busy 52 % of the cycles and vector
+// Bound by issue and power: bf16, 4096 tokens over 12k, 16 query and 4 kv heads of
+// 128: 490 to 550 us, 880 to 980 TFLOP/s of 1430 that a library product of 8192^3
+// reaches.  The matrix pipes are busy 51 % of the cycles and vector
 // instructions fill most of the rest (about 75 a tile and wave, 16 of them
-// exponentials at a quarter of the rate).  Measured and not kept: the next
+// exponentials at a quarter of the rate).  The clock falls under it: with values
+// of 0 the same instructions take 450 us, with keys of 0 too 418.  Measured and not kept: the next
 // tile's scores formed between the exponentials by scheduling groups (+5 %: the
 // accumulators are copied more), operands read four ahead (+3 %), wave priorities
 // around the matrix instructions (0 %).

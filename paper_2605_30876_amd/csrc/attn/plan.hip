@@ -94,7 +94,13 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
     keys += kt;
     most = max(most, kt);
   }
-  if (most > 0) atomicMax(&longest, most);
+  const long split = sh.aim;
+  const bool many = n_tiles > split / 2;
+  if (sh.tile_rows == 128 && many) {
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) most = max(most, __shfl_xor(most, d));
+    if ((tid & 63) == 0) atomicMax(&longest, most);
+  }
   long all;
   scan_exclusive<kThreads>(keys, lwaves, &all);
   // Pieces of `chunk` key tiles: sum ceil(kt / chunk) <= n_tiles + all / chunk,
@@ -109,8 +115,6 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   // Items of 32 rows are cheap to join: pieces of the average length even the
   // sequences out, of half of it where there are many sequences (64 of up to 16k tokens:
   // 191 -> 181 us).
-  const long split = sh.aim;
-  const bool many = n_tiles > split / 2;
   const long room = sh.tile_rows <= 64 ? (many && sh.tile_rows == 32 ? sh.split_items : split) : max(max(split - n_tiles, split / 2), 1l);
   long len = max(static_cast<long>(sh.min_tiles), (all + room - 1) / room);
   if (sh.tile_rows == 128 && many && 10l * longest * n_tiles > 13 * all)
