@@ -19,6 +19,7 @@ on one object must not overlap in time.
 """
 from __future__ import annotations
 
+import contextlib
 import math
 
 import torch
@@ -31,6 +32,11 @@ def _i32(t: torch.Tensor, name: str, device, n: int = 0) -> torch.Tensor:
         raise ValueError(f"{name} must be a contiguous int32 tensor on {device} of at least {n} values, "
                          f"not {t.dtype} {list(t.shape)} on {t.device}")
     return t
+
+
+def _stream(stream):
+    """The current stream set to a call's: what the call allocates and fills for itself is then ordered with its kernels."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class _On:
@@ -173,7 +179,8 @@ class PagedCache:
 
     def free(self, slots: torch.Tensor, stream=None):
         """Releases every page of the sequences."""
-        self.update(slots, torch.zeros_like(slots), stream=stream)
+        with _stream(stream):
+            self.update(slots, torch.zeros_like(slots), stream=stream)
 
     def fork(self, dst: torch.Tensor, src: torch.Tensor, keep: torch.Tensor, new_lens: torch.Tensor | None = None, stream=None):
         """Slot dst[i] becomes the first keep[i] tokens of slot src[i], sharing its full pages; with room for

@@ -1,0 +1,39 @@
+"""Calls of the attention's objects as a program makes them: on another stream than the current one, with batches that
+shrink, plans that outlive a compaction, updates that are refused, several hundred sequences, pages of every size.
+Marked ``gpu``."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as R
+from paper_2605_30876_amd.attention import AttentionLayer, BlockAttention, PagedCache, Rope
+from test_gpu_attention import FORMS, Setup, _form, _poison
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _busy():
+    """Keeps the current stream occupied for a while (at most a second) without the host's waiting."""
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+
+
+def test_free_on_another_stream(gpu_lib):
+    """What free() makes for its call is made on the call's stream: the current one is behind."""
+    cache = PagedCache(1, 64, 32, 1, 32, 8, 8)
+    slots, side = i32(list(range(8))), torch.cuda.Stream()
+    cache.resize(slots, i32([40] * 8))
+    blocks = [torch.full_like(slots, 7) for _ in range(32)]  # what an allocation on the current stream finds in its memory
+    torch.cuda.synchronize()
+    del blocks
+    _busy()
+    cache.free(slots, stream=side)
+    side.synchronize()
+    assert cache.lens.tolist() == [0] * 8 and int(cache.status[0]) == 0 and int(cache.refs.sum()) == 0
