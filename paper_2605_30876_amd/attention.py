@@ -273,11 +273,15 @@ class BlockAttention:
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
                stream=None) -> torch.Tensor:
-        """Attention of the (rotated) queries over the cache, into out [T, n_heads, head_dim]; lse [T, n_heads]
-        (float32) receives the log-sum-exp of every row."""
+        """Attention of the (rotated) queries over the cache, into out [T, n_heads, head_dim] (default: a new tensor,
+        allocated on the call's stream); lse [T, n_heads] (float32) receives the log-sum-exp of every row."""
         c = self.cache
         _heads(q, "q", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
-        out = torch.empty_like(q) if out is None else _heads(out, "out", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
+        if out is None:
+            with _stream(stream):
+                out = torch.empty_like(q)
+        else:
+            _heads(out, "out", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < self.T * self.n_heads
                                 or lse.device != c.device):
             raise ValueError(f"lse must be contiguous float32 [{self.T}, {self.n_heads}] on {c.device}")

@@ -37,3 +37,24 @@ def test_free_on_another_stream(gpu_lib):
     cache.free(slots, stream=side)
     side.synchronize()
     assert cache.lens.tolist() == [0] * 8 and int(cache.status[0]) == 0 and int(cache.refs.sum()) == 0
+
+
+def _pending(like, n=24):
+    """Tensors that are read on the current stream once it gets to it, and whose memory is free to the allocator."""
+    xs = [torch.full_like(like, 3.0) for _ in range(n)]
+    _busy()
+    ys = [x.clone() for x in xs]
+    del xs
+    return ys
+
+
+def test_attend_on_another_stream_allocates_there(gpu_lib):
+    s = Setup(BF16, 8, 2, 64, 32, [500], [8], 8, seed=8)
+    want, _ = s.run()
+    side = torch.cuda.Stream()
+    ys = _pending(s.qd[0])
+    got = s.att.attend(0, s.qd[0], stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert all(bool((y == 3.0).all()) for y in ys)
+    assert torch.equal(got[:8].cpu(), want[:8])
