@@ -147,12 +147,14 @@ class PagedCache:
                      lib.dmoe_cache_compact_workspace_size(n_pages))
         self._ws = [torch.empty((min(nbytes, 64 << 20),), dtype=torch.uint8, device=device)]
 
-    def _workspace(self, nbytes: int) -> torch.Tensor:
-        """The last workspace, or a larger one outside graph capture (a captured call keeps the one it was captured with)."""
+    def _workspace(self, nbytes: int, stream) -> torch.Tensor:
+        """The last workspace, or a larger one of the call's stream outside graph capture (a captured call keeps the one
+        it was captured with)."""
         if self._ws[-1].numel() < nbytes:
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("the cache's workspace is too small for this call: run it once before capturing it")
-            self._ws.append(torch.empty((nbytes,), dtype=torch.uint8, device=self.device))
+            with _stream(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("the cache's workspace is too small for this call: run it once before capturing it")
+                self._ws.append(torch.empty((nbytes,), dtype=torch.uint8, device=self.device))
         return self._ws[-1]
 
     def update(self, dst: torch.Tensor, new_lens: torch.Tensor, src: torch.Tensor | None = None,
@@ -170,7 +172,7 @@ class PagedCache:
                 _i32(t, name, d, n)
         status = self.status if status is None else _i32(status, "status", d, 1)
         with _On(self.device):
-            ws = self._workspace(lib.dmoe_cache_update_workspace_size(n, self.max_pages, self.n_pages))
+            ws = self._workspace(lib.dmoe_cache_update_workspace_size(n, self.max_pages, self.n_pages), stream)
             lib.dmoe_cache_update(self.c, dst, src, keep, new_lens, n, status, ws, stream)
 
     def resize(self, slots: torch.Tensor, new_lens: torch.Tensor, stream=None):
@@ -196,7 +198,7 @@ class PagedCache:
         if counts is not None:
             _i32(counts, "counts", self.device, 2)
         with _On(self.device):
-            ws = self._workspace(lib.dmoe_cache_compact_workspace_size(self.n_pages))
+            ws = self._workspace(lib.dmoe_cache_compact_workspace_size(self.n_pages), stream)
             lib.dmoe_cache_compact(self.c, table_out, refs_out, counts, ws, stream)
 
     def copy_pages(self, pairs: torch.Tensor, stream=None):

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import attention_ref as R
+from paper_2605_30876_amd import lib
 from paper_2605_30876_amd.attention import AttentionLayer, BlockAttention, PagedCache, Rope
 from test_gpu_attention import FORMS, Setup, _form, _poison
 
@@ -58,3 +59,19 @@ def test_attend_on_another_stream_allocates_there(gpu_lib):
     torch.cuda.synchronize()
     assert all(bool((y == 3.0).all()) for y in ys)
     assert torch.equal(got[:8].cpu(), want[:8])
+
+
+def test_a_larger_workspace_is_allocated_on_the_calls_stream(gpu_lib):
+    """An update of more entries than the cache has slots (refused: some come twice) needs a workspace of its own."""
+    cache = PagedCache(1, 64, 32, 1, 32, 4, 128)
+    n, side = 3000, torch.cuda.Stream()
+    slots, lens = i32([i % 4 for i in range(n)]), i32([1] * n)
+    before = cache._ws[-1].numel()
+    nbytes = lib.dmoe_cache_update_workspace_size(n, cache.max_pages, cache.n_pages)
+    assert nbytes > before
+    ys = _pending(torch.empty((nbytes // 4,), device="cuda"))
+    cache.resize(slots, lens, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert all(bool((y == 3.0).all()) for y in ys)
+    assert int(cache.status[0]) == -1 and cache.lens.tolist() == [0] * 4
