@@ -103,7 +103,8 @@ class PagedCache:
     """Keys and values of ``n_layers`` layers in ``n_pages`` pages of
     ``page_tokens`` tokens, held by ``n_slots`` sequences of up to
     ``max_pages`` pages.  k, v, table, lens, refs: existing arrays to use
-    (layouts: dmoe_cache in include/dmoe.h) instead of new, empty ones."""
+    (layouts: dmoe_cache in include/dmoe.h) instead of new, empty ones; the
+    others are then made on their device."""
 
     def __init__(self, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, n_slots: int,
                  max_pages: int, dtype: torch.dtype = torch.bfloat16, device="cuda", k=None, v=None, table=None, lens=None,
@@ -117,6 +118,8 @@ class PagedCache:
         self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads = n_layers, n_pages, page_tokens, n_kv_heads
         self.head_dim, self.n_slots, self.max_pages, self.dtype = head_dim, n_slots, max_pages, dtype
         elems = page_bytes // torch.empty((), dtype=dtype).element_size()
+        # new arrays lie where the given ones do: a kernel follows the addresses of all of them
+        device = next((t.device for t in (k, v, table, lens, refs) if t is not None), device)
 
         def pool(t, name):
             if t is None:
