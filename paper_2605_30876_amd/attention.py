@@ -316,11 +316,10 @@ class AttentionLayer:
         self.att, self.layer, self.w, self.H = att, layer, w, H
         new = lambda n: torch.empty((att.T, n), dtype=c.dtype, device=c.device)  # noqa: E731
         self.q, self.k, self.v = new(q), new(kv), new(kv)
-        self.o = torch.zeros((att.T, q), dtype=c.dtype, device=c.device)  # rows of no sequence stay 0
-        self.out = new(H)
+        self.o, self.out = new(q), new(H)
 
     def __call__(self, x: torch.Tensor, stream=None) -> torch.Tensor:
-        """x [T, H] plus its attention (a buffer of this object)."""
+        """x [T, H] plus its attention (a buffer of this object); rows of no sequence are x's."""
         a, c, w = self.att, self.att.cache, self.w
         if tuple(x.shape) != (a.T, self.H) or x.dtype != c.dtype or x.device != c.device:
             raise ValueError(f"x must be {c.dtype} [{a.T}, {self.H}] on {c.device}, not {x.dtype} {list(x.shape)} on {x.device}")
@@ -330,6 +329,8 @@ class AttentionLayer:
             torch.mm(x, w["wv"].t(), out=self.v)
             q = self.q.view(a.T, a.n_heads, c.head_dim)
             a.append(self.layer, self.k.view(a.T, c.n_kv_heads, c.head_dim), self.v.view(a.T, c.n_kv_heads, c.head_dim), q)
+            # rows of no sequence are 0 whichever they are: offsets change from step to step, also under a captured call
+            self.o.zero_()
             a.attend(self.layer, q, self.o.view(a.T, a.n_heads, c.head_dim))
             torch.addmm(x, self.o, w["wo"].t(), out=self.out)
         return self.out

@@ -75,3 +75,56 @@ def test_a_larger_workspace_is_allocated_on_the_calls_stream(gpu_lib):
     torch.cuda.synchronize()
     assert all(bool((y == 3.0).all()) for y in ys)
     assert int(cache.status[0]) == -1 and cache.lens.tolist() == [0] * 4
+
+
+class Half:
+    """One layer's attention half over two sequences of up to eight new tokens."""
+
+    def __init__(self, dtype=BF16, n=2, new=8, H=96, heads=4, kv=2, dim=32):
+        g = torch.Generator(device="cuda").manual_seed(11)
+        mat = lambda *s: torch.randn(*s, generator=g, device="cuda").mul_(1 / math.sqrt(s[1])).to(dtype)  # noqa: E731
+        self.cache = PagedCache(1, 20, 32, kv, dim, n, 4, dtype=dtype)
+        self.T, self.slots = n * new, i32(list(range(n)))
+        self.cache.resize(self.slots, i32([40 + 3 * i for i in range(n)]))
+        self.cache.k.zero_(), self.cache.v.fill_(0.5)
+        self.att = BlockAttention(self.cache, heads, n, new, self.T, mask_block=new, rope=Rope(dim))
+        self.w = {"wq": mat(heads * dim, H), "wk": mat(kv * dim, H), "wv": mat(kv * dim, H), "wo": mat(H, heads * dim)}
+        self.layer = AttentionLayer(self.att, 0, self.w)
+        self.off = i32([new * i for i in range(n + 1)])
+        self.x = mat(self.T, H)
+
+    def step(self, layer=None):
+        self.att.begin(self.off, self.slots)
+        self.att.plan()
+        return (layer or self.layer)(self.x).clone()
+
+
+@pytest.mark.parametrize("how", ["fewer rows", "no such slot", "a graph"])
+def test_rows_that_dropped_out_keep_nothing(gpu_lib, how):
+    """A full batch, then a smaller one: rows of no sequence are the input, as in a layer that has done nothing before."""
+    h = Half()
+    full = h.step()
+    assert not torch.equal(full[8:], h.x[8:])
+    if how == "a graph":
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            h.step()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                y = h.step()
+        torch.cuda.current_stream().wait_stream(side)
+    for off, slots in (([0, 8, 8], [0, 1]), ([0, 8, 16], [0, 1]), ([0, 5, 5], [0, 1]), ([0, 8, 16], [0, 9 if how == "no such slot" else 1])):
+        h.off.copy_(torch.tensor(off, dtype=torch.int32))
+        h.slots.copy_(torch.tensor(slots, dtype=torch.int32))
+        torch.cuda.synchronize()
+        if how == "a graph":
+            g.replay()
+            torch.cuda.synchronize()
+            got = y.clone()
+        else:
+            got = h.step()
+        want = h.step(AttentionLayer(h.att, 0, h.w))
+        assert torch.equal(got, want)
+        used = 8 if slots[1] == 9 else off[2]
+        assert torch.equal(got[used:], h.x[used:])
