@@ -103,8 +103,8 @@ class PagedCache:
     """Keys and values of ``n_layers`` layers in ``n_pages`` pages of
     ``page_tokens`` tokens, held by ``n_slots`` sequences of up to
     ``max_pages`` pages.  k, v, table, lens, refs: existing arrays to use
-    (layouts: dmoe_cache in include/dmoe.h) instead of new, empty ones; the
-    others are then made on their device."""
+    (layouts: dmoe_cache in include/dmoe.h) instead of new, empty ones (keys
+    and values 0); the others are then made on their device."""
 
     def __init__(self, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, n_slots: int,
                  max_pages: int, dtype: torch.dtype = torch.bfloat16, device="cuda", k=None, v=None, table=None, lens=None,
@@ -123,7 +123,7 @@ class PagedCache:
 
         def pool(t, name):
             if t is None:
-                return torch.empty((n_layers, n_pages, elems), dtype=dtype, device=device)
+                return torch.zeros((n_layers, n_pages, elems), dtype=dtype, device=device)
             if tuple(t.shape) != (n_layers, n_pages, elems) or t.dtype != dtype or not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous {dtype} [{n_layers}, {n_pages}, {elems}]")
             return t

@@ -128,3 +128,12 @@ def test_rows_that_dropped_out_keep_nothing(gpu_lib, how):
         assert torch.equal(got, want)
         used = 8 if slots[1] == 9 else off[2]
         assert torch.equal(got[used:], h.x[used:])
+
+
+def test_a_new_cache_holds_zeros(gpu_lib):
+    """Tokens that are given room but never stored are attended to like any others: not whatever the memory held."""
+    c = PagedCache(2, 8, 32, 2, 64, 1, 8)
+    blocks = [torch.full_like(c.k, float("nan")) for _ in range(16)]
+    del blocks, c
+    c = PagedCache(2, 8, 32, 2, 64, 1, 8)
+    assert (c.k == 0).all() and (c.v == 0).all()
