@@ -694,8 +694,9 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
  *
  * dmoe_attention_plan cuts the step's rows and keys into work items: long
  * sequences are split along their keys so that a few rows still use the whole
- * device.  It reads q_offsets, slots and lens and is valid until they change;
- * every layer of a step uses the same plan.
+ * device.  It goes by q_offsets, slots and lens and is valid until they change;
+ * every layer of a step uses the same plan.  Pages may move (dmoe_cache_compact,
+ * an update that keeps the lengths): dmoe_attention goes by the table as it is.
  *   plan       int32 [dmoe_attention_plan_ints] device memory
  *   workspace  dmoe_attention_workspace_size bytes; holds the partial results
  *              of one dmoe_attention call at a time: calls that share it must

@@ -256,7 +256,8 @@ class BlockAttention:
         return self.batch
 
     def plan(self, stream=None):
-        """The step's work items, for :meth:`attend` of every layer: after the lengths are set, before the first attend."""
+        """The step's work items, for :meth:`attend` of every layer: after the lengths are set, before the first attend;
+        until offsets, slots or lengths change (pages may move)."""
         with _On(self.cache.device):
             lib.dmoe_attention_plan(self.cache.c, self._started(), self.n_heads, self.mask_block, self._plan, stream)
 

@@ -465,10 +465,18 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
   int kt = it.kt0 + wk;
   int page = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
   int page1 = map.page(kt + kWK, kt1);
-  long at = map.holds(page) ? map.at(kt, page) : 0;
-  if (map.holds(page)) {
-    load_k(map.k + at);
-    if (!kTight) load_v(map.v + at);
+  long at;
+  auto first = [&] {
+    at = map.holds(page) ? map.at(kt, page) : 0;
+    if (map.holds(page)) {
+      load_k(map.k + at);
+      if (!kTight) load_v(map.v + at);
+    }
+  };
+  first();
+  if (const int now = map.page(kt, kt1); now != page) {  // moved since the plan was made
+    page = now;
+    first();
   }
   bool left = false;  // tiles for add_by_key
   auto turn = [&](auto masked) {
@@ -699,10 +707,19 @@ __global__ __launch_bounds__(256 * kWK, waves_per_simd<T>(DP)) void attention_bl
 #pragma unroll
   for (int n = 0; n < kTS; ++n) {
     pg.id[n] = wk ? it.page[4 + n] : kt + n < kt1 ? it.page[n] : -1;
-    pg1.id[n] = wk || (kWK > 1 && kt + kTS + n >= kt1) ? -1 : it.page[kTS + n];
   }
-  if (wk) pg1 = pages(kt + kTS);
   load(kt, pg, s0);
+  __builtin_amdgcn_sched_barrier(0);
+  const Ids now = pages(kt);
+  pg1 = pages(kt + kTS);
+  bool moved = false;  // since the plan was made
+#pragma unroll
+  for (int n = 0; n < kTS; ++n) moved = moved || now.id[n] != pg.id[n];
+  if (moved) {
+    pg = now;
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the stage is loaded again
+    load(kt, pg, s0);
+  }
   __builtin_amdgcn_sched_barrier(0);
   auto turn = [&](auto masked, Stage& cur, Stage& fill) {
     w.pin();

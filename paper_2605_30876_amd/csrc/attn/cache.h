@@ -94,8 +94,10 @@ struct AttnItem {
   int first, rows;            // first row of the tile, rows of the sequence
   int kt0, kt1;               // key tiles of 32 tokens
   int part;                   // partial result, or -1: the only item of its rows
-  // pages of the first four key tiles and of two from item_middle on (-1:
-  // none), known before the table could be
+  // Pages of the first four key tiles and of two from item_middle on (-1:
+  // none) as the table stood for the plan: loads start from them while the
+  // table is read, and are made again where it says otherwise (pages move, by
+  // a compaction, while a plan goes by lengths alone).
   int page[6];
   int pad;
 };

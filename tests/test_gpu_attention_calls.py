@@ -137,3 +137,29 @@ def test_a_new_cache_holds_zeros(gpu_lib):
     del blocks, c
     c = PagedCache(2, 8, 32, 2, 64, 1, 8)
     assert (c.k == 0).all() and (c.v == 0).all()
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_a_plan_outlives_a_compaction(gpu_lib, form):
+    """A plan goes by offsets, slots and lengths: pages that move after it was made are found where they are."""
+    s = _form(form, 24, slack=60)
+    n = s.cache.n_pages
+    held = s.cache.table[s.cache.table >= 0].long()
+    s.cache.refs[held] = 1
+    out, lse = s.run()
+    s.check(out, lse)
+    s.att.plan()
+    counts = torch.zeros(2, dtype=torch.int32, device="cuda")
+    s.cache.compact(counts=counts)
+    live, moved = counts.tolist()
+    assert live == held.numel() and moved > 4
+    s.cache.k[:, live:n] = float("nan")
+    s.cache.v[:, live:n] = float("nan")
+    again, lse2 = torch.full_like(out, 7.0, device="cuda"), torch.full_like(lse, 7.0, device="cuda")
+    s.att.attend(0, s.qd[0], again, lse2)
+    assert torch.equal(again.cpu(), out) and torch.equal(lse2.cpu(), lse)
+    # and pages taken away after the plan are not followed
+    s.cache.table.fill_(-1)
+    s.att.attend(0, s.qd[0], again, lse2)
+    rows = slice(0, s.off[-1])
+    assert (again[rows] == 0).all() and (lse2[rows] == -math.inf).all()
