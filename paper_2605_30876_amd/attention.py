@@ -239,15 +239,16 @@ class BlockAttention:
         self._plan = torch.zeros((ints,), dtype=torch.int32, device=cache.device)
         nbytes = lib.dmoe_attention_workspace_size(cache.c.dt, n_seqs, T, max_new, n_heads, cache.n_kv_heads, cache.head_dim)
         self.workspace = torch.empty((nbytes,), dtype=torch.uint8, device=cache.device)
-        self.batch = None
+        self.batch, self._planned = None, False
 
     def begin(self, q_offsets: torch.Tensor, slots: torch.Tensor | None = None):
         """The step's batch: sequence i is rows q_offsets[i] .. q_offsets[i+1] of its tensors and slot slots[i]
-        (default i) of the cache.  int32 device tensors, read by the calls that follow."""
+        (default i) of the cache.  int32 device tensors, read by the calls that follow; :meth:`attend` needs a
+        :meth:`plan` of it first."""
         _i32(q_offsets, "q_offsets", self.cache.device, self.n_seqs + 1)
         if slots is not None:
             _i32(slots, "slots", self.cache.device, self.n_seqs)
-        self._kept = (q_offsets, slots)
+        self._kept, self._planned = (q_offsets, slots), False
         self.batch = lib.dmoe_batch(lib.ptr(q_offsets), lib.ptr(slots), self.n_seqs, self.T, self.max_new)
 
     def _started(self):
@@ -260,6 +261,7 @@ class BlockAttention:
         until offsets, slots or lengths change (pages may move)."""
         with _On(self.cache.device):
             lib.dmoe_attention_plan(self.cache.c, self._started(), self.n_heads, self.mask_block, self._plan, stream)
+        self._planned = True
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor | None = None,
                q_out: torch.Tensor | None = None, stream=None):
@@ -291,6 +293,8 @@ class BlockAttention:
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < self.T * self.n_heads
                                 or lse.device != c.device):
             raise ValueError(f"lse must be contiguous float32 [{self.T}, {self.n_heads}] on {c.device}")
+        if not self._planned:
+            raise RuntimeError("plan() has not been called since begin()")
         with _On(c.device):
             lib.dmoe_attention(c.c, layer, self._started(), self.n_heads, self.mask_block, q, self.scale, self._plan, out, lse,
                                self.workspace, stream)

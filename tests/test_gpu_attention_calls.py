@@ -163,3 +163,16 @@ def test_a_plan_outlives_a_compaction(gpu_lib, form):
     s.att.attend(0, s.qd[0], again, lse2)
     rows = slice(0, s.off[-1])
     assert (again[rows] == 0).all() and (lse2[rows] == -math.inf).all()
+
+
+def test_attend_needs_a_plan_of_its_batch(gpu_lib):
+    s = Setup(BF16, 4, 2, 64, 32, [60, 50], [6, 2], 0)
+    s.att.begin(s.offd, s.slotsd)
+    with pytest.raises(RuntimeError, match="plan"):
+        s.att.attend(0, s.qd[0])
+    want, _ = s.run()
+    s.att.begin(s.offd, s.slotsd)
+    with pytest.raises(RuntimeError, match="plan"):
+        s.att.attend(0, s.qd[0])
+    s.att.plan()
+    assert torch.equal(s.att.attend(0, s.qd[0])[:8].cpu(), want[:8])
