@@ -612,6 +612,8 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
  *   table  [n_slots][max_pages] page ids; those of tokens from lens on are -1
  *   lens   [n_slots] tokens of the sequence (its new ones included)
  *   refs   [n_pages] sequences that hold the page; 0: free
+ *   refused [n_slots] *status of the sequence's last dmoe_cache_update if that was
+ *          not 0, else 0
  * A page holds, per kv head and tile of 32 tokens, 16-byte chunks of c values
  * (c = 8 for DMOE_BF16, 4 for DMOE_F32) in the order in which the attention's
  * matrix instructions read them; dp is head_dim rounded up to 32, 64, 96, 128,
@@ -635,6 +637,7 @@ typedef struct dmoe_cache {
   int32_t* refs; /* used by dmoe_cache_update and dmoe_cache_compact only, else may be NULL */
   dmoe_dtype dt;
   int n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages;
+  int32_t* refused; /* may be NULL: then no refusal is remembered */
 } dmoe_cache;
 
 /* Bytes of one page of keys (or of values) of one layer; 0 on invalid sizes. */
@@ -651,8 +654,10 @@ size_t dmoe_cache_page_bytes(dmoe_dtype dt, int page_tokens, int n_kv_heads, int
  * q_offsets [n_seqs + 1] non-decreasing from 0, q_offsets[n_seqs] <= T;
  * slots [n_seqs] in [0, n_slots), or NULL: sequence i is slot i.  Offsets and
  * slots out of range are cut to the range (rows outside [0, T) are never
- * touched, a sequence of a slot outside the table has no tokens).  max_new: an
- * upper bound of every sequence's new tokens (more are ignored).
+ * touched, a sequence of a slot outside the table has no tokens).  Neither has
+ * one whose slot is marked in the cache's refused: it was not given the room
+ * it asked for, and its last tokens are others than these, perhaps shared.
+ * max_new: an upper bound of every sequence's new tokens (more are ignored).
  * Limits: 1 <= n_seqs <= 4096, n_slots if slots is NULL; 1 <= T <= 2^26; max_new >= 1.
  */
 typedef struct dmoe_batch {
@@ -734,7 +739,8 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
  * last fork, or truncation, on: tokens before that are shared and must not be stored again.
  * *status (device int32, may be NULL): 0, done; n > 0, n pages are lacking; -1,
  * a slot out of range, a dst twice, a length or keep out of range, or a table
- * entry out of range.  Unless 0, nothing was changed.
+ * entry out of range.  Unless 0, nothing was changed but the cache's refused,
+ * where every dst in range gets it; a call that is done sets its dsts' to 0.
  * dst, src, keep, new_lens: int32 [n] device arrays.  workspace:
  * dmoe_cache_update_workspace_size bytes, not shared with a concurrent call.
  * Limits: 1 <= n <= 4096; n * max_pages < 2^31.

@@ -104,7 +104,12 @@ class PagedCache:
     ``page_tokens`` tokens, held by ``n_slots`` sequences of up to
     ``max_pages`` pages.  k, v, table, lens, refs: existing arrays to use
     (layouts: dmoe_cache in include/dmoe.h) instead of new, empty ones (keys
-    and values 0); the others are then made on their device."""
+    and values 0); the others are then made on their device.
+
+    ``status`` holds the outcome of the last update that was given no tensor
+    of its own for it; ``refused`` [n_slots] of every slot's last update, 0 if it was done.  A
+    slot that is marked there has no new tokens: :meth:`BlockAttention.append`
+    and ``attend`` leave its rows alone until an update of it succeeds (one to its present length does)."""
 
     def __init__(self, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, n_slots: int,
                  max_pages: int, dtype: torch.dtype = torch.bfloat16, device="cuda", k=None, v=None, table=None, lens=None,
@@ -143,8 +148,10 @@ class PagedCache:
         self.refs = ints(refs, "refs", (n_pages,), 0)
         self.device = self.k.device
         self.status = torch.zeros((1,), dtype=torch.int32, device=device)
+        self.refused = torch.zeros((n_slots,), dtype=torch.int32, device=device)
         self.c = lib.dmoe_cache(lib.ptr(self.k), lib.ptr(self.v), lib.ptr(self.table), lib.ptr(self.lens), lib.ptr(self.refs),
-                                dt, n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages)
+                                dt, n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages,
+                                lib.ptr(self.refused))
         # for calls on every slot, where that is not much; larger calls add one of their own
         nbytes = max(lib.dmoe_cache_update_workspace_size(min(n_slots, 4096), max_pages, n_pages),
                      lib.dmoe_cache_compact_workspace_size(n_pages))
@@ -164,7 +171,8 @@ class PagedCache:
                keep: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
         """Entry i: slot dst[i] holds the first keep[i] tokens of slot src[i] (default: its own) and room for
         new_lens[i] (dmoe_cache_update).  int32 device tensors.  The outcome is left in ``status`` (default
-        ``self.status``): 0 done, n > 0 pages lacking, -1 refused; unless 0 nothing was changed."""
+        ``self.status``): 0 done, n > 0 pages lacking, -1 refused; unless 0 nothing was changed but ``self.refused``
+        of the slots."""
         n = dst.numel()
         if n == 0:
             return
@@ -178,19 +186,20 @@ class PagedCache:
             ws = self._workspace(lib.dmoe_cache_update_workspace_size(n, self.max_pages, self.n_pages), stream)
             lib.dmoe_cache_update(self.c, dst, src, keep, new_lens, n, status, ws, stream)
 
-    def resize(self, slots: torch.Tensor, new_lens: torch.Tensor, stream=None):
+    def resize(self, slots: torch.Tensor, new_lens: torch.Tensor, stream=None, status: torch.Tensor | None = None):
         """Grows or truncates sequences to new_lens tokens."""
-        self.update(slots, new_lens, stream=stream)
+        self.update(slots, new_lens, status=status, stream=stream)
 
-    def free(self, slots: torch.Tensor, stream=None):
+    def free(self, slots: torch.Tensor, stream=None, status: torch.Tensor | None = None):
         """Releases every page of the sequences."""
         with _stream(stream):
-            self.update(slots, torch.zeros_like(slots), stream=stream)
+            self.update(slots, torch.zeros_like(slots), status=status, stream=stream)
 
-    def fork(self, dst: torch.Tensor, src: torch.Tensor, keep: torch.Tensor, new_lens: torch.Tensor | None = None, stream=None):
+    def fork(self, dst: torch.Tensor, src: torch.Tensor, keep: torch.Tensor, new_lens: torch.Tensor | None = None, stream=None,
+             status: torch.Tensor | None = None):
         """Slot dst[i] becomes the first keep[i] tokens of slot src[i], sharing its full pages; with room for
         new_lens[i] tokens (default keep[i])."""
-        self.update(dst, keep if new_lens is None else new_lens, src, keep, stream=stream)
+        self.update(dst, keep if new_lens is None else new_lens, src, keep, status, stream)
 
     def compact(self, table_out: torch.Tensor | None = None, refs_out: torch.Tensor | None = None,
                 counts: torch.Tensor | None = None, stream=None):

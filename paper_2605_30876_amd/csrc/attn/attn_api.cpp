@@ -57,8 +57,8 @@ dmoe_status check_cache(const char* fn, const dmoe_cache* c, bool refs) {
   REQUIRE(static_cast<long>(c->max_pages) * c->page_tokens <= kMaxTokens, "max_pages*page_tokens must be at most %ld", kMaxTokens);
   SUPPORT(c->n_slots <= kMaxSlots, "n_slots=%d must be at most %d", c->n_slots, kMaxSlots);
   REQUIRE(!misaligned(c->k) && !misaligned(c->v), "the cache's k and v must be 16-byte aligned");
-  REQUIRE(!misaligned_to(c->table, 4) && !misaligned_to(c->lens, 4) && !misaligned_to(c->refs, 4),
-          "the cache's table, lens and refs must be 4-byte aligned");
+  REQUIRE(!misaligned_to(c->table, 4) && !misaligned_to(c->lens, 4) && !misaligned_to(c->refs, 4) && !misaligned_to(c->refused, 4),
+          "the cache's table, lens, refs and refused must be 4-byte aligned");
   return DMOE_OK;
 }
 

@@ -47,8 +47,11 @@ __device__ __forceinline__ Seq load_seq(const dmoe_cache& c, const dmoe_batch& b
   s.slot = b.slots ? b.slots[i] : i;
   const bool known = s.slot >= 0 && s.slot < c.n_slots;
   s.slot = known ? s.slot : 0;
-  s.len = known ? min(max(c.lens[s.slot], 0), c.max_pages * c.page_tokens) : 0;
-  if (!known) s.n = 0;
+  // both loads on their way together
+  const int32_t* marks = c.refused ? c.refused : c.lens;
+  const int mark = marks[s.slot], len = c.lens[s.slot];
+  s.len = known ? min(max(len, 0), c.max_pages * c.page_tokens) : 0;
+  if (!known || (c.refused && mark != 0)) s.n = 0;
   s.pos0 = s.len - s.n;
   return s;
 }

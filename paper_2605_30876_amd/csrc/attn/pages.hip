@@ -79,6 +79,11 @@ __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const in
     for (int p = tid; p < c.n_pages; p += kThreads) lds_counts[p] = c.refs[p];
   }
   auto pages = [&](int tokens) { return (tokens + pt - 1) / pt; };
+  auto leave = [&](int outcome) {
+    for (int i = tid; i < n && c.refused; i += kThreads)
+      if (const int d = dst[i]; d >= 0 && d < c.n_slots) c.refused[d] = outcome;
+    if (tid == 0 && status) *status = outcome;
+  };
   for (int i = tid; i < (c.n_slots + 31) / 32; i += kThreads) seen[i] = 0;
   if (tid == 0) {
     bad = 0;
@@ -110,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const in
   if (!ok) atomicOr(&bad, 1);
   __syncthreads();
   if (bad) {
-    if (tid == 0 && status) *status = -1;
+    leave(-1);
     return;
   }
   // the pages kept, as the tables stand
@@ -131,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const in
   if (!ok) atomicOr(&bad, 1);
   __syncthreads();
   if (bad) {
-    if (tid == 0 && status) *status = -1;
+    leave(-1);
     return;
   }
   auto count_shared = [&](int sign) {
@@ -203,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const in
       for (int i = tid; i < n; i += kThreads)
         if (entries[i].part >= 0) counts.add(entries[i].part, -1);
     }
-    if (tid == 0 && status) *status = need - total;
+    leave(need - total);
     return;
   }
   for (int p = q0; p < q1 && at < need; ++p)
@@ -226,10 +231,8 @@ __global__ __launch_bounds__(kThreads) void update_kernel(dmoe_cache c, const in
     c.table[static_cast<long>(e.dst) * mp + j] = p;
   }
   for (int i = tid; i < n; i += kThreads) c.lens[entries[i].dst] = entries[i].len;
-  if (tid == 0) {
-    *n_pairs = copies;
-    if (status) *status = 0;
-  }
+  if (tid == 0) *n_pairs = copies;
+  leave(0);
   if constexpr (kLds) {
     __syncthreads();
     for (int p = tid; p < c.n_pages; p += kThreads) c.refs[p] = lds_counts[p];

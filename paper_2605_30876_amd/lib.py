@@ -84,7 +84,7 @@ class dmoe_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
                 ("refs", ctypes.c_void_p), ("dt", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_pages", ctypes.c_int),
                 ("page_tokens", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
-                ("n_slots", ctypes.c_int), ("max_pages", ctypes.c_int)]
+                ("n_slots", ctypes.c_int), ("max_pages", ctypes.c_int), ("refused", ctypes.c_void_p)]
 
 
 class dmoe_batch(ctypes.Structure):

@@ -25,3 +25,8 @@ def test_arrays_of_two_devices_are_refused(name):
              "lens": torch.zeros(1, dtype=torch.int32, device="meta"), "refs": torch.zeros(2, dtype=torch.int32, device="meta")}[name]
     with pytest.raises(ValueError):
         PagedCache(1, 2, 32, 1, 64, 1, 1, device="meta", k=_pool(), **{name: array})
+
+
+def test_a_cache_remembers_refusals():
+    c = PagedCache(1, 2, 32, 1, 64, 3, 1, device="cpu")
+    assert c.refused.tolist() == [0, 0, 0] and c.c.refused == c.refused.data_ptr()

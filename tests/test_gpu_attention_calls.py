@@ -176,3 +176,58 @@ def test_attend_needs_a_plan_of_its_batch(gpu_lib):
         s.att.attend(0, s.qd[0])
     s.att.plan()
     assert torch.equal(s.att.attend(0, s.qd[0])[:8].cpu(), want[:8])
+
+
+def _stored(cache):
+    return cache.k.clone(), cache.v.clone()
+
+
+@pytest.mark.parametrize("pages", [6, 9000])
+def test_a_refused_update_leaves_its_slots_alone(gpu_lib, pages):
+    """A sequence that was not given the room it asked for: a later call on another slot does not hide it, and nothing
+    is stored over what it shares with others."""
+    cache = PagedCache(1, pages, 32, 1, 32, 4, 8)
+    cache.k.zero_(), cache.v.zero_()
+    if pages > 6:
+        cache.refs[6:] = 1  # taken by others
+    cache.resize(i32([0]), i32([96]))
+    cache.fork(i32([1]), i32([0]), i32([96]))  # all three pages shared
+    cache.resize(i32([3]), i32([33]))
+    seen = torch.zeros(3, dtype=torch.int32, device="cuda")
+    cache.resize(i32([1, 2]), i32([104, 100]), status=seen[0:1])  # five pages, of which there is one
+    cache.resize(i32([3]), i32([40]), status=seen[1:2])
+    assert seen.tolist() == [4, 0, 0] and cache.refused.tolist() == [0, 4, 4, 0]
+    att = BlockAttention(cache, 2, 2, 8, 16, mask_block=8)
+    att.begin(i32([0, 8, 16]), i32([1, 3]))
+    kv, q = torch.ones(16, 1, 32, device="cuda").to(BF16), torch.ones(16, 2, 32, device="cuda").to(BF16)
+    before = _stored(cache)
+    att.append(0, kv, kv, q)
+    ka, va = R.places(BF16, 32, 1, 32, torch.arange(32, 40), cache.table[3, 1].cpu().expand(8))
+    for was, now, at in zip(before, _stored(cache), (ka, va)):
+        was.view(-1)[at.cuda()] = 1.0  # the other sequence's
+        assert torch.equal(was, now)
+    out = torch.full_like(q, 7.0)
+    att.plan()
+    att.attend(0, q, out)
+    assert (out[:8] == 7.0).all() and (out[8:] != 7.0).all()
+    # the same request with room for it
+    cache.resize(i32([1]), i32([104]), status=seen[2:3])
+    assert seen.tolist() == [4, 0, 0] and cache.refused.tolist() == [0, 0, 4, 0]
+    before = _stored(cache)
+    att.append(0, kv, kv, q)
+    ka, va = R.places(BF16, 32, 1, 32, torch.arange(96, 104), cache.table[1, 3].cpu().expand(8))
+    for was, now, at in zip(before, _stored(cache), (ka, va)):
+        was.view(-1)[at.cuda()] = 1.0
+        assert torch.equal(was, now)
+
+
+def test_a_wrong_update_marks_the_slots_it_names(gpu_lib):
+    cache = PagedCache(1, 6, 32, 1, 32, 4, 8)
+    cache.resize(i32([0, 1]), i32([40, 40]))
+    cache.resize(i32([0, 9, -3, 2]), i32([50, 1, 1, 8]))
+    assert cache.refused.tolist() == [-1, 0, -1, 0] and cache.lens.tolist() == [40, 40, 0, 0]
+    cache.resize(i32([0, 2]), i32([50, 8]))
+    assert cache.refused.tolist() == [0, 0, 0, 0] and cache.lens.tolist() == [50, 40, 8, 0]
+    cache.table[1, 1] = 99
+    cache.free(i32([1]))
+    assert cache.refused.tolist() == [0, -1, 0, 0]
