@@ -244,7 +244,7 @@ class MoELayer:
 
 
 def decode_step(layers: list, weights: list, xs: list, routing: str = "block", stream=None,
-                attention: list | None = None) -> torch.Tensor:
+                attention: list | None = None, residual: str = "step") -> torch.Tensor:
     """The MoE layers of one decode step, chained: layer l runs on xs[l], and
     the step's input plus layer l's output, rounded once to the storage
     type, is layer l+1's input xs[l+1].  Each layer thus waits for its
@@ -263,7 +263,15 @@ def decode_step(layers: list, weights: list, xs: list, routing: str = "block", s
     ``attention``: one :class:`.attention.AttentionLayer` per layer.  Layer l
     then runs on xs[l] plus its attention over the cache (whose keys and
     values it stores first); their batch must have been begun, and
-    the step plans it once, before its first layer."""
+    the step plans it once, before its first layer.  What attention adds
+    to xs[l] reaches the layers behind through this layer's y alone.
+
+    ``residual``: "step", as above, or "stream": layer l+1's input is layer
+    l's own, its attention included, plus y, as in a transformer's layer
+    (whose norms, which keep the stream's scale, are not here; the last
+    layer's sum is left to the caller: attention[-1].out + y)."""
+    if residual not in ("step", "stream"):
+        raise ValueError(f"residual must be 'step' or 'stream', not {residual!r}")
     if attention is not None:
         if len(attention) != len(layers):
             raise ValueError(f"{len(attention)} attention layers for {len(layers)} layers")
@@ -274,5 +282,6 @@ def decode_step(layers: list, weights: list, xs: list, routing: str = "block", s
     L = len(layers)
     for l, (m, w) in enumerate(zip(layers, weights)):
         x = xs[l] if attention is None else attention[l](xs[l], stream)
-        y = m.forward(x, w, routing, stream, residual=(xs[0], xs[l + 1]) if l + 1 < L else None)
+        base = xs[0] if residual == "step" else x
+        y = m.forward(x, w, routing, stream, residual=(base, xs[l + 1]) if l + 1 < L else None)
     return y

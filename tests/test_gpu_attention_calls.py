@@ -9,7 +9,9 @@ import torch
 import attention_ref as R
 from paper_2605_30876_amd import lib
 from paper_2605_30876_amd.attention import AttentionLayer, BlockAttention, PagedCache, Rope
+from paper_2605_30876_amd.layer import decode_step
 from test_gpu_attention import FORMS, Setup, _form, _poison
+from test_gpu_decode_attention import L, Model
 
 pytestmark = pytest.mark.gpu
 
@@ -231,3 +233,19 @@ def test_a_wrong_update_marks_the_slots_it_names(gpu_lib):
     cache.table[1, 1] = 99
     cache.free(i32([1]))
     assert cache.refused.tolist() == [0, -1, 0, 0]
+
+
+@pytest.mark.parametrize("attended", [False, True])
+@pytest.mark.parametrize("residual", ["step", "stream"])
+@pytest.mark.parametrize("name", ["small_bf16", "small_f32"])
+def test_the_residual_of_a_step(gpu_lib, name, residual, attended):
+    """Layer l+1's input: the step's input plus y, or the layer's own input (with its attention) plus y, rounded once."""
+    m = Model(name, "block")
+    m.cache.resize(m.slots, m.i32([m.bs] * m.n))
+    y = decode_step(m.m, m.w, m.xs, "block", attention=m.al if attended else None, residual=residual)
+    assert torch.equal(y, m.m[-1].y) and torch.isfinite(y).all()
+    for l in range(L - 1):
+        base = m.xs[0] if residual == "step" else m.al[l].out if attended else m.xs[l]
+        assert torch.equal(m.xs[l + 1], (base.float() + m.m[l].y.float()).to(base.dtype)), f"layer {l}"
+    with pytest.raises(ValueError):
+        decode_step(m.m, m.w, m.xs, "block", residual="layer")
