@@ -57,12 +57,20 @@ class _On:
             torch.cuda.set_device(self.back)
 
 
+def _no_gradient(t: torch.Tensor, name: str):
+    """These calls record nothing: a tensor whose gradient is asked for would lose it without a word."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError(f"{name} requires a gradient, which these calls do not record: call under torch.no_grad() or detach it "
+                           f"(a rotation's gradient is its inverse)")
+
+
 def _heads(t: torch.Tensor, name: str, rows: int | None, heads: int, dim: int, like: torch.dtype, device) -> torch.Tensor:
     """Checks a step's tensor [rows, heads, dim]: heads and their elements dense, rows any stride."""
     if t.dim() != 3 or tuple(t.shape[1:]) != (heads, dim) or (rows is not None and t.shape[0] < rows):
         raise ValueError(f"{name} must be [{'T' if rows is None else rows}, {heads}, {dim}], not {list(t.shape)}")
     if t.dtype != like or t.device != device:
         raise ValueError(f"{name} must be {like} on {device}, not {t.dtype} on {t.device}")
+    _no_gradient(t, name)
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
         raise ValueError(f"{name}: heads and their elements must be dense (strides {t.stride()})")
     return t
@@ -337,6 +345,8 @@ class AttentionLayer:
         a, c, w = self.att, self.att.cache, self.w
         if tuple(x.shape) != (a.T, self.H) or x.dtype != c.dtype or x.device != c.device:
             raise ValueError(f"x must be {c.dtype} [{a.T}, {self.H}] on {c.device}, not {x.dtype} {list(x.shape)} on {x.device}")
+        for name, t in (("x", x), *w.items()):
+            _no_gradient(t, name)
         with torch.no_grad(), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(c.device)):
             torch.mm(x, w["wq"].t(), out=self.q)
             torch.mm(x, w["wk"].t(), out=self.k)
