@@ -133,7 +133,8 @@ dmoe_status dmoe_rope_turns(int rot_dim, double base, dmoe_rope_scaling scaling,
     double f = std::pow(base, -2.0 * i / rot_dim) / kTwoPi;
     if (scaling == DMOE_ROPE_LINEAR) f /= factor;
     if (scaling == DMOE_ROPE_YARN) {
-      const double ramp = std::fmin(std::fmax((i - lo) / (hi != lo ? hi - lo : 0.001), 0.0), 1.0);
+      // ends that were cut to the pairs and met or crossed: every pair is slow, or every pair is fast
+      const double ramp = hi > lo ? std::fmin(std::fmax((i - lo) / (hi - lo), 0.0), 1.0) : hi <= 0.0 ? 1.0 : 0.0;
       f = f / factor * ramp + f * (1.0 - ramp);
     }
     turns[i] = f;

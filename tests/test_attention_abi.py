@@ -223,3 +223,15 @@ def test_the_reference_attention_by_hand():
     assert torch.allclose(out[1, 0], torch.tensor([1.0, 6.0], dtype=torch.float64)) and abs(float(lse[1, 0]) - math.log(4.0)) < 1e-6
     assert (out[0] == 0).all() and float(lse[0, 0]) == -math.inf
     assert R.ends([0, 31, 32, 40], 41, 32).tolist() == [32, 32, 41, 41] and R.ends([3], 5, 0).tolist() == [5]
+
+
+@pytest.mark.parametrize("rot", [2, 8, 64])
+@pytest.mark.parametrize("base,original,slow", [(10000.0, 4.0, True), (1.5, 6.0, True), (10000.0, 6.2, True), (2.0, 4096.0, False), (1.1, 300.0, False),
+                                                (10000.0, 1e30, False)])
+def test_yarn_ramps_beyond_the_pairs(rot, base, original, slow):
+    """All pairs slow (under one turn in `original` positions): all interpolated; all fast (over 32): all kept."""
+    plain, _ = lib.dmoe_rope_turns(rot, base, "none", 1.0, 0)
+    assert all(f * original < 1 if slow else f * original > 32 for f in plain)
+    got, _ = lib.dmoe_rope_turns(rot, base, "yarn", 8.0, original)
+    want = [f / 8 for f in plain] if slow else plain
+    assert all(abs(a - b) <= 1e-15 * b for a, b in zip(got, want))
