@@ -64,13 +64,14 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
       if (i < kKeptSeqs) seqs[i] = q;
       n = static_cast<int>((static_cast<long>(q.n) * sh.group + sh.tile_rows - 1) / sh.tile_rows);
     }
+    // Offsets that are not sorted could make more row tiles than the arrays
+    // hold, or an int: cut after each pass, whose own stay below 2^31 (rises
+    // of at most 2^30 rows, 128 to a tile, between at most 128 falls).
     int total;
-    const int at = scan_exclusive<kThreads>(n, iwaves, &total);
-    if (i < b.n_seqs) tiles[i] = n_tiles + at;
-    n_tiles += total;
+    const int at = scan_exclusive<kThreads>(n, iwaves, &total), most_tiles = static_cast<int>(sh.max_tiles);
+    if (i < b.n_seqs) tiles[i] = min(n_tiles + at, most_tiles);
+    n_tiles = min(n_tiles + total, most_tiles);
   }
-  // offsets that break their contract could make more row tiles than the arrays hold
-  n_tiles = min(n_tiles, static_cast<int>(sh.max_tiles));
   if (tid == 0) tiles[b.n_seqs] = n_tiles;
   __syncthreads();
   // longest rows first under a causal mask: the last tiles see the most keys

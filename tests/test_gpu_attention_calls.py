@@ -249,3 +249,21 @@ def test_the_residual_of_a_step(gpu_lib, name, residual, attended):
         assert torch.equal(m.xs[l + 1], (base.float() + m.m[l].y.float()).to(base.dtype)), f"layer {l}"
     with pytest.raises(ValueError):
         decode_step(m.m, m.w, m.xs, "block", residual="layer")
+
+
+def test_unsorted_offsets_stay_within_the_plan(gpu_lib):
+    """Every second sequence claims all rows: 2^31 row tiles, of which the plan has places for 2^20 and a few."""
+    T, n, heads = 1 << 17, 4096, 1024
+    cache = PagedCache(1, 4, 32, 1, 8, 4, 2)
+    cache.lens.fill_(40)
+    cache.table[:, 0], cache.table[:, 1] = 1, 2
+    att = BlockAttention(cache, heads, n, T, T, mask_block=1)
+    att.begin(i32([0, T] * (n // 2) + [0]), i32([i % 4 for i in range(n)]))
+    att.plan()
+    n_items, n_merges = att._plan[:2].tolist()
+    assert T * heads // 128 <= n_items <= T * heads // 128 + n and n_merges == 0
+    assert 4 + 16 * n_items <= att._plan.numel()
+    slot, row0, rows, length, first, all_rows, kt0, kt1 = att._plan[4:4 + 16 * n_items].view(-1, 16)[:, :8].unbind(1)
+    assert ((slot >= 0) & (slot < 4) & (row0 == 0) & (rows == T) & (length == 40)).all()
+    assert ((all_rows == T * heads) & (first >= 0) & (first < all_rows) & (first % 128 == 0)).all()
+    assert ((kt0 >= 0) & (kt0 <= kt1) & (kt1 <= 2)).all()
