@@ -267,3 +267,138 @@ def test_unsorted_offsets_stay_within_the_plan(gpu_lib):
     assert ((slot >= 0) & (slot < 4) & (row0 == 0) & (rows == T) & (length == 40)).all()
     assert ((all_rows == T * heads) & (first >= 0) & (first < all_rows) & (first % 128 == 0)).all()
     assert ((kt0 >= 0) & (kt0 <= kt1) & (kt1 <= 2)).all()
+
+
+@pytest.mark.parametrize("page", [96, 160])
+@pytest.mark.parametrize("form", ["two_halves", "two_halves_f32", "one_128", "one_256", "one_f32", "sixty_four", "sixty_four_f32", "thirty_two",
+                                  "thirty_two_f32_256"])
+def test_pages_whose_tiles_are_no_power_of_two(gpu_lib, form, page):
+    dtype, heads, kv, dim, _, n, capacity = FORMS[form]
+    new = [40, 33, 0, 21, 1, 40, 9, 2, 0][:n]
+    if form.startswith("thirty_two"):
+        new = [min(x, 32 * kv // heads) for x in new]
+    s = Setup(dtype, heads, kv, dim, page, [333, 64, 0, 900, 33, 159, 5, 0, 97][:n], new, 24, seed=page, capacity=capacity)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim", [(BF16, 96, 2, 64), (BF16, 1024, 1, 8), (F32, 17, 1, 32), (BF16, 57, 3, 40)])
+def test_many_heads_of_a_group(gpu_lib, dtype, heads, kv, dim):
+    s = Setup(dtype, heads, kv, dim, 32, [70, 1, 0, 33], [2, 1, 0, 2], 1, seed=heads)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("heads,kv,new", [(2, 2, 1), (16, 2, 5), (8, 1, 9)])
+def test_plans_of_several_passes(gpu_lib, heads, kv, new):
+    """600 sequences: more row tiles than the plan has threads, and more sequences than it keeps."""
+    lens = [(5 * i * i) % 97 for i in range(600)]
+    s = Setup(BF16, heads, kv, 32, 32, lens, [min(x, i % (new + 1)) for i, x in enumerate(lens)], 1, seed=3)
+    s.check(*s.run())
+
+
+def _append_case(dtype, heads, kv, dim, page, lens, new, rot, inter, seed):
+    """Stores a batch and compares with the definition; every element of the pool and of q_out."""
+    g = torch.Generator().manual_seed(seed)
+    n, dp = len(lens), R.padded(dim)
+    width = max(-(-m // page) for m in lens) + 1
+    pages = sum(-(-m // page) for m in lens) + 2
+    ids, at = torch.randperm(pages, generator=g).int(), 0
+    table = torch.full((n, width), -1, dtype=torch.int32)
+    for i, m in enumerate(lens):
+        h = -(-m // page)
+        table[i, :h] = ids[at:at + h]
+        at += h
+    cache = PagedCache(1, pages, page, kv, dim, n, width, dtype=dtype, table=table.cuda(), lens=i32(lens))
+    cache.k.fill_(77.0), cache.v.fill_(77.0)
+    off = [0]
+    for x in new:
+        off.append(off[-1] + x)
+    T = off[-1] + 3
+    q, k, v = (torch.randn(T, h, dim, generator=g).to(dtype) for h in (heads, kv, kv))
+    att = BlockAttention(cache, heads, n, max(new), T, rope=Rope(rot, interleaved=inter))
+    att.begin(i32(off))
+    q_out = torch.full((T, heads, dim), 7.0, dtype=dtype, device="cuda")
+    att.append(0, k.cuda(), v.cuda(), q.cuda(), q_out)
+    want_k = torch.full((pages * page * kv * dp,), 77.0, dtype=torch.float64)
+    want_v, want_q = want_k.clone(), torch.full((T, heads, dim), 7.0, dtype=torch.float64)
+    f, pad = R.turns(rot)[0], (0, dp - dim)
+    rows = torch.cat([torch.arange(b - min(m, x), b) for m, x, b in zip(lens, new, off[1:])])
+    pos = torch.cat([torch.arange(m - min(m, x), m) for m, x in zip(lens, new)])
+    seq = torch.cat([torch.full((min(m, x),), i) for i, (m, x) in enumerate(zip(lens, new))])
+    ka, va = R.places(dtype, page, kv, dp, pos, table[seq, pos // page])
+    want_q[rows] = R.rotate(q[rows], pos, f, 1.0, inter)
+    want_k[ka] = torch.nn.functional.pad(R.rotate(k[rows], pos, f, 1.0, inter), pad)
+    want_v[va] = torch.nn.functional.pad(v[rows].double(), pad)
+    # cos and sin 2^-22, two products and a sum 2^-23, the rounding to the type, of at most twice the largest value
+    tol = (2.0 ** -22 + 2.0 ** -23 + R.EPS[dtype]) * 2
+    assert torch.equal(cache.v.cpu().view(-1).double(), want_v)
+    assert bool(((cache.k.cpu().view(-1).double() - want_k).abs() <= tol * float(k.abs().max())).all())
+    assert torch.equal(cache.k.cpu().view(-1) == 77.0, want_k == 77.0)
+    assert bool(((q_out.cpu().double() - want_q).abs() <= tol * float(q.abs().max())).all())
+    assert torch.equal(q_out[off[-1]:].cpu(), torch.full((3, heads, dim), 7.0, dtype=dtype))
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim,rot,inter", [(BF16, 2, 1, 64, 64, False), (F32, 3, 3, 40, 22, False), (BF16, 7, 1, 32, 16, True),
+                                                          (BF16, 29, 1, 256, 128, False)])
+def test_append_counts_its_tiles(gpu_lib, dtype, heads, kv, dim, rot, inter):
+    """One long sequence among many short ones: the tiles there are, found by counting, 64 sequences at a time."""
+    lens = [(11 * i) % 70 for i in range(131)]
+    new = [min(x, i % 4) for i, x in enumerate(lens)]
+    lens[97], new[97] = 700, 650
+    lens[3], new[3] = 2, 5  # more new tokens than the sequence has
+    _append_case(dtype, heads, kv, dim, 32, lens, new, rot, inter, 17)
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim,rot,inter", [(BF16, 20, 2, 128, 128, False), (BF16, 26, 1, 8, 8, True), (F32, 11, 11, 64, 64, True),
+                                                          (BF16, 10, 5, 80, 36, False), (F32, 37, 1, 24, 24, False)])
+def test_append_of_many_tokens(gpu_lib, dtype, heads, kv, dim, rot, inter):
+    """Enough tokens for several heads to a workgroup, the last group not full."""
+    lens = [2500, 40, 1900, 0, 999]
+    _append_case(dtype, heads, kv, dim, 64, lens, [2500, 33, 1700, 0, 1], rot, inter, 23)
+
+
+@pytest.mark.parametrize("dtype,T,heads,dim,rot,inter", [(BF16, 4100, 13, 64, 64, False), (BF16, 5003, 7, 128, 64, True), (F32, 4100, 13, 32, 22, False),
+                                                         (BF16, 9000, 5, 8, 8, False), (F32, 4097, 11, 64, 64, False)])
+def test_rotation_of_many_rows(gpu_lib, dtype, T, heads, dim, rot, inter):
+    """Enough rows for several heads to a workgroup, the last group not full."""
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn(T, heads, dim, generator=g).to(dtype)
+    pos = torch.randint(0, 100_000, (T,), generator=g, dtype=torch.int32)
+    out = torch.full((T + 1, heads, dim), 7.0, dtype=dtype, device="cuda")
+    Rope(rot, interleaved=inter).apply(x.cuda(), pos.cuda(), out=out[:T])
+    want = R.rotate(x, pos, R.turns(rot)[0], 1.0, inter)
+    tol = (2.0 ** -22 + 2.0 ** -23 + R.EPS[dtype]) * 2 * float(x.abs().max())
+    assert bool(((out[:T].cpu().double() - want).abs() <= tol).all()) and (out[T:] == 7.0).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), torch.finfo(BF16).min])
+@pytest.mark.parametrize("dtype,new", [(BF16, 8), (BF16, 40), (F32, 8)])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_values_of_masked_places_reach_the_rows_that_see_them(gpu_lib, dtype, new, value, which):
+    """The counterpart of masked places that do not matter: the rows behind the first such token differ."""
+    s = Setup(dtype, 4, 2, 64, 32, [150], [new], 1, seed=3)
+    before, lse0 = s.run()
+    first = 150 - new + new // 2
+    _poison(s, 0, list(range(first, 150)), value, which)
+    out, lse = s.run()
+    rows = slice(new // 2, new)
+    if which == "v":
+        assert torch.equal(lse[rows], lse0[rows]) and (out[rows] != before[rows]).all()
+    else:  # the keys' scores are not numbers, or beyond all others, or below them
+        assert (lse[rows] != lse0[rows]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_single_tokens_of_an_attention_layer(gpu_lib, dtype):
+    """Autoregressive steps of three sequences: every step's new row against the definition on the cache's contents."""
+    h = Half(dtype, n=3, new=1)
+    for step in range(3):
+        h.cache.resize(h.slots, i32([41 + 3 * i + 15 * step for i in range(3)]))
+        h.cache.k.nan_to_num_(0.0), h.cache.v.nan_to_num_(0.0)  # tokens that no step stored
+        h.step()
+        c, o, q = h.cache, h.layer.o.cpu().view(3, 4, 32), h.layer.q.cpu().view(3, 4, 32)
+        for i, m in enumerate(c.lens.tolist()):
+            pos = torch.arange(m)
+            ka, va = R.places(dtype, 32, 2, 32, pos, c.table[i].cpu()[pos // 32])
+            ref = R.attention(q[i:i + 1], c.k.cpu().view(-1)[ka], c.v.cpu().view(-1)[va], torch.tensor([m]), 1 / math.sqrt(32))
+            tol, _ = R.bounds(dtype, 32, m, *ref)
+            assert bool(((o[i:i + 1].double() - ref[0]).abs() <= tol).all())
