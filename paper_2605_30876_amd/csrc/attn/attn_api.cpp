@@ -96,9 +96,14 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const char* pb = static_cast<const char*>(b);
   return pa < pb + nb && pb < pa + na;
 }
-// Bytes from a tensor's first to behind its last element.
-size_t span(long rows, long stride, long width, dmoe_dtype dt) {
-  return static_cast<size_t>((rows - 1) * stride + width) * dmoe::dtype_bytes(dt);
+// Whether two step's tensors share an element.  With one stride they may be
+// columns of one wider tensor; with two, their spans tell.
+bool rows_overlap(const void* a, long a_stride, const void* b, long b_stride, long rows, long width, dmoe_dtype dt) {
+  const size_t e = dmoe::dtype_bytes(dt), w = width * e, pitch = a_stride * e;
+  if (!overlap(a, ((rows - 1) * a_stride + width) * e, b, ((rows - 1) * b_stride + width) * e)) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+  const size_t off = (pa < pb ? pb - pa : pa - pb) % pitch;
+  return a_stride != b_stride || off < w || pitch - off < w;
 }
 
 bool valid_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
@@ -157,7 +162,7 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
   ROWS(x, x_stride, width, dt);
   ROWS(out, out_stride, width, dt);
   ALIGNED_TO(positions, 4);
-  REQUIRE((x == out && x_stride == out_stride) || !overlap(x, span(T, x_stride, width, dt), out, span(T, out_stride, width, dt)),
+  REQUIRE((x == out && x_stride == out_stride) || !rows_overlap(x, x_stride, out, out_stride, T, width, dt),
           "out must be x with the same stride or not overlap it");
   return hip_status(dmoe::launch_rope(x, x_stride, out, out_stride, dt, T, n_heads, head_dim, positions, rope, inverse != 0,
                                       static_cast<hipStream_t>(stream)),
@@ -191,7 +196,7 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
     ROWS(q, q_stride, width, cache->dt);
     ROWS(q_out, q_out_stride, width, cache->dt);
     REQUIRE((q == q_out && q_stride == q_out_stride) ||
-                !overlap(q, span(batch.T, q_stride, width, cache->dt), q_out, span(batch.T, q_out_stride, width, cache->dt)),
+                !rows_overlap(q, q_stride, q_out, q_out_stride, batch.T, width, cache->dt),
             "q_out must be q with the same stride or not overlap it");
   }
   dmoe::AppendArgs a{*cache, layer, batch, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, n_heads, rope};
@@ -236,8 +241,7 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   const long width = static_cast<long>(n_heads) * cache->head_dim;
   ROWS(q, q_stride, width, cache->dt);
   ROWS(out, out_stride, width, cache->dt);
-  REQUIRE(!overlap(q, span(batch.T, q_stride, width, cache->dt), out, span(batch.T, out_stride, width, cache->dt)),
-          "out must not overlap q");
+  REQUIRE(!rows_overlap(q, q_stride, out, out_stride, batch.T, width, cache->dt), "out must not overlap q");
   ALIGNED(plan);
   ALIGNED(workspace);
   ALIGNED_TO(lse, 4);

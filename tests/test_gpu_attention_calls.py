@@ -402,3 +402,28 @@ def test_single_tokens_of_an_attention_layer(gpu_lib, dtype):
             ref = R.attention(q[i:i + 1], c.k.cpu().view(-1)[ka], c.v.cpu().view(-1)[va], torch.tensor([m]), 1 / math.sqrt(32))
             tol, _ = R.bounds(dtype, 32, m, *ref)
             assert bool(((o[i:i + 1].double() - ref[0]).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_columns_of_one_tensor(gpu_lib, dtype):
+    """Inputs and outputs side by side in one wider tensor share rows' span and no element."""
+    s = Setup(dtype, 6, 2, 72, 32, [90, 40], [33, 2], 8, seed=6)
+    want, _ = s.run()
+    T, W = s.q.shape[1], 6 * 72
+    wide = torch.full((T, 3 * W + 8), 3.0, dtype=dtype, device="cuda")
+    part = lambda at: wide[:, at:at + W].view(T, 6, 72)  # noqa: E731
+    part(8).copy_(s.qd[0])
+    part(8 + W).fill_(7.0)
+    s.att.attend(0, part(8), part(8 + W))
+    assert torch.equal(part(8 + W).cpu(), want) and torch.equal(part(8), s.qd[0])
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    rope = Rope(72)
+    turned = rope.apply(s.qd[0].clone(), pos)
+    assert torch.equal(rope.apply(part(8), pos, out=part(8 + 2 * W)), turned)
+    kv = torch.randn(T, 2, 72, device="cuda").to(dtype)
+    s.att.append(0, kv, kv, part(8), part(8 + W))
+    used = s.off[-1]
+    assert torch.equal(part(8 + W)[:used], s.qd[0][:used]) and torch.equal(part(8 + 2 * W), turned) and (wide[:, :8] == 3.0).all()
+    for at in (16, W, 8):
+        with pytest.raises(lib.DmoeError, match="overlap"):
+            s.att.attend(0, part(8), part(at))
