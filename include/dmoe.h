@@ -711,7 +711,7 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
  * out_stride elements apart (multiples of 16 bytes); out must not overlap q.
  * lse: [T][n_heads].
  * Limits: n_heads a multiple of n_kv_heads, n_heads / n_kv_heads <= 1024;
- * scale > 0 and finite; T * n_heads <= 2^30.
+ * scale > 0 and scale * log2(e) finite; T * n_heads <= 2^30.
  */
 size_t dmoe_attention_plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
 size_t dmoe_attention_workspace_size(dmoe_dtype dt, int n_seqs, int T, int max_new, int n_heads, int n_kv_heads,

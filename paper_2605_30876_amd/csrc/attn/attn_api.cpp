@@ -237,7 +237,8 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   REQUIRE(layer >= 0 && layer < cache->n_layers, "layer=%d must be in [0, %d)", layer, cache->n_layers);
   REQUIRE(q && plan && out && workspace, "q, plan, out and workspace must not be NULL");
   REQUIRE(mask_block >= 0, "mask_block=%d must be >= 0", mask_block);
-  REQUIRE(scale > 0.f && std::isfinite(scale), "scale=%g must be above 0 and finite", static_cast<double>(scale));
+  REQUIRE(scale > 0.f && std::isfinite(scale * 1.44269504f), "scale=%g must be above 0 and scale * log2(e) finite",
+          static_cast<double>(scale));
   const long width = static_cast<long>(n_heads) * cache->head_dim;
   ROWS(q, q_stride, width, cache->dt);
   ROWS(out, out_stride, width, cache->dt);

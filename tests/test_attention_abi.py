@@ -235,3 +235,12 @@ def test_yarn_ramps_beyond_the_pairs(rot, base, original, slow):
     got, _ = lib.dmoe_rope_turns(rot, base, "yarn", 8.0, original)
     want = [f / 8 for f in plain] if slow else plain
     assert all(abs(a - b) <= 1e-15 * b for a, b in zip(got, want))
+
+
+def test_scales_beyond_float32_are_refused(L, p):
+    """The kernels' scores are in units of log 2: scale * log2(e) has to be a float32 too."""
+    name, f = "dmoe_attention", calls(p)["dmoe_attention"]
+    for scale in (3e38, 2.4e38):
+        assert status(L, name, *f(cache(p), batch(p), scale=scale, ints=0)) == BAD and "scale" in L.dmoe_last_error().decode(), scale
+    for scale in (2.3e38, 1e-40):  # what is refused then is the plan
+        assert status(L, name, *f(cache(p), batch(p), scale=scale, ints=0)) == BAD and "plan" in L.dmoe_last_error().decode(), scale
