@@ -562,8 +562,9 @@ dmoe_status dmoe_moe_forward(const void* x, const void* w_router, const float* b
  *   y1 = scale (x1 cos a - x2 sin a),  y2 = scale (x2 cos a + x1 sin a);
  * pairs are elements (2i, 2i + 1) if interleaved, else (i, i + R/2); elements
  * from R on pass through unchanged.  Angles are formed in binary64 (p f_i is
- * reduced to a fraction of a turn), so far positions lose nothing; the
- * rotation is float32, rounded once to the storage type.
+ * reduced to a fraction of a turn, which is taken to float32): off by 2^-23
+ * and |p| 2^-52 of a radian at most, 2^-20 at position 2^31.  Their sine and cosine and
+ * the rotation are float32, rounded once to the storage type.
  */
 typedef struct dmoe_rotary {
   const double* turns;  /* [rot_dim/2] device: turns per position (dmoe_rope_turns) */
@@ -673,7 +674,7 @@ typedef struct dmoe_batch {
  * stride; q and q_out may both be NULL).  rope.turns NULL: nothing is
  * rotated.  The positions' pages must have been given out (dmoe_cache_update)
  * and must be the sequence's own.  Storing the same positions again (a block
- * denoised over several steps) overwrites them.  Strides in elements between
+ * denoised over several steps) overwrites them.  q_out must not overlap k or v.  Strides in elements between
  * rows, multiples of 16 bytes.  Two sequences of a batch must not be the same
  * slot.
  * Limits: n_heads a multiple of n_kv_heads, up to 1024 * n_kv_heads and 8192, if q is set.

@@ -260,8 +260,9 @@ class BlockAttention:
 
     def begin(self, q_offsets: torch.Tensor, slots: torch.Tensor | None = None):
         """The step's batch: sequence i is rows q_offsets[i] .. q_offsets[i+1] of its tensors and slot slots[i]
-        (default i) of the cache.  int32 device tensors, read by the calls that follow; :meth:`attend` needs a
-        :meth:`plan` of it first."""
+        (default i) of the cache.  int32 device tensors, read by the calls that follow (kept here until the next
+        begin(); a graph that captured such calls needs them as long as it lives); :meth:`attend` needs a :meth:`plan`
+        of it first."""
         _i32(q_offsets, "q_offsets", self.cache.device, self.n_seqs + 1)
         if slots is not None:
             _i32(slots, "slots", self.cache.device, self.n_seqs)

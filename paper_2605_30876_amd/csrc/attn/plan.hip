@@ -1,9 +1,9 @@
 // The attention's work items, made on the device: a step's lengths never
 // visit the host, and every layer of the step uses the one plan.  One
 // workgroup: prefix sums over sequences and row tiles, then an item per thread.
-// 4.8 us for one sequence, 5.5 for 64: half of it the launch, the rest three
+// 5.4 us for one sequence, 6.6 for 64: half of it the launch, the rest three
 // round trips (offsets and slots, lengths, page ids) and the barriers; 1024
-// threads took 7.5.
+// threads took 2.7 more.
 #include "cache.h"
 
 namespace dmoe {
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   // workgroups but do not pass it, and row tiles of about one length that are more
   // than half of the aim are not split.  Of uneven lengths they are, into two
   // rounds, in pieces that are long beside their partial results: 60 blocks of up
-  // to 16k, 12 query and 3 kv heads of 32: 93 -> 69 us; 48 of up to 8k, 64 and 8 of 128: 285 -> 250;
-  // fp32, 73 of 24 tokens of up to 5k, 10 and 2 of 96: 240 -> 195.  With fewer row tiles it costs
+  // to 16k, 12 query and 3 kv heads of 32: 93 -> 67 us; 48 of up to 8k, 64 and 8 of 128: 285 -> 245;
+  // fp32, 73 of 24 tokens of up to 5k, 10 and 2 of 96: 240 -> 196.  With fewer row tiles it costs
   // more than it evens out: 32 blocks of up to 16k, 16 and 4 of 128: 66 -> 74.
   // Items of 32 rows are cheap to join: pieces of the average length even the
   // sequences out, of half of it where there are many sequences (64 of up to 16k tokens:

@@ -6,9 +6,9 @@
 // cos and sin are formed once, in registers, for all of its heads; no two
 // lanes load the same bytes and nothing passes through LDS.  The work is
 // bytes: every element is read and written once.  bf16, 32 query and 8 kv heads
-// of 128: 8000 prompt tokens in 59 us (217 MB, 3.7 TB/s; the values' turn through LDS
+// of 128: 8000 prompt tokens in 60 us (217 MB, 3.6 TB/s; the values' turn through LDS
 // is 11 us of it, a large copy runs at 4.9 TB/s); fp32, 4096 rows of 12 heads of 96: 8.5 us
-// (38 MB, 4.4 TB/s).  A block of 32 tokens takes 4.2 us, three round trips to memory and the launch.
+// (38 MB, 4.4 TB/s).  A block of 32 tokens takes 4.4 us, three round trips to memory and the launch.
 #include "cache.h"
 
 namespace dmoe {
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int tile
 }
 
 // Heads of a workgroup that rotates.  One where that leaves few workgroups (a
-// block of 32 tokens, 20 heads: 4.2 us against 4.5 with four); else as many as its lanes
+// block of 32 tokens, 20 heads: 0.3 us less than with four); else as many as its lanes
 // take at once (64 single tokens: 8.1 us with one, 6.2 with four; 46 sequences of 2, 24 heads of
 // 32: 15.5 with one, 6.1), and as keep kGroups workgroups, so that angles are formed for
 // as many heads as possible.  launched: token groups of the grid, some empty.
