@@ -346,8 +346,9 @@ class AttentionLayer:
         a, c, w = self.att, self.att.cache, self.w
         if tuple(x.shape) != (a.T, self.H) or x.dtype != c.dtype or x.device != c.device:
             raise ValueError(f"x must be {c.dtype} [{a.T}, {self.H}] on {c.device}, not {x.dtype} {list(x.shape)} on {x.device}")
-        for name, t in (("x", x), *w.items()):
-            _no_gradient(t, name)
+        _no_gradient(x, "x")
+        for name in ("wq", "wk", "wv", "wo"):
+            _no_gradient(w[name], name)
         with torch.no_grad(), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(c.device)):
             torch.mm(x, w["wq"].t(), out=self.q)
             torch.mm(x, w["wk"].t(), out=self.k)

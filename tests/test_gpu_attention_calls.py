@@ -427,3 +427,11 @@ def test_columns_of_one_tensor(gpu_lib, dtype):
     for at in (16, W, 8):
         with pytest.raises(lib.DmoeError, match="overlap"):
             s.att.attend(0, part(8), part(at))
+
+
+def test_weights_that_an_attention_layer_does_not_use(gpu_lib):
+    """A layer's whole set of weights may be passed, whatever else it holds."""
+    h = Half()
+    want = h.step()
+    more = {"bias": None, "norm": torch.ones(4, device="cuda", requires_grad=True), **h.w}
+    assert torch.equal(h.step(AttentionLayer(h.att, 0, more)), want)
