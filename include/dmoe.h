@@ -638,7 +638,7 @@ typedef struct dmoe_cache {
   int32_t* refs; /* used by dmoe_cache_update and dmoe_cache_compact only, else may be NULL */
   dmoe_dtype dt;
   int n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages;
-  int32_t* refused; /* may be NULL: then no refusal is remembered */
+  int32_t* refused; /* read by every call; NULL: no refusal is remembered */
 } dmoe_cache;
 
 /* Bytes of one page of keys (or of values) of one layer; 0 on invalid sizes. */

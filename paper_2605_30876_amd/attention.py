@@ -169,8 +169,9 @@ class PagedCache:
         """The last workspace, or a larger one of the call's stream outside graph capture (a captured call keeps the one
         it was captured with)."""
         if self._ws[-1].numel() < nbytes:
+            capturing = torch.cuda.is_current_stream_capturing()
             with _stream(stream):
-                if torch.cuda.is_current_stream_capturing():
+                if capturing or torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("the cache's workspace is too small for this call: run it once before capturing it")
                 self._ws.append(torch.empty((nbytes,), dtype=torch.uint8, device=self.device))
         return self._ws[-1]

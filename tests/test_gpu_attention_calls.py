@@ -435,3 +435,20 @@ def test_weights_that_an_attention_layer_does_not_use(gpu_lib):
     want = h.step()
     more = {"bias": None, "norm": torch.ones(4, device="cuda", requires_grad=True), **h.w}
     assert torch.equal(h.step(AttentionLayer(h.att, 0, more)), want)
+
+
+@pytest.mark.parametrize("where", ["current", "other"])
+def test_no_workspace_is_made_during_a_capture(gpu_lib, where):
+    """Whether the call is on the stream that captures or on another: memory is not allocated outside the graph's pool."""
+    cache = PagedCache(1, 64, 32, 1, 32, 4, 128)
+    slots, lens, side = i32([i % 4 for i in range(3000)]), i32([1] * 3000), torch.cuda.Stream()
+    g, n = torch.cuda.CUDAGraph(), len(cache._ws)
+    x = torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        with pytest.raises(RuntimeError, match="workspace"):
+            cache.resize(slots, lens, stream=side if where == "other" else None)
+        x.add_(1.0)
+    g.replay()
+    torch.cuda.synchronize()
+    assert len(cache._ws) == n and (x == 1.0).all() and cache.lens.tolist() == [0] * 4
