@@ -605,11 +605,34 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
                       int head_dim, const int32_t* positions, dmoe_rotary rope, int inverse, void* stream);
 
 /*
+ * What a cache holds of a key or value: the element itself, of the cache's dt,
+ * or a code and, for each 32 consecutive elements of a token's head, a scale.
+ *   DMOE_KV_PLAIN    elements of dt
+ *   DMOE_KV_FP8      e4m3 codes: 8 bits, 4 of the exponent (bias 7) and 3 of the fraction, largest 448
+ *   DMOE_KV_FP4      e2m1 codes: 4 bits, the sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6
+ *   DMOE_KV_FP8_FP4  keys as FP8, values as FP4
+ * A scale is a byte b and means 2^(b - 127); an element is its code times its
+ * group's scale, which bf16 holds exactly.  dmoe_cache_append takes for b the smallest at
+ * which no element of the group is off by more than half a step: the largest
+ * |element| is at most 464 (FP4: 7) times the scale; not below 17, and
+ * not above 246 (252), where the largest codes reach bf16's range (elements beyond
+ * become the largest code).  Codes are rounded to nearest, ties to the even
+ * code.  A group with an element that is not finite has b = 255 and codes of 0: all of it is NaN.
+ */
+typedef enum dmoe_kv_format {
+  DMOE_KV_PLAIN = 0,
+  DMOE_KV_FP8 = 1,
+  DMOE_KV_FP4 = 2,
+  DMOE_KV_FP8_FP4 = 3
+} dmoe_kv_format;
+
+/*
  * A paged cache: keys and values of n_layers layers in pages of page_tokens
  * tokens, and the page table of n_slots sequences.  All arrays are device
  * memory of the caller's (the struct itself is a HOST struct, read during the
  * call).
- *   k, v   [n_layers][n_pages][page], page = dmoe_cache_page_bytes bytes
+ *   k, v   [n_layers][n_pages][page], page = dmoe_cache_key_page_bytes (dmoe_cache_value_page_bytes) bytes
+ *   dt     of the rows that are stored and read, of queries and results; of the elements too if format is DMOE_KV_PLAIN
  *   table  [n_slots][max_pages] page ids; those of tokens from lens on are -1
  *   lens   [n_slots] tokens of the sequence (its new ones included)
  *   refs   [n_pages] sequences that hold the page; 0: free
@@ -624,6 +647,12 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
  *   v page [n_kv_heads][page_tokens/32][dp/32][16/c][2][32][c/4][4]:
  *     token 2c*s + 8j + 4h + t of the tile, element 32b + d at [b][s][h][d][j][t]
  * so that one matrix operand is one contiguous KiB.
+ * In a cache of few bits (format, below) a page holds, per kv head and tile of 32 tokens,
+ * 16-byte chunks of a token's codes, then its scale bytes; with w = 32 (16) elements to a chunk
+ * of 4-bit (8-bit) codes and sb the least power of two that holds dp/32:
+ *   page [n_kv_heads][page_tokens/32][tile], tile = [dp/w][32][16] codes, [32][sb] scales:
+ *     token r's elements w*j .. w*j + w-1 at [j][r] (4 bits: element 2i in the low half of
+ *     byte i), the scale of its elements 32g .. 32g + 31 at [r][g] (bytes from dp/32 on are not used)
  * A page id outside [0, n_pages) where a token should be is never followed:
  * nothing is stored there and no key is seen there.
  * Limits: n_layers, n_pages, n_slots, max_pages >= 1; page_tokens a multiple
@@ -639,10 +668,14 @@ typedef struct dmoe_cache {
   dmoe_dtype dt;
   int n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages;
   int32_t* refused; /* read by every call; NULL: no refusal is remembered */
+  dmoe_kv_format format; /* 0: DMOE_KV_PLAIN */
 } dmoe_cache;
 
-/* Bytes of one page of keys (or of values) of one layer; 0 on invalid sizes. */
+/* Bytes of one page of keys, and of values, of one layer; 0 on invalid sizes.
+ * dmoe_cache_page_bytes: of either, in a plain cache. */
 size_t dmoe_cache_page_bytes(dmoe_dtype dt, int page_tokens, int n_kv_heads, int head_dim);
+size_t dmoe_cache_key_page_bytes(dmoe_dtype dt, dmoe_kv_format format, int page_tokens, int n_kv_heads, int head_dim);
+size_t dmoe_cache_value_page_bytes(dmoe_dtype dt, dmoe_kv_format format, int page_tokens, int n_kv_heads, int head_dim);
 
 /*
  * The new tokens of a step.  Sequence i of n_seqs is slot slots[i] of the
@@ -674,7 +707,9 @@ typedef struct dmoe_batch {
  * stride; q and q_out may both be NULL).  rope.turns NULL: nothing is
  * rotated.  The positions' pages must have been given out (dmoe_cache_update)
  * and must be the sequence's own.  Storing the same positions again (a block
- * denoised over several steps) overwrites them.  q_out must not overlap k or v.  Strides in elements between
+ * denoised over several steps) overwrites them.  In a cache of few bits keys are rotated in binary64
+ * (turned by a, its cos and sin in binary64 too), rounded to float32 and from there to dt, then quantised (dmoe_kv_format): what
+ * is stored does not depend on the order of a sum.  q_out must not overlap k or v.  Strides in elements between
  * rows, multiples of 16 bytes.  Two sequences of a batch must not be the same
  * slot.
  * Limits: n_heads a multiple of n_kv_heads, up to 1024 * n_kv_heads and 8192, if q is set.
@@ -682,6 +717,20 @@ typedef struct dmoe_batch {
 dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch batch, const void* k, long k_stride,
                               const void* v, long v_stride, const void* q, long q_stride, void* q_out,
                               long q_out_stride, int n_heads, dmoe_rotary rope, void* stream);
+
+/*
+ * Keys and values of tokens as the cache holds them, of any format, into rows of
+ * dt: row q_offsets[i] + j of k and v [T][n_kv_heads][head_dim] receives token
+ * starts[i] + j of sequence i (starts NULL: its last tokens, as dmoe_cache_append
+ * stores them).  max_new bounds the tokens of a sequence.  A token that the sequence does not
+ * have (its position is negative, or lens or above) or that lies on no page
+ * is 0.  Rows of no sequence, and of one whose slot is marked in the cache's refused, are left
+ * as they are.  A slot may be read by several sequences of the batch.  Either of k and v may be
+ * NULL.  starts: int32 [n_seqs], cut to [0, max_pages*page_tokens].  Strides as for
+ * dmoe_cache_append; k and v must not overlap each other or the cache.
+ */
+dmoe_status dmoe_cache_read(const dmoe_cache* cache, int layer, dmoe_batch batch, const int32_t* starts, void* k,
+                            long k_stride, void* v, long v_stride, void* stream);
 
 /*
  * Attention of the step's new tokens over the cache.  Query head h reads kv
@@ -696,7 +745,8 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
  * A row that sees no key, or only keys of score -inf, is 0 with lse -inf.  What a row does not see does not
  * reach it, whatever it holds (NaN and infinities included).  Scores, softmax statistics and
  * sums are float32; with DMOE_BF16 the probabilities are rounded to bf16
- * (relative 2^-8, the matrix operand's type), their sum is not.
+ * (relative 2^-8, the matrix operand's type), their sum is not.  Codes of a cache of few bits enter the products as
+ * code * scale, exactly, with float32 rows too.
  *
  * dmoe_attention_plan cuts the step's rows and keys into work items: long
  * sequences are split along their keys so that a few rows still use the whole

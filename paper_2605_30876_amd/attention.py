@@ -114,6 +114,10 @@ class PagedCache:
     (layouts: dmoe_cache in include/dmoe.h) instead of new, empty ones (keys
     and values 0); the others are then made on their device.
 
+    ``format``: what the pages hold: "plain", elements of ``dtype``; "fp8" or "fp4", codes of 8 or 4 bits with a scale per 32
+    elements of a token's head; "fp8_fp4", keys in 8 bits and values in 4 (dmoe_kv_format).  The rows
+    that are appended, read and attended with are of ``dtype`` all the same.  k and v of a cache of few bits are uint8.
+
     ``status`` holds the outcome of the last update that was given no tensor
     of its own for it; ``refused`` [n_slots] of every slot's last update, 0 if it was done.  A
     slot that is marked there has no new tokens: :meth:`BlockAttention.append`
@@ -121,24 +125,29 @@ class PagedCache:
 
     def __init__(self, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, n_slots: int,
                  max_pages: int, dtype: torch.dtype = torch.bfloat16, device="cuda", k=None, v=None, table=None, lens=None,
-                 refs=None):
+                 refs=None, format: str = "plain"):
         dt = {torch.float32: lib.DMOE_F32, torch.bfloat16: lib.DMOE_BF16}.get(dtype)
         if dt is None:
             raise TypeError(f"unsupported element type {dtype}")
-        page_bytes = lib.dmoe_cache_page_bytes(dt, page_tokens, n_kv_heads, head_dim)
-        if page_bytes == 0:
+        if format not in lib.KV_FORMAT:
+            raise ValueError(f"format must be one of {sorted(lib.KV_FORMAT)}, not {format!r}")
+        fmt = lib.KV_FORMAT[format]
+        page_bytes = [size(dt, fmt, page_tokens, n_kv_heads, head_dim) for size in (lib.dmoe_cache_key_page_bytes, lib.dmoe_cache_value_page_bytes)]
+        if page_bytes[0] == 0:
             raise ValueError(f"no such page: page_tokens={page_tokens}, n_kv_heads={n_kv_heads}, head_dim={head_dim}")
         self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads = n_layers, n_pages, page_tokens, n_kv_heads
         self.head_dim, self.n_slots, self.max_pages, self.dtype = head_dim, n_slots, max_pages, dtype
-        elems = page_bytes // torch.empty((), dtype=dtype).element_size()
+        self.format = format
+        held = dtype if format == "plain" else torch.uint8
+        elems = [n // torch.empty((), dtype=held).element_size() for n in page_bytes]
         # new arrays lie where the given ones do: a kernel follows the addresses of all of them
         device = next((t.device for t in (k, v, table, lens, refs) if t is not None), device)
 
-        def pool(t, name):
+        def pool(t, name, elems):
             if t is None:
-                return torch.zeros((n_layers, n_pages, elems), dtype=dtype, device=device)
-            if tuple(t.shape) != (n_layers, n_pages, elems) or t.dtype != dtype or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous {dtype} [{n_layers}, {n_pages}, {elems}]")
+                return torch.zeros((n_layers, n_pages, elems), dtype=held, device=device)
+            if tuple(t.shape) != (n_layers, n_pages, elems) or t.dtype != held or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {held} [{n_layers}, {n_pages}, {elems}]")
             return t
 
         def ints(t, name, shape, fill):
@@ -148,7 +157,7 @@ class PagedCache:
                 raise ValueError(f"{name} must be int32 {list(shape)}")
             return _i32(t, name, self.k.device)
 
-        self.k, self.v = pool(k, "k"), pool(v, "v")
+        self.k, self.v = pool(k, "k", elems[0]), pool(v, "v", elems[1])
         if self.v.device != self.k.device:
             raise ValueError(f"k is on {self.k.device}, v on {self.v.device}")
         self.table = ints(table, "table", (n_slots, max_pages), -1)
@@ -159,7 +168,7 @@ class PagedCache:
         self.refused = torch.zeros((n_slots,), dtype=torch.int32, device=device)
         self.c = lib.dmoe_cache(lib.ptr(self.k), lib.ptr(self.v), lib.ptr(self.table), lib.ptr(self.lens), lib.ptr(self.refs),
                                 dt, n_layers, n_pages, page_tokens, n_kv_heads, head_dim, n_slots, max_pages,
-                                lib.ptr(self.refused))
+                                lib.ptr(self.refused), fmt)
         # for calls on every slot, where that is not much; larger calls add one of their own
         nbytes = max(lib.dmoe_cache_update_workspace_size(min(n_slots, 4096), max_pages, n_pages),
                      lib.dmoe_cache_compact_workspace_size(n_pages))
@@ -221,6 +230,33 @@ class PagedCache:
         with _On(self.device):
             ws = self._workspace(lib.dmoe_cache_compact_workspace_size(self.n_pages), stream)
             lib.dmoe_cache_compact(self.c, table_out, refs_out, counts, ws, stream)
+
+    def read(self, layer: int, q_offsets: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
+             slots: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_tokens: int | None = None, stream=None):
+        """Keys and values of tokens as the cache holds them, into k and v [T, n_kv_heads, head_dim] (either may be None): rows
+        q_offsets[i] .. q_offsets[i+1] receive the tokens from starts[i] on of slot slots[i] (default i), by default its
+        last ones (dmoe_cache_read).  Tokens that the sequence does not have are 0, rows of no sequence stay as they
+        are.  int32 device tensors; max_tokens: an upper bound of every sequence's tokens (default: every row)."""
+        d, T = self.device, next((t.shape[0] for t in (k, v) if t is not None), None)
+        if T is None:
+            raise ValueError("read() needs k or v")
+        n = q_offsets.numel() - 1
+        _i32(q_offsets, "q_offsets", d)
+        if n < 1:
+            raise ValueError("q_offsets must hold a value more than there are sequences")
+        for t, name in ((slots, "slots"), (starts, "starts")):
+            if t is not None:
+                _i32(t, name, d, n)
+        for t, name in ((k, "k"), (v, "v")):
+            if t is not None:
+                _heads(t, name, T, self.n_kv_heads, self.head_dim, self.dtype, d)
+                if t.shape[0] != T:
+                    raise ValueError(f"k and v must have the same rows, not {k.shape[0]} and {v.shape[0]}")
+        if T == 0:
+            return
+        with _On(d):
+            batch = lib.dmoe_batch(lib.ptr(q_offsets), lib.ptr(slots), n, T, T if max_tokens is None else max_tokens)
+            lib.dmoe_cache_read(self.c, layer, batch, starts, k, v, stream)
 
     def copy_pages(self, pairs: torch.Tensor, stream=None):
         """Copies page pairs[i, 0] to page pairs[i, 1], all layers."""

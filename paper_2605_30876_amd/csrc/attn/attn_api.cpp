@@ -24,6 +24,7 @@ bool valid_page(int page_tokens, int n_kv_heads, int head_dim) {
   return page_tokens >= 32 && page_tokens <= kMaxPageTokens && page_tokens % 32 == 0 && n_kv_heads >= 1 &&
          n_kv_heads <= kMaxKvHeads && valid_head_dim(head_dim);
 }
+bool valid_format(dmoe_kv_format f) { return f >= DMOE_KV_PLAIN && f <= DMOE_KV_FP8_FP4; }
 bool misaligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
 #define ALIGNED_TO(p, n) REQUIRE(!misaligned_to(p, n), #p " is not " #n "-byte aligned")
@@ -49,6 +50,7 @@ dmoe_status check_cache(const char* fn, const dmoe_cache* c, bool refs) {
   REQUIRE(c->k && c->v && c->table && c->lens, "the cache's k, v, table and lens must not be NULL");
   REQUIRE(!refs || c->refs, "the cache's refs must not be NULL");
   REQUIRE(valid_dtype(c->dt), "unknown dtype %d", static_cast<int>(c->dt));
+  REQUIRE(valid_format(c->format), "unknown cache format %d", static_cast<int>(c->format));
   REQUIRE(c->n_layers >= 1 && c->n_pages >= 1 && c->n_slots >= 1 && c->max_pages >= 1,
           "n_layers=%d, n_pages=%d, n_slots=%d and max_pages=%d must be >= 1", c->n_layers, c->n_pages, c->n_slots, c->max_pages);
   REQUIRE(valid_page(c->page_tokens, c->n_kv_heads, c->head_dim),
@@ -174,6 +176,16 @@ size_t dmoe_cache_page_bytes(dmoe_dtype dt, int page_tokens, int n_kv_heads, int
   return static_cast<size_t>(dmoe::page_elems(page_tokens, n_kv_heads, head_dim)) * dmoe::dtype_bytes(dt);
 }
 
+size_t dmoe_cache_key_page_bytes(dmoe_dtype dt, dmoe_kv_format format, int page_tokens, int n_kv_heads, int head_dim) {
+  if (!valid_dtype(dt) || !valid_format(format) || !valid_page(page_tokens, n_kv_heads, head_dim)) return 0;
+  return static_cast<size_t>(dmoe::page_bytes(dt, dmoe::key_bits(format), page_tokens, n_kv_heads, head_dim));
+}
+
+size_t dmoe_cache_value_page_bytes(dmoe_dtype dt, dmoe_kv_format format, int page_tokens, int n_kv_heads, int head_dim) {
+  if (!valid_dtype(dt) || !valid_format(format) || !valid_page(page_tokens, n_kv_heads, head_dim)) return 0;
+  return static_cast<size_t>(dmoe::page_bytes(dt, dmoe::value_bits(format), page_tokens, n_kv_heads, head_dim));
+}
+
 dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch batch, const void* k, long k_stride,
                               const void* v, long v_stride, const void* q, long q_stride, void* q_out,
                               long q_out_stride, int n_heads, dmoe_rotary rope, void* stream) {
@@ -200,7 +212,23 @@ dmoe_status dmoe_cache_append(const dmoe_cache* cache, int layer, dmoe_batch bat
             "q_out must be q with the same stride or not overlap it");
   }
   dmoe::AppendArgs a{*cache, layer, batch, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, n_heads, rope};
-  return hip_status(dmoe::launch_append(a, static_cast<hipStream_t>(stream)), __func__);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return hip_status(cache->format == DMOE_KV_PLAIN ? dmoe::launch_append(a, s) : dmoe::launch_append_quant(a, s), __func__);
+}
+
+dmoe_status dmoe_cache_read(const dmoe_cache* cache, int layer, dmoe_batch batch, const int32_t* starts, void* k,
+                            long k_stride, void* v, long v_stride, void* stream) {
+  FORWARD(check_cache(__func__, cache, false));
+  FORWARD(check_batch(__func__, cache, batch));
+  REQUIRE(layer >= 0 && layer < cache->n_layers, "layer=%d must be in [0, %d)", layer, cache->n_layers);
+  REQUIRE(k || v, "k and v must not both be NULL");
+  const long width = static_cast<long>(cache->n_kv_heads) * cache->head_dim;
+  if (k) ROWS(k, k_stride, width, cache->dt);
+  if (v) ROWS(v, v_stride, width, cache->dt);
+  REQUIRE(!k || !v || !rows_overlap(k, k_stride, v, v_stride, batch.T, width, cache->dt), "k and v must not overlap");
+  ALIGNED_TO(starts, 4);
+  dmoe::ReadArgs a{*cache, layer, batch, starts, k, k_stride, v, v_stride};
+  return hip_status(dmoe::launch_read(a, static_cast<hipStream_t>(stream)), __func__);
 }
 
 size_t dmoe_attention_plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
@@ -235,6 +263,7 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   FORWARD(check_batch(__func__, cache, batch));
   FORWARD(check_heads(__func__, batch.T, n_heads, cache->n_kv_heads));
   REQUIRE(layer >= 0 && layer < cache->n_layers, "layer=%d must be in [0, %d)", layer, cache->n_layers);
+  SUPPORT(cache->format == DMOE_KV_PLAIN, "no attention over a cache of few bits");
   REQUIRE(q && plan && out && workspace, "q, plan, out and workspace must not be NULL");
   REQUIRE(mask_block >= 0, "mask_block=%d must be >= 0", mask_block);
   REQUIRE(scale > 0.f && std::isfinite(scale * 1.44269504f), "scale=%g must be above 0 and scale * log2(e) finite",

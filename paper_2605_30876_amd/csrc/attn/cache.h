@@ -18,6 +18,29 @@ inline long page_elems(int page_tokens, int n_kv_heads, int head_dim) {
   return static_cast<long>(page_tokens) * n_kv_heads * padded_dim(head_dim);
 }
 
+// A cache in few bits: bits of an element of its keys and values (0: plain),
+// elements that share a scale, scale bytes of a token's head (a power of two), bytes of a tile.
+__host__ __device__ constexpr int key_bits(dmoe_kv_format f) { return f == DMOE_KV_PLAIN ? 0 : f == DMOE_KV_FP4 ? 4 : 8; }
+__host__ __device__ constexpr int value_bits(dmoe_kv_format f) { return f == DMOE_KV_PLAIN ? 0 : f == DMOE_KV_FP8 ? 8 : 4; }
+constexpr int kGroup = 32;
+__host__ __device__ constexpr int scale_row(int dp) { return dp <= 32 ? 1 : dp <= 64 ? 2 : dp <= 128 ? 4 : 8; }
+__host__ __device__ constexpr int quant_tile(int bits, int dp) { return dp * 4 * bits + kTileTokens * scale_row(dp); }
+// Bytes from the start of a tile to the code of token r's element d (4 bits: of an even one and the next) and to its scales.
+template <int kBits>
+__host__ __device__ constexpr int code_at(int r, int d) {
+  constexpr int per = 128 / kBits;  // elements of a 16-byte chunk
+  return (d / per * kTileTokens + r) * 16 + d % per * kBits / 8;
+}
+template <int kBits>
+__host__ __device__ constexpr int scale_at(int dp, int r) {
+  return dp * 4 * kBits + r * scale_row(dp);
+}
+// Bytes of a page of keys, or of values.
+inline long page_bytes(dmoe_dtype dt, int bits, int page_tokens, int n_kv_heads, int head_dim) {
+  if (bits == 0) return page_elems(page_tokens, n_kv_heads, head_dim) * static_cast<long>(dtype_bytes(dt));
+  return static_cast<long>(page_tokens / kTileTokens) * n_kv_heads * quant_tile(bits, padded_dim(head_dim));
+}
+
 // Elements from the start of a tile's keys (values) to one 16-byte chunk of
 // c values.  Keys: chunk of token r, elements c*j .. c*j + c-1.  Values: chunk
 // of element d, tokens 2c*s + 8j + 4h + t for j < c/4, t < 4.
@@ -181,6 +204,7 @@ struct AttnArgs {
 };
 hipError_t launch_attention_bf16(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
 hipError_t launch_attention_f32(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
+hipError_t launch_attention_quant(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
 hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
                                  int32_t* plan, hipStream_t s);
 
@@ -202,6 +226,18 @@ struct AppendArgs {
   dmoe_rotary rope;  // turns nullptr: no rotation
 };
 hipError_t launch_append(const AppendArgs& a, hipStream_t s);
+hipError_t launch_append_quant(const AppendArgs& a, hipStream_t s);
+struct ReadArgs {
+  dmoe_cache cache;
+  int layer;
+  dmoe_batch batch;
+  const int32_t* starts;  // or nullptr: the last tokens
+  void* k;                // either may be nullptr
+  long k_stride;
+  void* v;
+  long v_stride;
+};
+hipError_t launch_read(const ReadArgs& a, hipStream_t s);
 
 size_t update_workspace_bytes(long n, long max_pages, long n_pages);
 hipError_t launch_update(const dmoe_cache& c, const int32_t* dst, const int32_t* src, const int32_t* keep,

@@ -294,7 +294,8 @@ constexpr unsigned kCopyGrid = 4096;
 // `moved`, the table is rewritten too.  Non-temporal both ways: 586 MB of a
 // compaction in 122 us against 130 through the caches (4.8 TB/s, the rate of a
 // large copy).
-__global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairList l, long page_len, const int32_t* moved,
+// k_len, v_len: 16-byte pieces of a page of keys and of values.
+__global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairList l, long k_len, long v_len, const int32_t* moved,
                                                             int32_t* table_out) {
   const long gtid = static_cast<long>(blockIdx.x) * kCopyThreads + threadIdx.x;
   if (moved) {
@@ -305,13 +306,15 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairLi
     }
   }
   const int n = l.n ? min(*l.n, l.most) : l.most;
-  const long per_page = (page_len + kUnit - 1) / kUnit;
+  const long per_page = (max(k_len, v_len) + kUnit - 1) / kUnit;
   const long units = n * static_cast<long>(c.n_layers) * 2 * per_page;
   for (long u = blockIdx.x; u < units; u += gridDim.x) {
     const long part = u % per_page, rest = u / per_page;
     const int kv = static_cast<int>(rest % 2), layer = static_cast<int>(rest / 2 % c.n_layers), i = static_cast<int>(rest / 2 / c.n_layers);
     const int a = l.from[static_cast<long>(i) * l.step], b = l.to[static_cast<long>(i) * l.step];
     if (a < 0 || a >= c.n_pages || b < 0 || b >= c.n_pages) continue;
+    const long page_len = kv ? v_len : k_len;
+    if (part * kUnit >= page_len) continue;
     uint4* pool = static_cast<uint4*>(kv ? c.v : c.k) + static_cast<long>(layer) * c.n_pages * page_len;
     const u32x4* s = (const u32x4*)pool + a * page_len + part * kUnit;
     u32x4* d = (u32x4*)pool + b * page_len + part * kUnit;
@@ -327,10 +330,11 @@ __global__ __launch_bounds__(kCopyThreads) void copy_kernel(dmoe_cache c, PairLi
 }
 
 hipError_t copy_pages(const dmoe_cache& c, const PairList& l, const int32_t* moved, int32_t* table_out, hipStream_t s) {
-  const long page_len = page_elems(c.page_tokens, c.n_kv_heads, c.head_dim) * static_cast<long>(dtype_bytes(c.dt)) / 16;
-  const long units = l.most * static_cast<long>(c.n_layers) * 2 * ((page_len + kUnit - 1) / kUnit);
+  const long k_len = page_bytes(c.dt, key_bits(c.format), c.page_tokens, c.n_kv_heads, c.head_dim) / 16;
+  const long v_len = page_bytes(c.dt, value_bits(c.format), c.page_tokens, c.n_kv_heads, c.head_dim) / 16;
+  const long units = l.most * static_cast<long>(c.n_layers) * 2 * (((k_len > v_len ? k_len : v_len) + kUnit - 1) / kUnit);
   const unsigned grid = units < static_cast<long>(kCopyGrid) ? static_cast<unsigned>(units) : kCopyGrid;
-  copy_kernel<<<grid, kCopyThreads, 0, s>>>(c, l, page_len, moved, table_out);
+  copy_kernel<<<grid, kCopyThreads, 0, s>>>(c, l, k_len, v_len, moved, table_out);
   return hipGetLastError();
 }
 

@@ -38,7 +38,8 @@ EXPORTS = ("dmoe_router_workspace_size", "dmoe_router_logits", "dmoe_block_aggre
            "dmoe_version", "dmoe_rope_turns", "dmoe_rope", "dmoe_cache_page_bytes", "dmoe_cache_append",
            "dmoe_attention_plan_ints", "dmoe_attention_workspace_size", "dmoe_attention_plan", "dmoe_attention",
            "dmoe_cache_update_workspace_size", "dmoe_cache_update", "dmoe_cache_compact_workspace_size",
-           "dmoe_cache_compact", "dmoe_cache_copy_pages")
+           "dmoe_cache_compact", "dmoe_cache_copy_pages", "dmoe_cache_key_page_bytes", "dmoe_cache_value_page_bytes",
+           "dmoe_cache_read")
 
 
 class DmoeError(RuntimeError):
@@ -80,11 +81,15 @@ class dmoe_rotary(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+DMOE_KV_PLAIN, DMOE_KV_FP8, DMOE_KV_FP4, DMOE_KV_FP8_FP4 = 0, 1, 2, 3
+KV_FORMAT = {"plain": DMOE_KV_PLAIN, "fp8": DMOE_KV_FP8, "fp4": DMOE_KV_FP4, "fp8_fp4": DMOE_KV_FP8_FP4}
+
+
 class dmoe_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
                 ("refs", ctypes.c_void_p), ("dt", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_pages", ctypes.c_int),
                 ("page_tokens", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
-                ("n_slots", ctypes.c_int), ("max_pages", ctypes.c_int), ("refused", ctypes.c_void_p)]
+                ("n_slots", ctypes.c_int), ("max_pages", ctypes.c_int), ("refused", ctypes.c_void_p), ("format", ctypes.c_int)]
 
 
 class dmoe_batch(ctypes.Structure):
@@ -128,6 +133,9 @@ _SIGS = {
     "dmoe_rope_turns": ([_I, _D, _I, _D, _D, _P, ctypes.POINTER(ctypes.c_float)], _I),
     "dmoe_rope": ([_P, _L, _P, _L, _I, _I, _I, _I, _P, dmoe_rotary, _I, _P], _I),
     "dmoe_cache_page_bytes": ([_I] * 4, _S),
+    "dmoe_cache_key_page_bytes": ([_I] * 5, _S),
+    "dmoe_cache_value_page_bytes": ([_I] * 5, _S),
+    "dmoe_cache_read": ([_CACHE, _I, dmoe_batch, _P, _P, _L, _P, _L, _P], _I),
     "dmoe_cache_append": ([_CACHE, _I, dmoe_batch] + [_P, _L] * 4 + [_I, dmoe_rotary, _P], _I),
     "dmoe_attention_plan_ints": ([_I] * 5, _S),
     "dmoe_attention_workspace_size": ([_I] * 7, _S),
@@ -409,6 +417,19 @@ def dmoe_rope(x, out, T, n_heads, head_dim, positions, rope: dmoe_rotary, invers
 
 def dmoe_cache_page_bytes(dt, page_tokens, n_kv_heads, head_dim) -> int:
     return int(load().dmoe_cache_page_bytes(dt, page_tokens, n_kv_heads, head_dim))
+
+
+def dmoe_cache_key_page_bytes(dt, format, page_tokens, n_kv_heads, head_dim) -> int:
+    return int(load().dmoe_cache_key_page_bytes(dt, format, page_tokens, n_kv_heads, head_dim))
+
+
+def dmoe_cache_value_page_bytes(dt, format, page_tokens, n_kv_heads, head_dim) -> int:
+    return int(load().dmoe_cache_value_page_bytes(dt, format, page_tokens, n_kv_heads, head_dim))
+
+
+def dmoe_cache_read(cache: dmoe_cache, layer, batch: dmoe_batch, starts, k, v, stream=None):
+    _check(load().dmoe_cache_read(cache, layer, batch, ptr(starts), ptr(k), _row_stride(k), ptr(v), _row_stride(v),
+                                  stream_handle(stream)))
 
 
 def dmoe_cache_append(cache: dmoe_cache, layer, batch: dmoe_batch, k, v, q, q_out, n_heads,
