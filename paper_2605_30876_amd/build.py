@@ -22,7 +22,9 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdmoe.so")
 SOURCES = ["dmoe_api.cpp", "router.hip", "routing.hip", "topp.hip", "schedule.hip", "route.hip", "pack.hip",
            "ffn.hip", "ffn_f32.hip", "combine.hip", "noalloc.hip", "layer.hip", "attn/attn_api.cpp", "attn/rope.hip",
-           "attn/append_quant.hip", "attn/pages.hip", "attn/plan.hip", "attn/attention_bf16.hip", "attn/attention_f32.hip"]
+           "attn/append_quant.hip", "attn/pages.hip", "attn/plan.hip", "attn/attention_bf16.hip", "attn/attention_f32.hip",
+           "attn/attention_bf16_fp8.hip", "attn/attention_bf16_fp4.hip", "attn/attention_bf16_fp8_fp4.hip",
+           "attn/attention_f32_fp8.hip", "attn/attention_f32_fp4.hip", "attn/attention_f32_fp8_fp4.hip"]
 ARCH = os.environ.get("DMOE_OFFLOAD_ARCH", "gfx950")
 
 

@@ -1,0 +1,8 @@
+// The attention kernels of attention_quant.h: bf16 rows, keys and values in 8 bits.
+#include "attention_quant.h"
+
+namespace dmoe {
+
+template hipError_t launch_attention_quant<bf16_t, 8, 8>(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
+
+}  // namespace dmoe

@@ -108,6 +108,16 @@ bool rows_overlap(const void* a, long a_stride, const void* b, long b_stride, lo
   return a_stride != b_stride || off < w || pitch - off < w;
 }
 
+template <typename T>
+hipError_t attend(const dmoe::AttnArgs& a, const dmoe::AttnShape& sh, hipStream_t s) {
+  switch (a.cache.format) {
+    case DMOE_KV_FP8: return dmoe::launch_attention_quant<T, 8, 8>(a, sh, s);
+    case DMOE_KV_FP4: return dmoe::launch_attention_quant<T, 4, 4>(a, sh, s);
+    case DMOE_KV_FP8_FP4: return dmoe::launch_attention_quant<T, 8, 4>(a, sh, s);
+    default: return sizeof(T) == 4 ? dmoe::launch_attention_f32(a, sh, s) : dmoe::launch_attention_bf16(a, sh, s);
+  }
+}
+
 bool valid_shape(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
   return n_seqs >= 1 && n_seqs <= kMaxSeqs && T >= 1 && T <= kMaxRows && max_new >= 1 && n_kv_heads >= 1 && n_kv_heads <= kMaxKvHeads &&
          n_heads >= 1 && n_heads % n_kv_heads == 0 && n_heads / n_kv_heads <= kMaxGroup &&
@@ -263,7 +273,6 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   FORWARD(check_batch(__func__, cache, batch));
   FORWARD(check_heads(__func__, batch.T, n_heads, cache->n_kv_heads));
   REQUIRE(layer >= 0 && layer < cache->n_layers, "layer=%d must be in [0, %d)", layer, cache->n_layers);
-  SUPPORT(cache->format == DMOE_KV_PLAIN, "no attention over a cache of few bits");
   REQUIRE(q && plan && out && workspace, "q, plan, out and workspace must not be NULL");
   REQUIRE(mask_block >= 0, "mask_block=%d must be >= 0", mask_block);
   REQUIRE(scale > 0.f && std::isfinite(scale * 1.44269504f), "scale=%g must be above 0 and scale * log2(e) finite",
@@ -283,7 +292,7 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   REQUIRE(ws_bytes >= need, "workspace of %zu bytes is smaller than the %zu bytes needed", ws_bytes, need);
   dmoe::AttnArgs a{*cache, layer, batch, n_heads, mask_block, q, q_stride, scale, plan, out, out_stride, lse, workspace};
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return hip_status(cache->dt == DMOE_BF16 ? dmoe::launch_attention_bf16(a, sh, s) : dmoe::launch_attention_f32(a, sh, s), __func__);
+  return hip_status(cache->dt == DMOE_BF16 ? attend<dmoe::bf16_t>(a, sh, s) : attend<float>(a, sh, s), __func__);
 }
 
 size_t dmoe_cache_update_workspace_size(int n, int max_pages, int n_pages) {

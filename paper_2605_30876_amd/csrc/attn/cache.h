@@ -165,6 +165,8 @@ size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads);
 size_t attn_workspace_bytes(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads, int dp);
 // Two workgroups of the block kernel fit a CU where a wave's registers fit half of a SIMD's.
 constexpr bool two_per_cu(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) <= 256; }
+// and in a cache of few bits, whose products are bf16 and whose fp32 queries take three registers for one
+constexpr bool quant_two_per_cu(dmoe_dtype dt, int dp) { return dp <= (dt == DMOE_F32 ? 64 : 128); }
 AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads);
 
 inline size_t plan_ints(const AttnShape& s) {
@@ -204,6 +206,8 @@ struct AttnArgs {
 };
 hipError_t launch_attention_bf16(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
 hipError_t launch_attention_f32(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
+// T: the rows' type; bits of keys and of values
+template <typename T, int kKB, int kVB>
 hipError_t launch_attention_quant(const AttnArgs& a, const AttnShape& sh, hipStream_t s);
 hipError_t launch_attention_plan(const dmoe_cache& c, const dmoe_batch& b, const AttnShape& sh, int mask_block,
                                  int32_t* plan, hipStream_t s);

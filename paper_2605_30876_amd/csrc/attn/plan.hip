@@ -212,12 +212,14 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   // one workgroup a CU: where a wave needs more than half of a SIMD's
   // registers, and where eight waves work on an item, which they do if the
   // batch's row tiles alone do not fill the device
-  const bool half = two_per_cu(c.dt, padded_dim(c.head_dim));
-  s.wide = half && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
+  const bool few = c.format != DMOE_KV_PLAIN;  // bits: bf16 products, whatever the rows
+  const int dp = padded_dim(c.head_dim);
+  const bool half = few ? quant_two_per_cu(c.dt, dp) : two_per_cu(c.dt, dp);
+  s.wide = !few && half && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
   if (!half || s.wide) s.aim = s.aim > 1 ? s.aim / 2 : 1;
   if (s.wide) s.min_tiles = kMinWide;
-  s.even_tiles = c.dt == DMOE_F32 ? kEvenF32 : kEvenBf16;
-  s.unit = stage_tiles(c.dt, padded_dim(c.head_dim));
+  s.even_tiles = c.dt == DMOE_F32 && !few ? kEvenF32 : kEvenBf16;
+  s.unit = stage_tiles(few ? DMOE_BF16 : c.dt, dp);
   return s;
 }
 
