@@ -1,13 +1,18 @@
 // Attention over a cache of few bits.
 //
 // The products are those of attention.h on the bf16 matrix cores: S^T = K Q^T with a
-// row to a lane, online softmax in base 2, O^T += V^T P^T.  code * scale is exact in bf16, so
-// codes become matrix operands by the conversion instructions alone, two
-// values each, the scale applied by them.  A page holds keys and values alike, token by token:
-// a lane's 16 bytes are consecutive elements of one token, which is a key operand as it is
-// (the order of a reduction's elements is free, as long as queries are loaded in the same one);
-// values are written to LDS in rows of tokens and read back turned (ds_read_b64_tr_b16:
-// four tokens of one element a lane), in the order of the registers that hold probabilities.
+// row to a lane, online softmax in base 2, O^T += V^T P^T, on tiles of 32 or 16
+// rows.  code * scale is exact in bf16, so codes become matrix operands by the
+// conversion instructions alone, two values each, the scale applied by them.  A page holds
+// keys and values alike, token by token: a lane's 16 bytes are consecutive elements of
+// one token, which is a key operand as it is (the order of a reduction's elements is free,
+// as long as queries are loaded in the same one); values are written to LDS
+// in rows of tokens and read back turned (ds_read_b64_tr_b16: four tokens of one
+// element a lane), in the order of the registers that hold probabilities.
+//
+// Not used: the matrix instructions that take codes and scales as they are.  They align a
+// product's terms to the largest and keep 12 bits below it (measured: sums of 64 off by 2^-12
+// of the largest term), where the bf16 ones keep float32's.
 //
 // fp32 rows: queries and probabilities are cut into three bf16 parts of eight bits, which hold
 // them exactly, and multiplied one after another: three bf16 products take 96 cycles where
@@ -25,6 +30,7 @@ using quant::scale_of;
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // bf16 parts of a row's queries and probabilities.
 template <typename T>
@@ -40,9 +46,10 @@ __device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&f)[3]) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const uint32_t u = __float_as_uint(x[2 * i + e]), hi = u & 0xffff0000u;
-      const float r = (u & 0x7f800000u) == 0x7f800000u ? 0.f : x[2 * i + e] - __uint_as_float(hi);
+      const bool finite = (u & 0x7f800000u) != 0x7f800000u;
+      const float r = finite ? x[2 * i + e] - __uint_as_float(hi) : 0.f;
       const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
-      a[e][0] = hi | ((u & 0x7f800000u) == 0x7f800000u && (u & 0xffffu) ? 0x10000u : 0u);
+      a[e][0] = hi | (!finite && (u & 0xffffu) ? 0x10000u : 0u);  // a NaN stays one
       a[e][1] = mid;
       a[e][2] = __float_as_uint(r - __uint_as_float(mid));
     }
@@ -53,63 +60,67 @@ __device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&f)[3]) {
   for (int p = 0; p < 3; ++p) f[p] = __builtin_bit_cast(bf16x8, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
 }
 
-// A token's scale bytes.
-template <int DP>
-struct Scales {
-  uint32_t w[DP > 128 ? 2 : 1];
-  __device__ __forceinline__ void load(const uint8_t* p) {
-    if constexpr (scale_row(DP) == 1)
-      w[0] = *p;
-    else if constexpr (scale_row(DP) == 2)
-      w[0] = *reinterpret_cast<const uint16_t*>(p);
-    else if constexpr (scale_row(DP) == 4)
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
-    else {
-      const uint2 x = *reinterpret_cast<const uint2*>(p);
-      w[0] = x.x;
-      w[1] = x.y;
-    }
-  }
-  // of group g, or of group g + 1 in the second half of the wave
-  __device__ __forceinline__ float of(int g) const { return scale_of(w[g / 4] >> (8 * (g % 4)) & 255u); }
-  __device__ __forceinline__ float of_two(int g, int half) const { return scale_of(w[g / 4] >> (8 * (g % 4) + 8 * half) & 255u); }
-};
-
-// A tile's keys (or values) as a wave loads them: load j of a lane (token lane % 32, half
-// lane / 32) is the token's chunk 2j + half.
-template <int DP, int kBits>
-struct TileCodes {
-  static constexpr int kChunks = DP * kBits / 128;      // of a token
-  static constexpr int kLoads = (kChunks + 1) / 2;      // the last of an odd number: only the first half has one
-  static constexpr int kPer = 16 / kBits;               // operands of a load: 8 elements each
-  u32x4 c[kLoads];
-  Scales<DP> s;
-  template <bool kStream>
-  __device__ __forceinline__ void load(const uint8_t* tile, int lane) {
+// Codes and scale bytes of a token that nobody sees become 0; false if what is left is perhaps not finite.
+template <int kBits, int kN>
+__device__ __forceinline__ bool cut_codes(u32x4 (&c)[kN], uint8_t (&s)[kN], int i, bool seen) {
+  bool finite = s[i] <= quant::kHighest<kBits>;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      if (2 * j + 1 < kChunks || lane < 32) {
-        const u32x4* p = reinterpret_cast<const u32x4*>(tile + (j * 64 + lane) * 16);
-        c[j] = kStream ? __builtin_nontemporal_load(p) : *p;
+  for (int x = 0; x < 4; ++x) {
+    // 8 bits: 0x7f is NaN
+    if constexpr (kBits == 8) finite = finite && (((c[i][x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) == 0;
+    c[i][x] = seen ? c[i][x] : 0;
+  }
+  s[i] = seen ? s[i] : 127;
+  return finite || !seen;
+}
+
+// A token's codes as the kG lanes that share it load them: pieces of 16 bytes a lane, then of
+// 8 and 4 where the rest is less.  Piece i of lane group g is kBytes(i) bytes from at(i) + g * kBytes(i) on.
+template <int DP, int kBits, int kG>
+struct LaneCodes {
+  static constexpr int kRow = DP * kBits / 8;                        // bytes of a token
+  static constexpr int kFull = kRow / (16 * kG), kRest = kRow % (16 * kG);
+  static constexpr int kPieces = kFull + (kRest >= 8 * kG) + (kRest % (8 * kG) >= 4 * kG);
+  static __host__ __device__ constexpr int bytes(int i) { return i < kFull ? 16 : i == kFull && kRest >= 8 * kG ? 8 : 4; }
+  static __host__ __device__ constexpr int at(int i) {
+    return i <= kFull ? i * 16 * kG : kFull * 16 * kG + 8 * kG;
+  }
+  static __host__ __device__ constexpr int operands(int i) { return bytes(i) / kBits; }  // of 8 elements
+  static __host__ __device__ constexpr int first(int i) { return at(i) / (kG * kBits); }  // operands before piece i
+  static constexpr int kOperands = kRow / (kG * kBits);
+  // first element of operand o of piece i
+  static __host__ __device__ constexpr int element(int i, int o, int g) { return (at(i) + g * bytes(i)) * 8 / kBits + 8 * o; }
+
+  u32x4 c[kPieces];
+  uint8_t s[kPieces];  // scale bytes
+  template <bool kStream>
+  __device__ __forceinline__ void load(const uint8_t* tile, int r, int g) {
+    auto get = [](const auto* p) { return kStream ? __builtin_nontemporal_load(p) : *p; };
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = at(i) + g * bytes(i);
+      const uint8_t* p = tile + (x / 16 * kTileTokens + r) * 16 + x % 16;
+      if (bytes(i) == 16) {
+        c[i] = get(reinterpret_cast<const u32x4*>(p));
+      } else if (bytes(i) == 8) {
+        const u32x2 w = get(reinterpret_cast<const u32x2*>(p));
+        c[i] = u32x4{w[0], w[1], 0, 0};
       } else {
-        c[j] = u32x4{0, 0, 0, 0};
+        c[i] = u32x4{get(reinterpret_cast<const uint32_t*>(p)), 0, 0, 0};
       }
+      s[i] = tile[scale_at<kBits>(DP, r) + x * 8 / kBits / kGroup];
     }
-    s.load(tile + scale_at<kBits>(DP, lane & 31));
   }
-  __device__ __forceinline__ float scale(int j, int half) const {
-    if constexpr (kBits == 8) return s.of(j);
-    // an odd number of groups: there is nothing in the second half, and codes of 0 at any finite scale
-    if (2 * j + 1 >= kChunks) return half ? 1.f : s.of(2 * j);
-    return s.of_two(2 * j, half);
-  }
-  // operand o of load j
-  __device__ __forceinline__ bf16x8 operand(int j, int o, float scale) const {
-    const uint32_t w[2] = {c[j][o * kBits / 4], c[j][kBits == 8 ? 2 * o + 1 : o]};
+  __device__ __forceinline__ bf16x8 operand(int i, int o, float scale) const {
+    const uint32_t w[2] = {c[i][o * kBits / 4], c[i][kBits == 8 ? 2 * o + 1 : o]};
     return decode<kBits>(w, scale);
   }
-  // first element of a lane's operand o of load j
-  static __device__ __forceinline__ int element(int j, int o, int half) { return (128 / kBits) * (2 * j + half) + 8 * o; }
+  __device__ __forceinline__ bool cut(bool seen) {
+    bool finite = true;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) finite = cut_codes<kBits>(c, s, i, seen) && finite;
+    return finite;
+  }
 };
 
 // Values of a tile in LDS: 32 rows of tokens, kRow bytes apart.  Rows of four tokens lie in
@@ -122,20 +133,32 @@ struct TurnedValues {
   static constexpr int kBytes = kTileTokens * kRow;
   static __device__ __forceinline__ int piece(int r, int p) { return r * kRow + (p ^ (r >> 2 & 3)) * 16; }
   static __device__ __forceinline__ void write(char* lds, int r, int p, const bf16x8& x) { *reinterpret_cast<bf16x8*>(lds + piece(r, p)) = x; }
-  // Where a lane's pieces of 4 tokens x 16 elements start: within a group of 16 lanes, lane i points at
-  // token i / 4, elements 4 (i % 4) on, and receives element i of the four tokens.
+};
+
+// Reads of values turned, for results of kR rows: operand s of block b, element 4j + t of lane (element d = lane % kR of
+// the block, group g = lane / kR), is token 4G (2s + j) + 4g + t, G = 64 / kR.  Within 16 lanes, lane i
+// points at token i / 4 of four, elements 4 (i % 4) on, and receives element i of the four tokens.
+template <int DP, int kR>
+struct TurnedRead {
+  static constexpr int kG = 64 / kR, kRow = TurnedValues<DP>::kRow;
   int at[2];
-  __device__ __forceinline__ TurnedValues(int lane) {
-    const int half = lane >> 5, i = lane & 15, p = (lane >> 4 & 1) * 2 + (i & 3) / 2;
+  __device__ __forceinline__ TurnedRead(int lane) {
+    const int g = lane / kR, i = lane & 15, p = (kR == 32 ? (lane >> 4 & 1) * 2 : 0) + (i & 3) / 2;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) at[j] = (8 * j + 4 * half + i / 4) * kRow + (p ^ ((2 * j + half) & 3)) * 16 + (i & 1) * 8;
+    for (int j = 0; j < 2; ++j) {
+      const int t = 4 * kG * j + 4 * g;  // the first of the four tokens
+      at[j] = (t + i / 4) * kRow + (p ^ (t >> 2 & 3)) * 16 + (i & 1) * 8;
+    }
   }
-  // tokens 16s + 8j + 4 half + t (element 4j + t) of element 32b + lane % 32
   __device__ __forceinline__ bf16x8 read(const char* lds, int b, int s) const {
     bf16x4 x[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(lds + at[j] + s * (16 * kRow) + b * 64));
+    for (int j = 0; j < 2; ++j) {
+      // 16 elements on are two pieces on: with pieces that change places, another bit of the place
+      const int a = kR == 16 && (b & 1) ? at[j] ^ 32 : at[j];
+      x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+          (__attribute__((address_space(3))) bf16x4*)(lds + a + s * (8 * kG * kRow) + b * kR / 32 * 64));
+    }
     return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
@@ -144,13 +167,43 @@ struct TurnedValues {
 // instructions act in their order.
 __device__ __forceinline__ void lds_order() { asm volatile("" ::: "memory"); }
 
-// A wave's 32 rows: WaveRows' sums and softmax, with queries in kK operands of parts.
-template <typename T, int DP, int kK>
-struct QuantRows : WaveRows<bf16_t, DP> {
-  typedef WaveRows<bf16_t, DP> Base;
-  typedef Types<bf16_t> Ty;
-  static constexpr int kB = Base::kB, kS = Base::kS, kP = kParts<T>;
+template <int kG>
+__device__ __forceinline__ float groups_max(float v) {
+  if constexpr (kG == 4) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  }
+  return other_half_max(v);
+}
+template <int kG>
+__device__ __forceinline__ float groups_sum(float v) {
+  if constexpr (kG == 4) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  return other_half_sum(v);
+}
+
+// A wave's kR rows (lane % kR) against tiles of 32 keys.  Group g = lane / kR of the wave holds keys 4G (i / 4) + 4g +
+// i % 4 in register i of a tile's scores, G = 64 / kR, and elements kR b + 4G (i / 4) + 4g + i % 4 in register i of block b of
+// the sums.
+template <typename T, int DP, int kR, bool kPin>
+struct QuantRows {
+  static constexpr int kG = 64 / kR, kP = kParts<T>;
+  static constexpr int kK = DP / (8 * kG);  // operands of a token's keys: 8 elements of every group
+  static constexpr int kS = 4 / kG;         // operands of a tile's values
+  static constexpr int kB = DP / kR;        // blocks of the output
+  static constexpr int kN = 32 / kG;        // scores of a tile in a lane
+  static constexpr int kO = kR * kR / 64;   // registers of a block
+  typedef float Sums __attribute__((ext_vector_type(kO)));
   bf16x8 q[kP][kK];
+  Sums o[kB];
+  float m, l;  // l: of this group's keys
+  int end;     // keys the row sees
+  int lo, hi;  // the least and most of the wave's rows (uniform)
+
+  static __device__ __forceinline__ constexpr int key(int i, int g) { return 4 * kG * (i / 4) + 4 * g + i % 4; }
+  static __device__ __forceinline__ constexpr int element(int b, int i, int g) { return kR * b + key(i, g); }
 
   // element(j): the first element of operand j
   template <typename Place, typename F>
@@ -178,15 +231,83 @@ struct QuantRows : WaveRows<bf16_t, DP> {
       }
     }
   }
-  __device__ __forceinline__ void score(f32x16& s, const bf16x8& k, int j) const {
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < kO; ++i) o[b][i] = 0.f;
+  }
+  // WaveRows::pin
+  __device__ __forceinline__ void pin() {
+    if constexpr (kPin) {
+#pragma unroll
+      for (int b = 0; b < kB; ++b) asm volatile("" : "+a"(o[b]));
+    }
+  }
+  static __device__ __forceinline__ void mma(Sums& acc, const bf16x8& a, const bf16x8& b) {
+    if constexpr (kR == 32)
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+    else
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+  }
+  // operand j of keys kR x .. kR x + kR - 1 of a tile
+  __device__ __forceinline__ void score(float (&s)[kN], int x, const bf16x8& k, int j) const {
+    Sums acc;
+#pragma unroll
+    for (int i = 0; i < kO; ++i) acc[i] = s[kO * x + i];
     // smallest parts first
 #pragma unroll
-    for (int p = kP - 1; p >= 0; --p) Ty::mma(s, k, q[p][j]);
+    for (int p = kP - 1; p >= 0; --p) mma(acc, k, q[p][j]);
+#pragma unroll
+    for (int i = 0; i < kO; ++i) s[kO * x + i] = acc[i];
+  }
+  // WaveRows::softmax; the groups' maxima meet only where one of them has to be raised.  masked: keys of tile n from
+  // seen[n] on are not seen.
+  template <int NT>
+  __device__ __forceinline__ void softmax(float (&s)[NT][kN], float scale2, bool masked, const int (&seen)[NT], int g) {
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) s[n][i] = key(i, g) < seen[n] ? s[n][i] : -INFINITY;
+    }
+    float t = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) t = fmaxf(t, s[n][i]);
+    t *= scale2;
+    pin();
+    if (__any(t > m + kLazy)) {
+      const float nm = fmaxf(m, groups_max<kG>(t));
+      const float a = nm == m ? 1.f : exp2_hw(m - nm);
+      m = nm;
+      scale(a);
+    }
+    pin();
+    const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        s[n][i] = exp2_hw(__builtin_fmaf(s[n][i], scale2, -off));
+        l += s[n][i];
+      }
+  }
+  __device__ __forceinline__ void scale(float fac) {
+    l *= fac;
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < kO; ++i) o[b][i] *= fac;
   }
   // probabilities of operand s of a tile's values
-  static __device__ __forceinline__ void probs(const f32x16& p, int s, bf16x8 (&f)[kP]) {
+  static __device__ __forceinline__ void probs(const float (&p)[kN], int s, bf16x8 (&f)[kP]) {
     if constexpr (kP == 1) {
-      f[0] = Ty::probs(p, s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[0][i] = static_cast<__bf16>(p[8 * s + i]);
     } else {
       float x[8];
 #pragma unroll
@@ -195,7 +316,7 @@ struct QuantRows : WaveRows<bf16_t, DP> {
     }
   }
   template <typename F>
-  __device__ __forceinline__ void add(const f32x16& p, F value) {
+  __device__ __forceinline__ void add(const float (&p)[kN], F value) {
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       bf16x8 f[kP];
@@ -204,35 +325,86 @@ struct QuantRows : WaveRows<bf16_t, DP> {
       for (int b = 0; b < kB; ++b) {
         const bf16x8 v = value(b, s);
 #pragma unroll
-        for (int x = kP - 1; x >= 0; --x) Ty::mma(this->o[b], v, f[x]);
+        for (int x = kP - 1; x >= 0; --x) mma(o[b], v, f[x]);
       }
     }
   }
-  // Base::add_keys with parts
-  __device__ __forceinline__ void add_keys(const f32x16& p, const bf16x8 (&v)[kB][kS], int key0, int half) {
+  // WaveRows::add_keys: a key's products are added to the rows that see it
+  __device__ __forceinline__ void add_keys(const float (&p)[kN], const bf16x8 (&v)[kB][kS], int key0, int g) {
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       bf16x8 f[kP];
       probs(p, s, f);
 #pragma unroll 1
-      for (int r = 0; r < 16; ++r) {
-        const bool mine = (r >> 2 & 1) == half;
-        const int slot = mine ? (r >> 3) * 4 + (r & 3) : -1;
-        const bool sees = key0 + 16 * s + r < this->end;
+      for (int r = 0; r < 8 * kG; ++r) {
+        const int slot = r / 4 % kG == g ? r / (4 * kG) * 4 + r % 4 : -1;
+        const bool sees = key0 + 8 * kG * s + r < end;
 #pragma unroll
         for (int b = 0; b < kB; ++b) {
-          const bf16x8 x = Base::only(v[b][s], slot);
-          f32x16 t;
+          const bf16x8 x = WaveRows<bf16_t, 32>::only(v[b][s], slot);
+          Sums t;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) t[i] = 0.f;
+          for (int i = 0; i < kO; ++i) t[i] = 0.f;
 #pragma unroll
-          for (int y = kP - 1; y >= 0; --y) Ty::mma(t, x, Base::only(f[y], slot));
+          for (int y = kP - 1; y >= 0; --y) mma(t, x, WaveRows<bf16_t, 32>::only(f[y], slot));
 #pragma unroll
-          for (int i = 0; i < 16; ++i) this->o[b][i] += sees ? t[i] : 0.f;
+          for (int i = 0; i < kO; ++i) o[b][i] += sees ? t[i] : 0.f;
           __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
+  }
+};
+
+// The item's rows of a wave, kR of them: as RowPlace.
+template <typename T, int DP, int kR>
+struct QuantPlace {
+  int row, tok, qh;
+  bool live, any;
+  template <typename Rows>
+  __device__ __forceinline__ QuantPlace(Rows& w, const AttnArgs& a, const AttnItem& it, int g, int hk, int row_lo, int lane) {
+    const int row_hi = min(row_lo + kR, it.rows) - 1;
+    const int pos0 = it.len - it.n;
+    row = row_lo + lane % kR;
+    live = row < it.rows;
+    any = row_hi >= row_lo;
+    tok = live ? row / g : 0;
+    qh = hk * g + (live ? row - tok * g : 0);
+    w.end = live ? visible_end(pos0 + tok, it.len, a.mask_block) : 0;
+    w.lo = any ? visible_end(pos0 + row_lo / g, it.len, a.mask_block) : 0;
+    w.hi = any ? visible_end(pos0 + row_hi / g, it.len, a.mask_block) : 0;
+  }
+  __device__ __forceinline__ const T* query(const AttnArgs& a, const AttnItem& it) const {
+    return static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
+  }
+  template <typename Rows>
+  __device__ __forceinline__ void store(const Rows& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk,
+                                        int group, int part_rows) const {
+    if (!live) return;
+    if (it.part >= 0) {
+      const long at = (static_cast<long>(it.part) * a.cache.n_kv_heads + hk) * sh.tile_rows + (row - it.first);
+      float* po = static_cast<float*>(a.workspace) + (at - (row - it.first)) * DP;
+#pragma unroll
+      for (int b = 0; b < Rows::kB; ++b)
+#pragma unroll
+        for (int i = 0; i < Rows::kO; i += 4)
+          store4(po + partial_at(DP, row - it.first, Rows::element(b, i, group)), f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
+      if (group == 0)
+        *reinterpret_cast<float2*>(static_cast<float*>(a.workspace) + static_cast<long>(part_rows) * DP + at * 2) = make_float2(w.m, w.l);
+      return;
+    }
+    const bool some = w.l > 0.f || w.l != w.l;
+    const float inv = some ? 1.f / w.l : 0.f;
+    T* op = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim;
+#pragma unroll
+    for (int b = 0; b < Rows::kB; ++b)
+#pragma unroll
+      for (int i = 0; i < Rows::kO; i += 4) {
+        const int d = Rows::element(b, i, group);
+        if (d < a.cache.head_dim) store4(op + d, f32x4{w.o[b][i] * inv, w.o[b][i + 1] * inv, w.o[b][i + 2] * inv, w.o[b][i + 3] * inv});
+      }
+    if (a.lse && group == 0)
+      a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = some ? (w.m + log2f(w.l)) * kLn2 : -INFINITY;
   }
 };
 
@@ -255,36 +427,62 @@ struct QuantMap {
   }
   __device__ __forceinline__ int page(int kt, int end) const { return kt < end ? table[shift >= 0 ? kt >> shift : kt / -shift] : -1; }
   __device__ __forceinline__ bool holds(int page) const { return static_cast<unsigned>(page) < static_cast<unsigned>(n_pages); }
-  // tiles from k and v to a tile on a page that is held
+  // tiles from k and v to a tile on a page; of no page: some tile of the pool
   __device__ __forceinline__ long at(int kt, int page) const {
-    return (layer0 + page) * per_page + (shift >= 0 ? kt & ((1 << shift) - 1) : kt % -shift);
+    return (layer0 + (holds(page) ? page : 0)) * per_page + (shift >= 0 ? kt & ((1 << shift) - 1) : kt % -shift);
   }
   __device__ __forceinline__ const uint8_t* key(long tile) const { return k + tile * kKTile; }
   __device__ __forceinline__ const uint8_t* value(long tile) const { return v + tile * kVTile; }
 };
 
-// A tile's values, loaded by this wave, through its LDS.
-template <int DP, int kVB>
-__device__ __forceinline__ void turn_values(const TileCodes<DP, kVB>& c, char* lds, int lane) {
-  typedef TileCodes<DP, kVB> Codes;
-  const int half = lane >> 5, r = lane & 31;
-  lds_order();
+// A tile's codes in a wave's registers: keys by kR tokens, values by 32.
+template <int DP, int kKB, int kVB, int kR>
+struct WaveTile {
+  typedef LaneCodes<DP, kKB, 64 / kR> Keys;
+  typedef LaneCodes<DP, kVB, 2> Values;
+  Keys k[32 / kR];
+  Values v;
+  template <bool kStream>
+  __device__ __forceinline__ void load_keys(const uint8_t* tile, int lane) {
 #pragma unroll
-  for (int j = 0; j < Codes::kLoads; ++j) {
-    const float scale = c.scale(j, half);
-    if (2 * j + 1 < Codes::kChunks || lane < 32) {
-#pragma unroll
-      for (int o = 0; o < Codes::kPer; ++o)
-        TurnedValues<DP>::write(lds, r, (2 * j + half) * Codes::kPer + o, c.operand(j, o, scale));
-    }
+    for (int x = 0; x < 32 / kR; ++x) k[x].template load<kStream>(tile, kR * x + lane % kR, lane / kR);
   }
-  lds_order();
-}
+  template <bool kStream>
+  __device__ __forceinline__ void load_values(const uint8_t* tile, int lane) {
+    v.template load<kStream>(tile, lane % 32, lane / 32);
+  }
+  template <typename Rows>
+  __device__ __forceinline__ void scores(const Rows& w, float (&s)[Rows::kN]) const {
+#pragma unroll
+    for (int i = 0; i < Rows::kN; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < Keys::kPieces; ++i)
+#pragma unroll
+      for (int x = 0; x < 32 / kR; ++x) {
+        const float scale = scale_of(k[x].s[i]);
+#pragma unroll
+        for (int o = 0; o < Keys::operands(i); ++o) w.score(s, x, k[x].operand(i, o, scale), Keys::first(i) + o);
+      }
+  }
+  // the values to this wave's place in LDS
+  __device__ __forceinline__ void open_values(char* lds, int lane) const {
+    lds_order();
+#pragma unroll
+    for (int i = 0; i < Values::kPieces; ++i) {
+      const float scale = scale_of(v.s[i]);
+      const int p = Values::element(i, 0, lane / 32) / 8;
+#pragma unroll
+      for (int o = 0; o < Values::operands(i); ++o) TurnedValues<DP>::write(lds, lane % 32, p + o, v.operand(i, o, scale));
+    }
+    lds_order();
+  }
+};
 
-// Tiles of a masked stretch that hold values that are not finite, once the running maximum is the last one (WaveRows::add_by_key).
-template <typename Rows, typename Map, int DP, int kKB, int kVB, typename Element>
-__device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int kt1, int step, float scale2, int lane, char* lds, Element query_operand) {
-  const int half = lane >> 5;
+// Tiles of a masked stretch that hold values that are not finite, once the running maximum is the last one
+// (WaveRows::add_by_key).  scores(s, keys): a tile's scores.
+template <int DP, int kKB, int kVB, int kR, typename Rows, typename Map, typename Scores>
+__device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int kt1, int step, float scale2, int lane, char* lds, Scores scores) {
+  const int g = lane / kR;
 #pragma unroll 1
   for (; kt < kt1; kt += step) {
     const int page = map.page(kt, kt1), key0 = kt * kTileTokens;
@@ -292,135 +490,170 @@ __device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int 
     const long at = map.at(kt, page);
     bf16x8 v[Rows::kB][Rows::kS];
     {
-      TileCodes<DP, kVB> vc;
-      vc.template load<false>(map.value(at), lane);
-      turn_values<DP, kVB>(vc, lds, lane);
-      const TurnedValues<DP> turned(lane);
+      WaveTile<DP, kKB, kVB, kR> t;
+      t.template load_values<false>(map.value(at), lane);
+      if (__all(t.v.cut(lane % 32 < w.hi - key0))) continue;
+      t.open_values(lds, lane);
+      const TurnedRead<DP, kR> turned(lane);
 #pragma unroll
       for (int b = 0; b < Rows::kB; ++b)
 #pragma unroll
         for (int s = 0; s < Rows::kS; ++s) v[b][s] = turned.read(lds, b, s);
     }
-    if (w.cut(v, key0, half)) continue;
-    f32x16 s;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
-    query_operand(s, map.key(at));
+    float s[Rows::kN];
+    scores(s, map.key(at));
     const float off = w.m == -INFINITY ? 0.f : w.m;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = tile_key(i, half) < w.end - key0 ? exp2_hw(__builtin_fmaf(s[i], scale2, -off)) : 0.f;
-    w.add_keys(s, v, key0, half);
+    for (int i = 0; i < Rows::kN; ++i) s[i] = Rows::key(i, g) < w.end - key0 ? exp2_hw(__builtin_fmaf(s[i], scale2, -off)) : 0.f;
+    w.add_keys(s, v, key0, g);
   }
 }
 
-template <typename T>
-constexpr int quant_waves(int dp) {
-  return quant_two_per_cu(sizeof(T) == 4 ? DMOE_F32 : DMOE_BF16, dp) ? 2 : 1;
+// kWK waves' sums over different keys joined: join_waves.
+template <int kWK, typename Rows>
+__device__ __forceinline__ void join_quant(Rows& w, float* lds, int first, int wk, int lane) {
+  constexpr int kLen = (Rows::kO * Rows::kB + 2) * 64;
+#pragma unroll
+  for (int n = kWK / 2; n >= 1; n /= 2) {
+    float* buf = lds + (first + wk % n) * kLen;
+    if (wk >= n && wk < 2 * n) {
+      buf[lane] = w.m;
+      buf[64 + lane] = w.l;
+#pragma unroll
+      for (int b = 0; b < Rows::kB; ++b)
+#pragma unroll
+        for (int i = 0; i < Rows::kO; i += 4)
+          store4(buf + 128 + (Rows::kO / 4 * b + i / 4) * 256 + lane * 4, f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
+    }
+    __syncthreads();
+    if (wk < n) {
+      const float om = buf[lane], ol = buf[64 + lane];
+      const float nm = fmaxf(w.m, om);
+      const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = om == nm ? 1.f : exp2_hw(om - nm);
+      w.scale(fa);
+      w.m = nm;
+      w.l += fb * ol;
+#pragma unroll
+      for (int b = 0; b < Rows::kB; ++b)
+#pragma unroll
+        for (int i = 0; i < Rows::kO; i += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 128 + (Rows::kO / 4 * b + i / 4) * 256 + lane * 4);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
+        }
+    }
+    __syncthreads();
+  }
 }
 
-// Few rows: attention_rows_kernel's split of the work (32 kWR rows of one kv head per workgroup, 4 / kWR waves to 32 of
-// them, each on every (4 / kWR)-th key tile), the codes of the next tile on their way while one is used.
-template <typename T, int DP, int kKB, int kVB, int kWR>
-__global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
-  typedef TileCodes<DP, kKB> KCodes;
-  typedef TileCodes<DP, kVB> VCodes;
-  typedef QuantRows<T, DP, KCodes::kLoads * KCodes::kPer> Rows;
-  constexpr int kB = Rows::kB, kS = Rows::kS, kWK = 4 / kWR;
+// Registers of a tile's codes in a lane, and tiles on their way: as many as keep the memory busy.
+template <int DP, int kKB, int kVB>
+constexpr int tile_regs = DP * (kKB + kVB) / 64 + 4;
+template <int DP, int kKB, int kVB>
+constexpr int tiles_ahead = tile_regs<DP, kKB, kVB> <= 24 ? 3 : tile_regs<DP, kKB, kVB> <= 48 ? 2 : 1;
+// Waves of a SIMD: what queries, sums, codes and the rest of a wave leave room for.
+template <typename T, int DP, int kKB, int kVB, int kR>
+constexpr int rows_regs = kParts<T> * DP * kR / 128 + DP * kR / 64 + tiles_ahead<DP, kKB, kVB> * tile_regs<DP, kKB, kVB> + kR / 2 + 64;
+template <typename T, int DP, int kKB, int kVB, int kR>
+constexpr int rows_waves = rows_regs<T, DP, kKB, kVB, kR> <= 168 ? 3 : rows_regs<T, DP, kKB, kVB, kR> <= 256 ? 2 : 1;
+
+// Few rows: kR kWR of one kv head per workgroup, kR to a wave, 4 / kWR waves to the same ones, each on every (4 / kWR)-th
+// key tile, joined through LDS.  Codes go straight into registers, the next tiles' while one is used: loads are
+// straight-line code, so that waiting for a tile does not wait for those behind it.
+template <typename T, int DP, int kKB, int kVB, int kR, int kWR>
+__global__ __launch_bounds__(256, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+  constexpr bool kPin = rows_waves<T, DP, kKB, kVB, kR> == 1;
+  typedef QuantRows<T, DP, kR, kPin> Rows;
+  typedef WaveTile<DP, kKB, kVB, kR> Tile;
+  typedef typename Tile::Keys Keys;
+  constexpr int kWK = 4 / kWR, kAhead = tiles_ahead<DP, kKB, kVB>;
   constexpr bool kStream = kWR == 1;
   extern __shared__ float lds[];
   const int hkv = a.cache.n_kv_heads;
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
   AttnItem it;
   if (!load_item(a, item_i, it)) return;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int lane = threadIdx.x & 63, g = lane / kR;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % kWK, wr = wave / kWK;
   char* mine = reinterpret_cast<char*>(lds) + wave * TurnedValues<DP>::kBytes;
-  const TurnedValues<DP> turned(lane);
+  const TurnedRead<DP, kR> turned(lane);
   Rows w;
   w.clear();
-  const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wr, lane);
-  w.load(rows, a, it, [&](int j) { return KCodes::element(j / KCodes::kPer, j % KCodes::kPer, half); });
+  const QuantPlace<T, DP, kR> rows(w, a, it, sh.group, hk, it.first + kR * wr, lane);
   const float scale2 = a.scale * kLog2e;
   const QuantMap<DP, kKB, kVB> map(a, it.slot, hk);
   const int kt1 = min(it.kt1, (w.hi + kTileTokens - 1) / kTileTokens);
-  KCodes kc;
-  VCodes vc;
-  auto scores = [&](f32x16& s, const KCodes& c) {
-#pragma unroll
-    for (int j = 0; j < KCodes::kLoads; ++j) {
-      const float scale = c.scale(j, half);
-#pragma unroll
-      for (int o = 0; o < KCodes::kPer; ++o) w.score(s, c.operand(j, o, scale), j * KCodes::kPer + o);
-    }
-  };
-  // page ids are known two of this wave's tiles ahead, its keys and values one
+  Tile tile[kAhead];
+  // pages of the tiles on their way, and of the one after them
   int kt = it.kt0 + wk;
-  int page = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
-  int page1 = map.page(kt + kWK, kt1);
-  auto first = [&] {
-    if (!map.holds(page)) return;
-    const long at = map.at(kt, page);
-    kc.template load<kStream>(map.key(at), lane);
-    vc.template load<kStream>(map.value(at), lane);
+  int page[kAhead + 1];
+  auto fetch = [&](Tile& t, int at_kt, int pg) {
+    const long at = map.at(at_kt, pg);
+    t.template load_keys<kStream>(map.key(at), lane);
+    t.template load_values<kStream>(map.value(at), lane);
   };
-  first();
-  if (const int now = map.page(kt, kt1); now != page) {  // moved since the plan was made
-    page = now;
-    first();
+  page[0] = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
+  fetch(tile[0], kt, page[0]);
+  const int now = map.page(kt, kt1);
+#pragma unroll
+  for (int i = 1; i <= kAhead; ++i) page[i] = map.page(kt + i * kWK, kt1);
+  w.load(rows, a, it, [&](int j) {
+    int d = 0;
+#pragma unroll
+    for (int i = 0; i < Keys::kPieces; ++i)
+      if (j >= Keys::first(i)) d = Keys::element(i, j - Keys::first(i), g);
+    return d;
+  });
+#pragma unroll
+  for (int i = 1; i < kAhead; ++i) fetch(tile[i], kt + i * kWK, page[i]);
+  if (now != page[0]) {  // moved since the plan was made
+    page[0] = now;
+    fetch(tile[0], kt, now);
   }
-  bool left = false;  // tiles for add_by_key
-  auto turn = [&](auto masked) {
+  // tiles that every row sees whole come first
+  const int whole = min(kt1, w.lo / kTileTokens);
+  int left = kt1;  // the first tile for add_by_key
+  auto turn = [&](Tile& t) {
     w.pin();
-    const int page2 = map.page(kt + 2 * kWK, kt1);
-    const bool here = map.holds(page), more = map.holds(page1);
-    const long at1 = more ? map.at(kt + kWK, page1) : 0;
-    f32x16 s[1];
-    if (here) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
-      scores(s[0], kc);
-    }
-    if (more) kc.template load<kStream>(map.key(at1), lane);
-    if (here) turn_values<DP, kVB>(vc, mine, lane);
-    if (more) vc.template load<kStream>(map.value(at1), lane);
-    if (here) {
-      const int key0 = kt * kTileTokens;
-      w.template softmax<1>(s, scale2, key0, masked, half);
-      if constexpr (!masked) {
+    const int after = map.page(kt + (kAhead + 1) * kWK, kt1);
+    const int key0 = kt * kTileTokens;
+    const bool masked = kt >= whole;
+    bool finite = true;
+    if (masked) finite = __all(t.v.cut(lane % 32 < w.hi - key0));
+    float s[1][Rows::kN];
+    t.scores(w, s[0]);
+    t.open_values(mine, lane);
+    fetch(t, kt + kAhead * kWK, page[kAhead]);
+    if (map.holds(page[0])) {
+      const int seen[1] = {w.end - key0};
+      w.template softmax<1>(s, scale2, masked, seen, g);
+      // a value that is not finite must not reach the rows that do not see it
+      if (finite)
         w.add(s[0], [&](int b, int x) { return turned.read(mine, b, x); });
-      } else {
-        bf16x8 v[kB][kS];
-#pragma unroll
-        for (int b = 0; b < kB; ++b)
-#pragma unroll
-          for (int x = 0; x < kS; ++x) v[b][x] = turned.read(mine, b, x);
-        if (w.cut(v, key0, half))
-          w.add(s[0], [&](int b, int x) { return v[b][x]; });
-        else
-          left = true;
-      }
+      else
+        left = min(left, kt);
     }
     kt += kWK;
-    page = page1;
-    page1 = page2;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) page[i] = page[i + 1];
+    page[kAhead] = after;
   };
-  // tiles that every row sees whole, then the others
-  const int whole = min(kt1, w.lo / kTileTokens);
-  while (kt < whole) turn(std::false_type());
+  while (kt < kt1) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i == 0 || kt < kt1) turn(tile[i]);
+  }
   w.pin();
-  const int first_masked = kt;
-  while (kt < kt1) turn(std::true_type());
-  w.pin();
-  if (left)
-    add_by_key<Rows, QuantMap<DP, kKB, kVB>, DP, kKB, kVB>(w, map, first_masked, kt1, kWK, scale2, lane, mine, [&](f32x16& s, const uint8_t* p) {
-      KCodes c;
-      c.template load<false>(p, lane);
-      scores(s, c);
+  if (left < kt1)
+    add_by_key<DP, kKB, kVB, kR>(w, map, left, kt1, kWK, scale2, lane, mine, [&](float (&s)[Rows::kN], const uint8_t* p) {
+      Tile t;
+      t.template load_keys<false>(p, lane);
+      t.scores(w, s);
     });
-  w.l = other_half_sum(w.l);
-  if constexpr (kWK > 1) __syncthreads();  // the values' places are taken by the sums
-  join_waves<kWK, kB>(w, lds, wr * (kWK / 2), wk, lane);
-  if (wk == 0) rows.store(w, a, sh, it, hk, half, part_rows);
+  w.l = groups_sum<Rows::kG>(w.l);
+  __syncthreads();  // the values' places are taken by the sums
+  join_quant<kWK>(w, lds, wr * (kWK / 2), wk, lane);
+  if (wk == 0) rows.store(w, a, sh, it, hk, g, part_rows);
 }
 
 // Keys and values of kTS tiles in LDS: keys as operands, element 16j + 8 half + e of
@@ -430,6 +663,7 @@ struct QuantStage {
   static constexpr int kTS = stage_tiles(DMOE_BF16, DP), kK = DP / 16;
   bf16x8 k[kTS][kK][64];
   char v[kTS][TurnedValues<DP>::kBytes];
+  int bad[4];  // the tile whose values are perhaps not all finite, where rows see some of them and not others
   char more[kTS == 1 ? TurnedValues<DP>::kBytes - DP * 64 : 64];  // the two stages hold a tile's values of four waves
 };
 
@@ -442,7 +676,7 @@ struct StageCodes {
   static __device__ __forceinline__ bool has(int i) { return kUnits % 256 == 0 || static_cast<int>(threadIdx.x) + 256 * i < kUnits; }
   static __device__ __forceinline__ int tile(int i) { return (threadIdx.x + 256 * i) / (kChunks * kTileTokens); }
   static __device__ __forceinline__ int chunk(int i) { return (threadIdx.x + 256 * i) / kTileTokens % kChunks; }
-  // base[n]: where tile n lies, or nullptr
+  // base[n]: where tile n lies
   __device__ __forceinline__ void load(const uint8_t* const (&base)[kTS]) {
     const int r = threadIdx.x % kTileTokens;
 #pragma unroll
@@ -450,9 +684,20 @@ struct StageCodes {
       const uint8_t* p = base[0];
 #pragma unroll
       for (int n = 1; n < kTS; ++n) p = tile(i) == n ? base[n] : p;
-      if (!has(i) || !p) continue;
+      if (!has(i)) continue;
       c[i] = *reinterpret_cast<const u32x4*>(p + (chunk(i) * kTileTokens + r) * 16);
       s[i] = p[scale_at<kBits>(DP, r) + chunk(i) * 128 / (kBits * kGroup)];
+    }
+  }
+  // seen[n]: tokens of tile n that are seen by some row; bad(n): it holds a value that is perhaps not finite
+  template <typename F>
+  __device__ __forceinline__ void cut(const int (&seen)[kTS], F bad) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      int upto = seen[0];
+#pragma unroll
+      for (int n = 1; n < kTS; ++n) upto = tile(i) == n ? seen[n] : upto;
+      if (!cut_codes<kBits>(c, s, i, static_cast<int>(threadIdx.x) % kTileTokens < upto) && has(i)) bad(tile(i));
     }
   }
   template <typename F>
@@ -470,14 +715,19 @@ struct StageCodes {
   }
 };
 
+template <typename T>
+constexpr int quant_waves(int dp) {
+  return quant_two_per_cu(sizeof(T) == 4 ? DMOE_F32 : DMOE_BF16, dp) ? 2 : 1;
+}
+
 // Many rows: 128 of one kv head per workgroup, 32 to a wave, all four waves on the same keys.  Codes of kTS tiles
 // are loaded two stages ahead, opened into LDS one stage ahead, each by one of the
 // threads; one barrier a stage.
 template <typename T, int DP, int kKB, int kVB>
 __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef QuantStage<DP> Stage;
-  typedef QuantRows<T, DP, Stage::kK> Rows;
-  constexpr int kB = Rows::kB, kS = Rows::kS, kK = Stage::kK, kTS = Stage::kTS;
+  typedef QuantRows<T, DP, 32, quant_waves<T>(DP) == 1> Rows;
+  constexpr int kK = Stage::kK, kTS = Stage::kTS;
   __shared__ Stage s0, s1;
   const int hkv = a.cache.n_kv_heads;
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
@@ -485,10 +735,10 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
   if (!load_item(a, item_i, it)) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const TurnedValues<DP> turned(lane);
+  const TurnedRead<DP, 32> turned(lane);
   Rows w;
   w.clear();
-  const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wave, lane);
+  const QuantPlace<T, DP, 32> rows(w, a, it, sh.group, hk, it.first + 32 * wave, lane);
   w.load(rows, a, it, [&](int j) { return 16 * j + 8 * half; });
   const float scale2 = a.scale * kLog2e;
   const QuantMap<DP, kKB, kVB> map(a, it.slot, hk);
@@ -508,83 +758,68 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
     const uint8_t *kb[kTS], *vb[kTS];
 #pragma unroll
     for (int n = 0; n < kTS; ++n) {
-      const bool on = map.holds(pg.id[n]);
-      const long at = on ? map.at(kt + n, pg.id[n]) : 0;
-      kb[n] = on ? map.key(at) : nullptr;
-      vb[n] = on ? map.value(at) : nullptr;
+      const long at = map.at(kt + n, pg.id[n]);
+      kb[n] = map.key(at);
+      vb[n] = map.value(at);
     }
     kc.load(kb);
     vc.load(vb);
   };
-  // what lies on no page leaves something in LDS that is not used
-  auto open = [&](Stage& st) {
+  // stages whose keys every row of the workgroup sees, all of them on pages, come first in a sequence that has them
+  auto end_of = [&](int row) { return visible_end(it.len - it.n + row / sh.group, it.len, a.mask_block); };
+  const int whole = end_of(it.first) / kTileTokens, hi = end_of(min(it.first + 128, it.rows) - 1);
+  auto plain = [&](int kt, const Ids& pg) {
+    bool all = kt + kTS <= whole;
+#pragma unroll
+    for (int n = 0; n < kTS; ++n) all = all && map.holds(pg.id[n]);
+    return all;
+  };
+  auto open = [&](int kt, const Ids& pg, Stage& st) {
     const int r = threadIdx.x % kTileTokens;
+    if (!plain(kt, pg)) {
+      int seen[kTS];
+#pragma unroll
+      for (int n = 0; n < kTS; ++n) seen[n] = map.holds(pg.id[n]) ? hi - (kt + n) * kTileTokens : 0;
+      kc.cut(seen, [](int) {});
+      vc.cut(seen, [&](int n) { st.bad[n] = kt + n; });
+    }
     kc.open([&](int n, int p, const bf16x8& x) { st.k[n][p / 2][32 * (p & 1) + r] = x; });
     vc.open([&](int n, int p, const bf16x8& x) { TurnedValues<DP>::write(st.v[n], r, p, x); });
   };
-  auto score = [&](f32x16& s, const Stage& st, int n) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < kK; ++j) w.score(s, st.k[n][j][lane], j);
-  };
-  // A stage that every row sees whole; its tiles may still lie on no page, or behind the item's last.
-  auto compute = [&](const Ids& pg, const Stage& st) {
+  int left = it.kt1;  // the first tile for add_by_key
+  auto compute = [&](int kt, const Ids& pg, const Stage& st) {
     if (!rows.any) return;
-    bool on[kTS];
-    bool all = true, none = true;
+    float s[kTS][Rows::kN];
 #pragma unroll
     for (int n = 0; n < kTS; ++n) {
-      on[n] = map.holds(pg.id[n]);
-      all = all && on[n];
-      none = none && !on[n];
+#pragma unroll
+      for (int i = 0; i < Rows::kN; ++i) s[n][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kK; ++j) w.score(s[n], 0, st.k[n][j][lane], j);
     }
-    if (none) return;
-    f32x16 s[kTS];
+    const bool masked = !plain(kt, pg);
+    int seen[kTS];
 #pragma unroll
-    for (int n = 0; n < kTS; ++n) score(s[n], st, n);
-    if (!all) {
-#pragma unroll
-      for (int n = 0; n < kTS; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = on[n] ? s[n][i] : -INFINITY;
-    }
-    w.template softmax<kTS>(s, scale2, 0, false, half);
+    for (int n = 0; n < kTS; ++n) seen[n] = map.holds(pg.id[n]) ? w.end - (kt + n) * kTileTokens : 0;
+    w.template softmax<kTS>(s, scale2, masked, seen, half);
 #pragma unroll
     for (int n = 0; n < kTS; ++n) {
-      if (!on[n]) continue;
-      w.add(s[n], [&](int b, int x) { return turned.read(st.v[n], b, x); });
-    }
-  };
-  // Any stage, tile by tile.
-  bool left = false;  // tiles for add_by_key
-  auto compute_masked = [&](int kt, const Ids& pg, const Stage& st) {
-#pragma unroll
-    for (int n = 0; n < kTS; ++n) {
-      const int key0 = (kt + n) * kTileTokens;
-      if (!map.holds(pg.id[n]) || key0 >= w.hi) continue;
-      f32x16 s[1];
-      score(s[0], st, n);
-      w.template softmax<1>(s, scale2, key0, true, half);
-      __builtin_amdgcn_sched_barrier(0);
-      bf16x8 v[kB][kS];
-#pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int x = 0; x < kS; ++x) v[b][x] = turned.read(st.v[n], b, x);
-      if (w.cut(v, key0, half))
-        w.add(s[0], [&](int b, int x) { return v[b][x]; });
+      // a value that is not finite must not reach the rows that do not see it
+      if (masked && __builtin_amdgcn_readfirstlane(st.bad[n]) == kt + n)
+        left = min(left, kt + n);
       else
-        left = true;
-      __builtin_amdgcn_sched_barrier(0);
+        w.add(s[n], [&](int b, int x) { return turned.read(st.v[n], b, x); });
     }
   };
   int kt = kt0;
   Ids pg = pages(kt), pg1 = pages(kt + kTS);
+  if (threadIdx.x < 2 * kTS) (threadIdx.x < kTS ? s0 : s1).bad[threadIdx.x % kTS] = -1;
   load(kt, pg);
-  open(s0);
+  __syncthreads();
+  open(kt, pg, s0);
   load(kt + kTS, pg1);
-  auto turn = [&](auto masked, Stage& cur, Stage& fill) {
+  // every wave takes all turns, for their barriers
+  auto turn = [&](Stage& cur, Stage& fill) {
     w.pin();
     // a stage's writes are done, by all; the other buffer has been read
     lds_order();
@@ -592,54 +827,35 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
     __builtin_amdgcn_s_barrier();
     lds_order();
     const Ids pg2 = pages(kt + 2 * kTS);
-    open(fill);
+    open(kt + kTS, pg1, fill);
     load(kt + 2 * kTS, pg2);
-    if constexpr (masked)
-      compute_masked(kt, pg, cur);
-    else
-      compute(pg, cur);
+    __builtin_amdgcn_sched_barrier(0);
+    compute(kt, pg, cur);
     kt += kTS;
     pg = pg1;
     pg1 = pg2;
   };
-  // stages whose keys every row of the workgroup sees, then the others; every
-  // wave takes all turns, for their barriers
-  const int whole = visible_end(it.len - it.n + it.first / sh.group, it.len, a.mask_block) / kTileTokens;
-  const int stages = whole >= kt1 ? max(kt1 - kt + kTS - 1, 0) / kTS : max(whole - kt, 0) / kTS;
-  const int first_masked = kt + stages * kTS;
   int done = 0;
-  for (; done + 2 <= stages; done += 2) {
-    turn(std::false_type(), s0, s1);
-    turn(std::false_type(), s1, s0);
+  for (; done + 2 <= turns; done += 2) {
+    turn(s0, s1);
+    turn(s1, s0);
   }
-  if (done < stages) {
-    turn(std::false_type(), s0, s1);
-    ++done;
-  }
-  for (; done < turns; ++done) {
-    if (done & 1)
-      turn(std::true_type(), s1, s0);
-    else
-      turn(std::true_type(), s0, s1);
-  }
+  if (done < turns) turn(s0, s1);
   __syncthreads();  // the stages are done with
-  if (left) {
+  if (left < kt1) {
     static_assert(sizeof(Stage) >= 2 * TurnedValues<DP>::kBytes);
     char* room = reinterpret_cast<char*>(wave < 2 ? &s0 : &s1) + (wave & 1) * TurnedValues<DP>::kBytes;
-    add_by_key<Rows, QuantMap<DP, kKB, kVB>, DP, kKB, kVB>(w, map, first_masked, kt1, 1, scale2, lane, room, [&](f32x16& s, const uint8_t* p) {
-      // operands in the queries' order, straight from memory: lane's token, elements 16j + 8 half on
+    add_by_key<DP, kKB, kVB, 32>(w, map, left, kt1, 1, scale2, lane, room, [&](float (&s)[Rows::kN], const uint8_t* p) {
+      // operands in the queries' order, straight from memory: the lane's token, elements 16j + 8 half on
       const int r = lane & 31;
-#pragma unroll 1
+#pragma unroll
+      for (int i = 0; i < Rows::kN; ++i) s[i] = 0.f;
+#pragma unroll
       for (int j = 0; j < kK; ++j) {
         const int d = 16 * j + 8 * half;
-        uint32_t x[2];
-        const uint8_t* c = p + code_at<kKB>(r, d);
-        x[0] = *reinterpret_cast<const uint32_t*>(c);
-        x[1] = kKB == 8 ? *reinterpret_cast<const uint32_t*>(c + 4) : 0;
-        const bf16x8 k = decode<kKB>(x, scale_of(p[scale_at<kKB>(DP, r) + d / kGroup]));
-#pragma unroll
-        for (int y = 0; y < kK; ++y)
-          if (y == j) w.score(s, k, y);
+        const uint32_t* c = reinterpret_cast<const uint32_t*>(p + code_at<kKB>(r, d));
+        const uint32_t x[2] = {c[0], kKB == 8 ? c[1] : 0u};
+        w.score(s, 0, decode<kKB>(x, scale_of(p[scale_at<kKB>(DP, r) + d / kGroup])), j);
       }
     });
   }
@@ -647,21 +863,26 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
   rows.store(w, a, sh, it, hk, half, part_rows);
 }
 
+template <typename T, int DP, int kKB, int kVB, int kR, int kWR>
+void launch_quant_rows(const AttnArgs& a, const AttnShape& sh, unsigned items, int part_rows, hipStream_t s) {
+  constexpr size_t join = 2 * (kR * DP / 64 + 2) * 64 * sizeof(float), values = 4 * TurnedValues<DP>::kBytes;
+  quant_rows_kernel<T, DP, kKB, kVB, kR, kWR><<<items, 256, join > values ? join : values, s>>>(a, sh, part_rows);
+}
+
 template <typename T, int DP, int kKB, int kVB>
 hipError_t launch_quant_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
   const int hkv = a.cache.n_kv_heads;
   const unsigned items = static_cast<unsigned>(sh.max_items() * hkv);
   const int part_rows = static_cast<int>(sh.max_parts() * hkv * sh.tile_rows);
-  if (sh.tile_rows <= 64) {
-    const size_t join = 2 * (16 * (DP / 32) + 2) * 64 * sizeof(float), values = 4 * TurnedValues<DP>::kBytes;
-    const size_t lds = join > values ? join : values;
-    if (sh.tile_rows == 32)
-      quant_rows_kernel<T, DP, kKB, kVB, 1><<<items, 256, lds, s>>>(a, sh, part_rows);
-    else
-      quant_rows_kernel<T, DP, kKB, kVB, 2><<<items, 256, lds, s>>>(a, sh, part_rows);
-  } else {
+  const long most = static_cast<long>(a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) * sh.group;
+  if (sh.tile_rows == 32 && most <= 16)
+    launch_quant_rows<T, DP, kKB, kVB, 16, 1>(a, sh, items, part_rows, s);
+  else if (sh.tile_rows == 32)
+    launch_quant_rows<T, DP, kKB, kVB, 32, 1>(a, sh, items, part_rows, s);
+  else if (sh.tile_rows == 64)
+    launch_quant_rows<T, DP, kKB, kVB, 32, 2>(a, sh, items, part_rows, s);
+  else
     quant_block_kernel<T, DP, kKB, kVB><<<items, 256, 0, s>>>(a, sh, part_rows);
-  }
   return launch_merge<T, DP>(a, sh, part_rows, s);
 }
 
