@@ -362,49 +362,49 @@ struct QuantPlace {
   int row, tok, qh;
   bool live, any;
   template <typename Rows>
-  __device__ __forceinline__ QuantPlace(Rows& w, const AttnArgs& a, const AttnItem& it, int g, int hk, int row_lo, int lane) {
-    const int row_hi = min(row_lo + kR, it.rows) - 1;
-    const int pos0 = it.len - it.n;
+  __device__ __forceinline__ QuantPlace(Rows& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk, int row_lo, int lane) {
     row = row_lo + lane % kR;
     live = row < it.rows;
-    any = row_hi >= row_lo;
-    tok = live ? row / g : 0;
-    qh = hk * g + (live ? row - tok * g : 0);
-    w.end = live ? visible_end(pos0 + tok, it.len, a.mask_block) : 0;
-    w.lo = any ? visible_end(pos0 + row_lo / g, it.len, a.mask_block) : 0;
-    w.hi = any ? visible_end(pos0 + row_hi / g, it.len, a.mask_block) : 0;
+    any = row_lo < it.rows;
+    tok = live ? sh.by_group.of(row) : 0;
+    qh = hk * sh.group + (live ? row - tok * sh.group : 0);
+    w.end = live ? seen_end(a, sh, it, tok) : 0;
+    w.lo = any ? seen_end(a, sh, it, sh.by_group.of(row_lo)) : 0;
+    w.hi = any ? seen_end(a, sh, it, sh.by_group.of(min(row_lo + kR, it.rows) - 1)) : 0;
+  }
+  // visible_end of the item's token
+  static __device__ __forceinline__ int seen_end(const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int tok) {
+    const int p = it.len - it.n + tok;
+    if (p < 0) return 0;
+    if (a.mask_block <= 0) return it.len;
+    const long e = (static_cast<long>(sh.by_mask.of(p)) + 1) * a.mask_block;
+    return e < it.len ? static_cast<int>(e) : it.len;
   }
   __device__ __forceinline__ const T* query(const AttnArgs& a, const AttnItem& it) const {
     return static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
   }
-  template <typename Rows>
-  __device__ __forceinline__ void store(const Rows& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk,
-                                        int group, int part_rows) const {
+  // The row's sums, x(i) elements d(i) .. d(i) + 3 of them for i < kN: divided into out, or as they are into the workspace;
+  // with `whole`, what belongs to the row once.
+  template <int kN, typename X, typename D>
+  __device__ __forceinline__ void store(X x, D d, float m, float l, bool whole, const AttnArgs& a, const AttnShape& sh, const AttnItem& it,
+                                        int hk, int part_rows) const {
     if (!live) return;
     if (it.part >= 0) {
-      const long at = (static_cast<long>(it.part) * a.cache.n_kv_heads + hk) * sh.tile_rows + (row - it.first);
-      float* po = static_cast<float*>(a.workspace) + (at - (row - it.first)) * DP;
+      const long tile = (static_cast<long>(it.part) * a.cache.n_kv_heads + hk) * sh.tile_rows;
+      const int r = row - it.first;
+      float* po = static_cast<float*>(a.workspace) + tile * DP;
 #pragma unroll
-      for (int b = 0; b < Rows::kB; ++b)
-#pragma unroll
-        for (int i = 0; i < Rows::kO; i += 4)
-          store4(po + partial_at(DP, row - it.first, Rows::element(b, i, group)), f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
-      if (group == 0)
-        *reinterpret_cast<float2*>(static_cast<float*>(a.workspace) + static_cast<long>(part_rows) * DP + at * 2) = make_float2(w.m, w.l);
+      for (int i = 0; i < kN; ++i) store4(po + partial_at(DP, r, d(i)), x(i));
+      if (whole) reinterpret_cast<float2*>(static_cast<float*>(a.workspace) + static_cast<long>(part_rows) * DP)[tile + r] = make_float2(m, l);
       return;
     }
-    const bool some = w.l > 0.f || w.l != w.l;
-    const float inv = some ? 1.f / w.l : 0.f;
+    const bool some = l > 0.f || l != l;
+    const float inv = some ? 1.f / l : 0.f;
     T* op = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim;
 #pragma unroll
-    for (int b = 0; b < Rows::kB; ++b)
-#pragma unroll
-      for (int i = 0; i < Rows::kO; i += 4) {
-        const int d = Rows::element(b, i, group);
-        if (d < a.cache.head_dim) store4(op + d, f32x4{w.o[b][i] * inv, w.o[b][i + 1] * inv, w.o[b][i + 2] * inv, w.o[b][i + 3] * inv});
-      }
-    if (a.lse && group == 0)
-      a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = some ? (w.m + log2f(w.l)) * kLn2 : -INFINITY;
+    for (int i = 0; i < kN; ++i)
+      if (d(i) < a.cache.head_dim) store4(op + d(i), x(i) * inv);
+    if (whole && a.lse) a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = some ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
 };
 
@@ -415,21 +415,21 @@ struct QuantMap {
   const uint8_t *k, *v;
   const __attribute__((address_space(4))) int32_t* table;
   long layer0;
-  int n_pages, shift, per_page;  // per_page: tiles of all kv heads
-  __device__ __forceinline__ QuantMap(const AttnArgs& a, int slot, int hk) : n_pages(a.cache.n_pages) {
+  int n_pages, tpp, per_page;  // tiles of a page of one kv head, of all
+  FastDiv by_page;
+  __device__ __forceinline__ QuantMap(const AttnArgs& a, const AttnShape& sh, int slot, int hk)
+      : n_pages(a.cache.n_pages), tpp(a.cache.page_tokens / kTileTokens), by_page(sh.by_page) {
     table = (const __attribute__((address_space(4))) int32_t*)(a.cache.table + static_cast<long>(slot) * a.cache.max_pages);
-    const int tpp = a.cache.page_tokens / kTileTokens;
-    shift = (tpp & (tpp - 1)) == 0 ? 31 - __builtin_clz(tpp) : -tpp;
     per_page = tpp * a.cache.n_kv_heads;
     layer0 = static_cast<long>(a.layer) * n_pages;
     k = static_cast<const uint8_t*>(a.cache.k) + static_cast<long>(hk * tpp) * kKTile;
     v = static_cast<const uint8_t*>(a.cache.v) + static_cast<long>(hk * tpp) * kVTile;
   }
-  __device__ __forceinline__ int page(int kt, int end) const { return kt < end ? table[shift >= 0 ? kt >> shift : kt / -shift] : -1; }
+  __device__ __forceinline__ int page(int kt, int end) const { return kt < end ? table[by_page.of(kt)] : -1; }
   __device__ __forceinline__ bool holds(int page) const { return static_cast<unsigned>(page) < static_cast<unsigned>(n_pages); }
   // tiles from k and v to a tile on a page; of no page: some tile of the pool
   __device__ __forceinline__ long at(int kt, int page) const {
-    return (layer0 + (holds(page) ? page : 0)) * per_page + (shift >= 0 ? kt & ((1 << shift) - 1) : kt % -shift);
+    return (layer0 + (holds(page) ? page : 0)) * per_page + (kt - by_page.of(kt) * tpp);
   }
   __device__ __forceinline__ const uint8_t* key(long tile) const { return k + tile * kKTile; }
   __device__ __forceinline__ const uint8_t* value(long tile) const { return v + tile * kVTile; }
@@ -478,21 +478,22 @@ struct WaveTile {
   }
 };
 
-// Tiles of a masked stretch that hold values that are not finite, once the running maximum is the last one
-// (WaveRows::add_by_key).  scores(s, keys): a tile's scores.
-template <int DP, int kKB, int kVB, int kR, typename Rows, typename Map, typename Scores>
-__device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int kt1, int step, float scale2, int lane, char* lds, Scores scores) {
+// Tiles left out because they hold, before token hi, a value that is perhaps not finite, once the running maximum is the
+// last one (WaveRows::add_by_key).  masked(kt): the tile was looked at for that; scores(s, keys): a tile's scores.
+template <int DP, int kKB, int kVB, int kR, typename Rows, typename Map, typename Masked, typename Scores>
+__device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int kt1, int step, int hi, float scale2, int lane, char* lds,
+                                           Masked masked, Scores scores) {
   const int g = lane / kR;
 #pragma unroll 1
   for (; kt < kt1; kt += step) {
     const int page = map.page(kt, kt1), key0 = kt * kTileTokens;
-    if (!map.holds(page) || key0 >= w.hi) continue;
+    if (!map.holds(page) || key0 >= w.hi || !masked(kt)) continue;
     const long at = map.at(kt, page);
     bf16x8 v[Rows::kB][Rows::kS];
     {
       WaveTile<DP, kKB, kVB, kR> t;
       t.template load_values<false>(map.value(at), lane);
-      if (__all(t.v.cut(lane % 32 < w.hi - key0))) continue;
+      if (__all(t.v.cut(lane % 32 < hi - key0))) continue;
       t.open_values(lds, lane);
       const TurnedRead<DP, kR> turned(lane);
 #pragma unroll
@@ -509,94 +510,95 @@ __device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int 
   }
 }
 
-// kWK waves' sums over different keys joined: join_waves.
-template <int kWK, typename Rows>
-__device__ __forceinline__ void join_quant(Rows& w, float* lds, int first, int wk, int lane) {
-  constexpr int kLen = (Rows::kO * Rows::kB + 2) * 64;
+// The sums of kW waves over different keys joined and stored: every wave lays its own in LDS, then takes an equal share of all.
+// (A tree of pairs had eight waves wait for 3.5 us; code that runs once costs its way into the instruction cache.)
+template <int kW, typename Rows, typename Place>
+__device__ __forceinline__ void join_store(const Rows& w, float* lds, int wave, int lane, const Place& rows, const AttnArgs& a, const AttnShape& sh,
+                                           const AttnItem& it, int hk, int part_rows) {
+  constexpr int kUnits = Rows::kO * Rows::kB / 4, kLen = (4 * kUnits + 2) * 64, kMine = (kUnits + kW - 1) / kW;
+  static_assert(Rows::kO == 4 || Rows::kO == 16);
+  float* mine = lds + wave * kLen;
+  mine[lane] = w.m;
+  mine[64 + lane] = w.l;
 #pragma unroll
-  for (int n = kWK / 2; n >= 1; n /= 2) {
-    float* buf = lds + (first + wk % n) * kLen;
-    if (wk >= n && wk < 2 * n) {
-      buf[lane] = w.m;
-      buf[64 + lane] = w.l;
-#pragma unroll
-      for (int b = 0; b < Rows::kB; ++b)
-#pragma unroll
-        for (int i = 0; i < Rows::kO; i += 4)
-          store4(buf + 128 + (Rows::kO / 4 * b + i / 4) * 256 + lane * 4, f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
-    }
-    __syncthreads();
-    if (wk < n) {
-      const float om = buf[lane], ol = buf[64 + lane];
-      const float nm = fmaxf(w.m, om);
-      const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = om == nm ? 1.f : exp2_hw(om - nm);
-      w.scale(fa);
-      w.m = nm;
-      w.l += fb * ol;
-#pragma unroll
-      for (int b = 0; b < Rows::kB; ++b)
-#pragma unroll
-        for (int i = 0; i < Rows::kO; i += 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 128 + (Rows::kO / 4 * b + i / 4) * 256 + lane * 4);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
-        }
-    }
-    __syncthreads();
+  for (int u = 0; u < kUnits; ++u) {
+    const int b = u / (Rows::kO / 4), i = u % (Rows::kO / 4) * 4;
+    store4(mine + 128 + u * 256 + lane * 4, f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]});
   }
+  __syncthreads();
+  if (kUnits % kW && wave * kMine >= kUnits) return;
+  float f[kW], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int x = 0; x < kW; ++x) {
+    f[x] = lds[x * kLen + lane];
+    m = fmaxf(m, f[x]);
+  }
+#pragma unroll
+  for (int x = 0; x < kW; ++x) {
+    f[x] = f[x] == m ? 1.f : exp2_hw(f[x] - m);
+    l += f[x] * lds[x * kLen + 64 + lane];
+  }
+  const int g = lane / (64 / Rows::kG);
+  f32x4 o[kMine];
+#pragma unroll
+  for (int y = 0; y < kMine; ++y) {
+    o[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kW; ++x) o[y] += f[x] * *reinterpret_cast<const f32x4*>(lds + x * kLen + 128 + (wave * kMine + y) * 256 + lane * 4);
+  }
+  rows.template store<kMine>([&](int y) { return o[y]; },
+                             [&](int y) {
+                               const int u = wave * kMine + y;
+                               return Rows::element(u / (Rows::kO / 4), u % (Rows::kO / 4) * 4, g);
+                             },
+                             m, l, wave == 0 && g == 0, a, sh, it, hk, part_rows);
 }
 
-// Registers of a tile's codes in a lane, and tiles on their way: as many as keep the memory busy.
-template <int DP, int kKB, int kVB>
-constexpr int tile_regs = DP * (kKB + kVB) / 64 + 4;
-template <int DP, int kKB, int kVB>
-constexpr int tiles_ahead = tile_regs<DP, kKB, kVB> <= 24 ? 3 : tile_regs<DP, kKB, kVB> <= 48 ? 2 : 1;
-// Waves of a SIMD: what queries, sums, codes and the rest of a wave leave room for.
+// Waves of a SIMD in the kernel of few rows: two where a lane's queries, sums and codes leave room for the rest in half of the
+// registers.  64 single tokens of up to 16k, 16 and 4 heads of 256 in 4 bits: 86 us with two, 103 with one; of up to 8k in
+// 8 bits, which do not fit: 205 (spilled) and 96.  Three, where they fit, measured as two.
 template <typename T, int DP, int kKB, int kVB, int kR>
-constexpr int rows_regs = kParts<T> * DP * kR / 128 + DP * kR / 64 + tiles_ahead<DP, kKB, kVB> * tile_regs<DP, kKB, kVB> + kR / 2 + 64;
-template <typename T, int DP, int kKB, int kVB, int kR>
-constexpr int rows_waves = rows_regs<T, DP, kKB, kVB, kR> <= 168 ? 3 : rows_regs<T, DP, kKB, kVB, kR> <= 256 ? 2 : 1;
+constexpr int rows_waves = kParts<T> * DP * kR / 128 + DP * kR / 64 + DP * (kKB + kVB) / 64 < 160 ? 2 : 1;
 
-// Few rows: kR kWR of one kv head per workgroup, kR to a wave, 4 / kWR waves to the same ones, each on every (4 / kWR)-th
-// key tile, joined through LDS.  Codes go straight into registers, the next tiles' while one is used: loads are
-// straight-line code, so that waiting for a tile does not wait for those behind it.
-template <typename T, int DP, int kKB, int kVB, int kR, int kWR>
-__global__ __launch_bounds__(256, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+// Few rows: kR of one kv head per workgroup, its kW waves each on every kW-th key tile, joined through LDS.  Codes go
+// straight into registers, past the caches, the next tile's while one is used.
+template <typename T, int DP, int kKB, int kVB, int kR, int kW>
+__global__ __launch_bounds__(64 * kW, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   constexpr bool kPin = rows_waves<T, DP, kKB, kVB, kR> == 1;
   typedef QuantRows<T, DP, kR, kPin> Rows;
   typedef WaveTile<DP, kKB, kVB, kR> Tile;
   typedef typename Tile::Keys Keys;
-  constexpr int kWK = 4 / kWR, kAhead = tiles_ahead<DP, kKB, kVB>;
-  constexpr bool kStream = kWR == 1;
   extern __shared__ float lds[];
   const int hkv = a.cache.n_kv_heads;
   const int item_i = blockIdx.x / hkv, hk = blockIdx.x % hkv;
   AttnItem it;
   if (!load_item(a, item_i, it)) return;
   const int lane = threadIdx.x & 63, g = lane / kR;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % kWK, wr = wave / kWK;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* mine = reinterpret_cast<char*>(lds) + wave * TurnedValues<DP>::kBytes;
   const TurnedRead<DP, kR> turned(lane);
   Rows w;
   w.clear();
-  const QuantPlace<T, DP, kR> rows(w, a, it, sh.group, hk, it.first + kR * wr, lane);
+  const QuantPlace<T, DP, kR> rows(w, a, sh, it, hk, it.first, lane);
   const float scale2 = a.scale * kLog2e;
-  const QuantMap<DP, kKB, kVB> map(a, it.slot, hk);
+  const QuantMap<DP, kKB, kVB> map(a, sh, it.slot, hk);
   const int kt1 = min(it.kt1, (w.hi + kTileTokens - 1) / kTileTokens);
-  Tile tile[kAhead];
-  // pages of the tiles on their way, and of the one after them
-  int kt = it.kt0 + wk;
-  int page[kAhead + 1];
-  auto fetch = [&](Tile& t, int at_kt, int pg) {
+  // page ids are known two of this wave's tiles ahead, codes one; of no page, and behind the last tile, some tile of the pool's
+  int kt = it.kt0 + wave;
+  int page = -1;
+  if (wave >= 4)
+    page = map.page(kt, kt1);
+  else if (kt < kt1)
+    page = wave < 2 ? wave == 0 ? it.page[0] : it.page[1] : wave == 2 ? it.page[2] : it.page[3];
+  Tile t;
+  auto fetch = [&](int at_kt, int pg) {
     const long at = map.at(at_kt, pg);
-    t.template load_keys<kStream>(map.key(at), lane);
-    t.template load_values<kStream>(map.value(at), lane);
+    t.template load_keys<true>(map.key(at), lane);
+    t.template load_values<true>(map.value(at), lane);
   };
-  page[0] = kt < kt1 ? (wk < 2 ? wk == 0 ? it.page[0] : it.page[1] : wk == 2 ? it.page[2] : it.page[3]) : -1;
-  fetch(tile[0], kt, page[0]);
+  fetch(kt, page);
   const int now = map.page(kt, kt1);
-#pragma unroll
-  for (int i = 1; i <= kAhead; ++i) page[i] = map.page(kt + i * kWK, kt1);
+  int page1 = map.page(kt + kW, kt1);
   w.load(rows, a, it, [&](int j) {
     int d = 0;
 #pragma unroll
@@ -604,27 +606,24 @@ __global__ __launch_bounds__(256, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_
       if (j >= Keys::first(i)) d = Keys::element(i, j - Keys::first(i), g);
     return d;
   });
-#pragma unroll
-  for (int i = 1; i < kAhead; ++i) fetch(tile[i], kt + i * kWK, page[i]);
-  if (now != page[0]) {  // moved since the plan was made
-    page[0] = now;
-    fetch(tile[0], kt, now);
+  if (now != page) {  // moved since the plan was made
+    page = now;
+    fetch(kt, page);
   }
   // tiles that every row sees whole come first
   const int whole = min(kt1, w.lo / kTileTokens);
   int left = kt1;  // the first tile for add_by_key
-  auto turn = [&](Tile& t) {
+  while (kt < kt1) {
     w.pin();
-    const int after = map.page(kt + (kAhead + 1) * kWK, kt1);
-    const int key0 = kt * kTileTokens;
+    const int page2 = map.page(kt + 2 * kW, kt1), key0 = kt * kTileTokens;
     const bool masked = kt >= whole;
     bool finite = true;
     if (masked) finite = __all(t.v.cut(lane % 32 < w.hi - key0));
     float s[1][Rows::kN];
     t.scores(w, s[0]);
     t.open_values(mine, lane);
-    fetch(t, kt + kAhead * kWK, page[kAhead]);
-    if (map.holds(page[0])) {
+    fetch(kt + kW, page1);
+    if (map.holds(page)) {
       const int seen[1] = {w.end - key0};
       w.template softmax<1>(s, scale2, masked, seen, g);
       // a value that is not finite must not reach the rows that do not see it
@@ -633,27 +632,20 @@ __global__ __launch_bounds__(256, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_
       else
         left = min(left, kt);
     }
-    kt += kWK;
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) page[i] = page[i + 1];
-    page[kAhead] = after;
-  };
-  while (kt < kt1) {
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (i == 0 || kt < kt1) turn(tile[i]);
+    kt += kW;
+    page = page1;
+    page1 = page2;
   }
   w.pin();
   if (left < kt1)
-    add_by_key<DP, kKB, kVB, kR>(w, map, left, kt1, kWK, scale2, lane, mine, [&](float (&s)[Rows::kN], const uint8_t* p) {
-      Tile t;
-      t.template load_keys<false>(p, lane);
-      t.scores(w, s);
+    add_by_key<DP, kKB, kVB, kR>(w, map, left, kt1, kW, w.hi, scale2, lane, mine, [](int) { return true; }, [&](float (&s)[Rows::kN], const uint8_t* p) {
+      Tile other;
+      other.template load_keys<false>(p, lane);
+      other.scores(w, s);
     });
   w.l = groups_sum<Rows::kG>(w.l);
   __syncthreads();  // the values' places are taken by the sums
-  join_quant<kWK>(w, lds, wr * (kWK / 2), wk, lane);
-  if (wk == 0) rows.store(w, a, sh, it, hk, g, part_rows);
+  join_store<kW>(w, lds, wave, lane, rows, a, sh, it, hk, part_rows);
 }
 
 // Keys and values of kTS tiles in LDS: keys as operands, element 16j + 8 half + e of
@@ -738,10 +730,10 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
   const TurnedRead<DP, 32> turned(lane);
   Rows w;
   w.clear();
-  const QuantPlace<T, DP, 32> rows(w, a, it, sh.group, hk, it.first + 32 * wave, lane);
+  const QuantPlace<T, DP, 32> rows(w, a, sh, it, hk, it.first + 32 * wave, lane);
   w.load(rows, a, it, [&](int j) { return 16 * j + 8 * half; });
   const float scale2 = a.scale * kLog2e;
-  const QuantMap<DP, kKB, kVB> map(a, it.slot, hk);
+  const QuantMap<DP, kKB, kVB> map(a, sh, it.slot, hk);
   const int kt0 = it.kt0, kt1 = it.kt1, turns = (kt1 - kt0 + kTS - 1) / kTS;
   struct Ids {
     int id[kTS];
@@ -766,7 +758,7 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
     vc.load(vb);
   };
   // stages whose keys every row of the workgroup sees, all of them on pages, come first in a sequence that has them
-  auto end_of = [&](int row) { return visible_end(it.len - it.n + row / sh.group, it.len, a.mask_block); };
+  auto end_of = [&](int row) { return rows.seen_end(a, sh, it, sh.by_group.of(row)); };
   const int whole = end_of(it.first) / kTileTokens, hi = end_of(min(it.first + 128, it.rows) - 1);
   auto plain = [&](int kt, const Ids& pg) {
     bool all = kt + kTS <= whole;
@@ -845,7 +837,12 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
   if (left < kt1) {
     static_assert(sizeof(Stage) >= 2 * TurnedValues<DP>::kBytes);
     char* room = reinterpret_cast<char*>(wave < 2 ? &s0 : &s1) + (wave & 1) * TurnedValues<DP>::kBytes;
-    add_by_key<DP, kKB, kVB, 32>(w, map, left, kt1, 1, scale2, lane, room, [&](float (&s)[Rows::kN], const uint8_t* p) {
+    // the workgroup's flags, not the wave's: a tile may be left out for what only other waves' rows see
+    auto masked = [&](int kt) {
+      const int first = kt0 + (kt - kt0) / kTS * kTS;
+      return !plain(first, pages(first));
+    };
+    add_by_key<DP, kKB, kVB, 32>(w, map, left, kt1, 1, hi, scale2, lane, room, masked, [&](float (&s)[Rows::kN], const uint8_t* p) {
       // operands in the queries' order, straight from memory: the lane's token, elements 16j + 8 half on
       const int r = lane & 31;
 #pragma unroll
@@ -860,13 +857,14 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
     });
   }
   w.l = other_half_sum(w.l);
-  rows.store(w, a, sh, it, hk, half, part_rows);
+  rows.template store<4 * Rows::kB>([&](int y) { return f32x4{w.o[y / 4][y % 4 * 4], w.o[y / 4][y % 4 * 4 + 1], w.o[y / 4][y % 4 * 4 + 2], w.o[y / 4][y % 4 * 4 + 3]}; },
+                                    [&](int y) { return Rows::element(y / 4, y % 4 * 4, half); }, w.m, w.l, half == 0, a, sh, it, hk, part_rows);
 }
 
-template <typename T, int DP, int kKB, int kVB, int kR, int kWR>
+template <typename T, int DP, int kKB, int kVB, int kR, int kW>
 void launch_quant_rows(const AttnArgs& a, const AttnShape& sh, unsigned items, int part_rows, hipStream_t s) {
-  constexpr size_t join = 2 * (kR * DP / 64 + 2) * 64 * sizeof(float), values = 4 * TurnedValues<DP>::kBytes;
-  quant_rows_kernel<T, DP, kKB, kVB, kR, kWR><<<items, 256, join > values ? join : values, s>>>(a, sh, part_rows);
+  constexpr size_t join = kW * (kR * DP / 64 + 2) * 64 * sizeof(float), values = kW * TurnedValues<DP>::kBytes;
+  quant_rows_kernel<T, DP, kKB, kVB, kR, kW><<<items, 64 * kW, join > values ? join : values, s>>>(a, sh, part_rows);
 }
 
 template <typename T, int DP, int kKB, int kVB>
@@ -875,21 +873,23 @@ hipError_t launch_quant_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t 
   const unsigned items = static_cast<unsigned>(sh.max_items() * hkv);
   const int part_rows = static_cast<int>(sh.max_parts() * hkv * sh.tile_rows);
   const long most = static_cast<long>(a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) * sh.group;
-  if (sh.tile_rows == 32 && most <= 16)
-    launch_quant_rows<T, DP, kKB, kVB, 16, 1>(a, sh, items, part_rows, s);
-  else if (sh.tile_rows == 32)
-    launch_quant_rows<T, DP, kKB, kVB, 32, 1>(a, sh, items, part_rows, s);
-  else if (sh.tile_rows == 64)
-    launch_quant_rows<T, DP, kKB, kVB, 32, 2>(a, sh, items, part_rows, s);
-  else
+  if (sh.tile_rows == 128)
     quant_block_kernel<T, DP, kKB, kVB><<<items, 256, 0, s>>>(a, sh, part_rows);
+  else if (most <= 16)
+    launch_quant_rows<T, DP, kKB, kVB, 16, 4>(a, sh, items, part_rows, s);
+  else
+    launch_quant_rows<T, DP, kKB, kVB, 32, rows_waves<T, DP, kKB, kVB, 32> == 2 ? 8 : 4>(a, sh, items, part_rows, s);
   return launch_merge<T, DP>(a, sh, part_rows, s);
 }
 
 }  // namespace attn
 
 template <typename T, int kKB, int kVB>
-hipError_t launch_attention_quant(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
+hipError_t launch_attention_quant(const AttnArgs& a, const AttnShape& shape, hipStream_t s) {
+  AttnShape sh = shape;
+  sh.by_group = fast_div(sh.group);
+  sh.by_page = fast_div(a.cache.page_tokens / kTileTokens);
+  sh.by_mask = fast_div(a.mask_block > 0 ? a.mask_block : 1);
   switch (padded_dim(a.cache.head_dim)) {
     case 32: return attn::launch_quant_dim<T, 32, kKB, kVB>(a, sh, s);
     case 64: return attn::launch_quant_dim<T, 64, kKB, kVB>(a, sh, s);

@@ -23,6 +23,9 @@ constexpr int kMinWide = 8;
 // Pieces that even out row tiles of 128, key tiles: long enough not to notice their partial results.
 constexpr int kEvenBf16 = 48;
 constexpr int kEvenF32 = 16;
+constexpr int kSplitWide = 256;   // items of eight waves: one a CU
+constexpr int kMinEight = 16;     // their key tiles: two a wave
+constexpr long kFew32 = 128, kFewTiles32 = 128, kFewKeys32 = 20000;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
 
 // Largest i with a[i] <= x, for a[0] = 0 <= x < a[n].
@@ -116,7 +119,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   // Items of 32 rows are cheap to join: pieces of the average length even the
   // sequences out, of half of it where there are many sequences (64 of up to 16k tokens:
   // 191 -> 181 us).
-  const long room = sh.tile_rows <= 64 ? (many && sh.tile_rows == 32 ? sh.split_items : split) : max(max(split - n_tiles, split / 2), 1l);
+  const long room = sh.tile_rows == 32 && many   ? sh.split_items
+                    : sh.tile_rows <= 64 && !sh.wide ? split
+                                                     : max(max(split - n_tiles, split / 2), 1l);
   long len = max(static_cast<long>(sh.min_tiles), (all + room - 1) / room);
   if (sh.tile_rows == 128 && many && 10l * longest * n_tiles > 13 * all)
     len = min(len, max(static_cast<long>(sh.even_tiles), (all + 2 * split - 1) / (2 * split)));
@@ -190,6 +195,7 @@ AttnShape shape_of(int tile_rows, int n_seqs, int T, int max_new, int n_heads, i
   s.even_tiles = 0;
   s.wide = false;
   s.unit = 1;
+  s.by_group = s.by_page = s.by_mask = fast_div(1);
   return s;
 }
 
@@ -198,6 +204,18 @@ AttnShape shape_of(int tile_rows, int n_seqs, int T, int max_new, int n_heads, i
 AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   const long most = most_rows(b.T, b.max_new, n_heads / c.n_kv_heads);
   auto shape = [&](int rows) { return shape_of(rows, b.n_seqs, b.T, b.max_new, n_heads, c.n_kv_heads); };
+  const bool few = c.format != DMOE_KV_PLAIN;  // bits: bf16 products, whatever the rows
+  if (few && most > 16) {
+    AttnShape s = shape(32);
+    const long tiles = s.max_tiles * c.n_kv_heads, keys = static_cast<long>(c.max_pages) * c.page_tokens / kTileTokens;
+    if (most <= 32 || (s.max_tiles <= kFew32 && tiles <= kFewTiles32 && tiles * keys <= kFewKeys32)) {
+      s.wide = true;
+      s.aim = kSplitWide / c.n_kv_heads > 1 ? kSplitWide / c.n_kv_heads : 1;
+      s.split_items = 2 * s.aim;
+      s.min_tiles = kMinEight;
+      return s;
+    }
+  }
   if (most <= 32) return shape(32);
   // More than 64 rows a sequence: 128 to a workgroup read the cache once where
   // 64 read it twice, but a workgroup of 64 starts sooner and there are twice as
@@ -207,12 +225,11 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   // against 25.3 at 16000; of eight: 16.4 against 19.1 at 400, 31.8 against 30.2 at 4096.
   const AttnShape two = shape(64);
   const long tiles = two.max_tiles * c.n_kv_heads, keys = static_cast<long>(c.max_pages) * c.page_tokens / kTileTokens;
-  if (most <= 64 || tiles <= kFewTiles || tiles * keys <= kFewKeys) return two;
+  if (!few && (most <= 64 || tiles <= kFewTiles || tiles * keys <= kFewKeys)) return two;
   AttnShape s = shape(128);
   // one workgroup a CU: where a wave needs more than half of a SIMD's
   // registers, and where eight waves work on an item, which they do if the
   // batch's row tiles alone do not fill the device
-  const bool few = c.format != DMOE_KV_PLAIN;  // bits: bf16 products, whatever the rows
   const int dp = padded_dim(c.head_dim);
   const bool half = few ? quant_two_per_cu(c.dt, dp) : two_per_cu(c.dt, dp);
   s.wide = !few && half && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
@@ -229,6 +246,10 @@ size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
     const size_t m = plan_ints(shape_of(rows, n_seqs, T, max_new, n_heads, n_kv_heads));
     n = m > n && (rows > 32 || most_rows(T, max_new, n_heads / n_kv_heads) <= 32) ? m : n;
   }
+  // 32 rows to an item also where there are more of them, but few (attn_shape)
+  AttnShape few = shape_of(32, n_seqs, T, max_new, n_heads, n_kv_heads);
+  if (few.max_tiles > kFew32) few.max_tiles = kFew32;
+  n = plan_ints(few) > n ? plan_ints(few) : n;
   return n;
 }
 
