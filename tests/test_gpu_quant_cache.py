@@ -131,14 +131,42 @@ def test_rotated_keys(gpu_lib, fmt, dtype, dim, rot, inter, scaling, start):
     out = [torch.zeros(s.T, 2, dim, dtype=dtype, device="cuda") for _ in range(2)]
     s.cache.read(0, s.offd, *out, slots=s.slotsd, max_tokens=40)
     assert all(same(x.cpu().double(), want) for x, want in zip(out, rows))
-    # the queries are those that a plain cache's append gives
-    plain = PagedCache(1, 3, 1024, 2, dim, 2, 1 << 11, dtype=dtype)
-    plain.lens[:] = i32([start + 40, start + 3])
-    att = BlockAttention(plain, 4, 2, 40, s.T, rope=rope)
-    att.begin(s.offd)
-    want = torch.zeros_like(q_out)
-    att.append(0, s.k.cuda(), s.v.cuda(), q=s.q.cuda(), q_out=want)
-    assert torch.equal(q_out, want)
+    # Queries are turned in float32: (cos, sin) off by 2^-22, one product of two fused with the sum (2^-23), one rounding
+    # to the type, of at most 2 scale max|x| in size.  (Equal bits to a plain cache's append would ask for the same product fused.)
+    f, scale = rope.turns.cpu().tolist(), float(torch.tensor(rope.scale))
+    for i in range(2):
+        at = slice(s.off[i], s.off[i + 1])
+        want = R.rotate(s.q[at], s.positions(i), f, scale, inter)
+        size = 2 * scale * s.q[at].double().abs().amax(-1, keepdim=True)
+        assert bool(((q_out[at].cpu().double() - want).abs() <= (2.0 ** -22 + 2.0 ** -23 + R.EPS[dtype]) * size).all())
+        assert torch.equal(q_out[at, :, rot:].cpu(), s.q[at, :, rot:])
+    assert bool((q_out[s.off[-1]:] == 0).all())
+
+
+@pytest.mark.parametrize("fmt,inter", [("fp8", False), ("fp8", True), ("fp4", True)])
+def test_keys_are_rounded_twice(gpu_lib, fmt, inter):
+    """From 64 bits to float32 and from there to bf16: keys of which float32 lies in the middle of two bf16s and 64 bits do
+    not, where the other bf16 has another code."""
+    rope = Rope(128, interleaved=inter)
+    f = rope.turns.cpu().tolist()
+    g = torch.Generator().manual_seed(3)
+    k = torch.randn(4000, 8, 128, generator=g).to(BF16)
+    y = R.rotate(k, torch.arange(4000), f, 1.0, inter)
+    near = y.float().to(BF16)
+    below = (y.float().view(torch.int32) >> 16).to(torch.int16)
+    straight = torch.where(y.abs() > y.float().double().abs(), below + 1, below).view(BF16)  # of ties
+    tie = (y.float().view(torch.int32) & 0xffff == 0x8000) & (y != y.float().double())
+    rows = [(t, h) for t, h, e in tie.nonzero().tolist()]
+    twice = torch.stack([near[t, h] for t, h in rows])
+    once = torch.stack([torch.where(tie[t, h], straight[t, h], near[t, h]) for t, h in rows])
+    hard = [r for r, a, b in zip(rows, twice, once) if not torch.equal(Q.held(a, Q.BITS[fmt][0]), Q.held(b, Q.BITS[fmt][0]))]
+    assert len(hard) >= 1, "the definition itself has to tell them apart"
+    s = Store(fmt, BF16, 1, 1, 128, 1024, [t + 1 for t, _ in hard], [1] * len(hard), rope, special=False)
+    for i, (t, h) in enumerate(hard):
+        s.k[i, 0] = k[t, h]
+    s.expect(0, f, 1.0, inter)
+    s.att.append(0, s.k.cuda(), s.v.cuda())
+    assert torch.equal(s.cache.k.cpu(), s.pools[0]) and torch.equal(s.cache.v.cpu(), s.pools[1])
 
 
 def fill(cache, tokens, g, slots=None):
