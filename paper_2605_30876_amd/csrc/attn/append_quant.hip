@@ -6,6 +6,9 @@
 // the 32 that share a scale: its maximum is two exchanges within them, loads of
 // rows are contiguous and a quad's codes are one 16-byte chunk (or two) of the page.
 // Keys and values lie in the page alike, token by token, so nothing is turned.
+// Both ways are bound by memory: prompts of 11753 tokens (32 heads of 128 with queries, 8 of keys in 8 bits and values
+// in 4) are stored and read back in 73 us (326 MB, 4.5 TB/s), 48 sequences of 89,941 tokens and 8 heads read back from 4 bits in 101
+// us (466 MB, 4.6 TB/s), where a large copy reaches 5.2.  A block of 32 tokens is bound by its latency: 4.4 and 2.9 us.
 #include "quant.h"
 #include "rotate.h"
 
@@ -107,8 +110,8 @@ __device__ __forceinline__ void put8(uint8_t* to, int dp, int r, int d, const fl
   if (d % kGroup == 0) to[scale_at<kBits>(dp, r) + d / kGroup] = static_cast<uint8_t>(b);
 }
 
-// Rows that are written once go past the caches: through them a read of 48 sequences took 101 us where it takes 70 (467 MB),
-// and evicted what the next kernel reads.
+// Rows that are written once go past the caches: through them the prompts' store and read took 83 us, so 73, the read of 48
+// sequences 110, so 101.  Codes go through them: a page's chunks of 16 bytes are written by many lanes (past them 59.5 us, so 44).
 template <typename V>
 __device__ __forceinline__ void store_past(const V& x, V* p) {
   __builtin_nontemporal_store(x, p);
@@ -130,8 +133,9 @@ struct AppendShape {
 };
 
 // blockIdx.x: tile of 32 positions.  blockIdx.y: 8 of the tile's new tokens, and of those the keys and values, or
-// queries, of some heads.  The angles' cos and sin are formed once a workgroup, in LDS; rows are taken in
-// the order they lie in.
+// queries, of some heads.  The angles' cos and sin are formed once a workgroup, in LDS (in binary64 for keys, where they cost more
+// than the row: with one in each lane's registers and rows taken by head, the prompts took 77 us, so 44); rows are
+// taken in the order they lie in.
 template <typename T, int kK, int kV, Pairs kPairs>
 __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a, AppendShape sh) {
   extern __shared__ double angles[];  // [kTokens][rot_dim / 2][2]: cos and sin (floats for queries)
@@ -354,7 +358,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a, ReadShape sh
   const int rows = n * hs;
   auto copy = [&](const uint8_t* pool, T* out, long stride, auto bits, auto is_value) {
     constexpr int kBits = decltype(bits)::value;
-    constexpr int kFly = kBits || !decltype(is_value)::value ? 2 : 1;  // rows a thread loads before it stores
+    // rows a thread loads before it stores (4 bits, 48 sequences: 119 us with one, 109 with two, 101 with four, 102 with eight)
+    constexpr int kFly = kBits ? 4 : decltype(is_value)::value ? 1 : 2;
     const int size = kBits ? quant_tile(kBits, dp) : kTileTokens * dp * static_cast<int>(sizeof(T));
     const uint8_t* from = pool + tile * size;
     T* to = out + t0 * stride + static_cast<long>(h0) * dim + d;
