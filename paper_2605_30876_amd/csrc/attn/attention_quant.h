@@ -561,7 +561,11 @@ template <typename T, int DP, int kKB, int kVB, int kR>
 constexpr int rows_waves = kParts<T> * DP * kR / 128 + DP * kR / 64 + DP * (kKB + kVB) / 64 < 160 ? 2 : 1;
 
 // Few rows: kR of one kv head per workgroup, its kW waves each on every kW-th key tile, joined through LDS.  Codes go
-// straight into registers, past the caches, the next tile's while one is used.
+// straight into registers, past the caches, the next tile's while one is used.  Bound by those loads: 64 single tokens
+// over 363,063 (32 and 8 heads of 128 in 4 bits, page 64; 396 MB) 85 us, 4.7 TB/s, of which 70 are left with
+// loads alone; one over 131,000 (143 MB) 38 us with plan and merge.  Loads further ahead, or a third wave of a SIMD: as
+// fast; through the caches 98.  For 16 rows eight waves took 94 us, so four.  A block of 32 tokens over 4096, four kv heads of 32 rows by 4: a
+// chain of one load after another, 9.5 us where 7 TB/s would take 1.
 template <typename T, int DP, int kKB, int kVB, int kR, int kW>
 __global__ __launch_bounds__(64 * kW, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   constexpr bool kPin = rows_waves<T, DP, kKB, kVB, kR> == 1;
@@ -714,7 +718,10 @@ constexpr int quant_waves(int dp) {
 
 // Many rows: 128 of one kv head per workgroup, 32 to a wave, all four waves on the same keys.  Codes of kTS tiles
 // are loaded two stages ahead, opened into LDS one stage ahead, each by one of the
-// threads; one barrier a stage.
+// threads; one barrier a stage.  Bound by matrix products and the exponentials between them: 4096 rows of 16 heads of 128
+// over 16384 keys in 4 bits, 525 us, 920 TFLOP/s (a library product 1210; a cache of bf16 490 us).  fp32 rows of 256
+// elements have no room for the queries' parts and spill 460 to 524 bytes a lane, which still beats 32
+// rows a workgroup: 1024 tokens over 4096 260 us, so 306.
 template <typename T, int DP, int kKB, int kVB>
 __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
   typedef QuantStage<DP> Stage;

@@ -1,5 +1,6 @@
 // C ABI of the attention section of dmoe.h: argument validation on the host,
 // then the launchers.
+#include <algorithm>
 #include <cmath>
 
 #include "attn/cache.h"
@@ -261,7 +262,7 @@ dmoe_status dmoe_attention_plan(const dmoe_cache* cache, dmoe_batch batch, int n
   ALIGNED(plan);
   REQUIRE(mask_block >= 0, "mask_block=%d must be >= 0", mask_block);
   const dmoe::AttnShape sh = dmoe::attn_shape(*cache, batch, n_heads);
-  const size_t ints = dmoe::plan_ints(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads);
+  const size_t ints = std::max(dmoe::plan_ints(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads), dmoe::plan_ints(sh));
   REQUIRE(plan_ints >= ints, "a plan of %zu ints is smaller than the %zu needed", plan_ints, ints);
   return hip_status(dmoe::launch_attention_plan(*cache, batch, sh, mask_block, plan, static_cast<hipStream_t>(stream)), __func__);
 }
@@ -285,10 +286,11 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   ALIGNED(workspace);
   ALIGNED_TO(lse, 4);
   const dmoe::AttnShape sh = dmoe::attn_shape(*cache, batch, n_heads);
-  const size_t ints = dmoe::plan_ints(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads);
+  const size_t ints = std::max(dmoe::plan_ints(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads), dmoe::plan_ints(sh));
   REQUIRE(plan_ints >= ints, "a plan of %zu ints is smaller than the %zu needed", plan_ints, ints);
-  const size_t need = dmoe::attn_workspace_bytes(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads,
-                                                 dmoe::padded_dim(cache->head_dim));
+  const int dp = dmoe::padded_dim(cache->head_dim);
+  const size_t need = std::max(dmoe::attn_workspace_bytes(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads, dp),
+                               dmoe::attn_workspace_bytes(sh, cache->n_kv_heads, dp));
   REQUIRE(ws_bytes >= need, "workspace of %zu bytes is smaller than the %zu bytes needed", ws_bytes, need);
   dmoe::AttnArgs a{*cache, layer, batch, n_heads, mask_block, q, q_stride, scale, plan, out, out_stride, lse, workspace};
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -25,7 +25,7 @@ constexpr int kEvenBf16 = 48;
 constexpr int kEvenF32 = 16;
 constexpr int kSplitWide = 256;   // items of eight waves: one a CU
 constexpr int kMinEight = 16;     // their key tiles: two a wave
-constexpr long kFew32 = 128, kFewTiles32 = 128, kFewKeys32 = 20000;
+constexpr long kFew32 = 128, kFewTiles32 = 128, kFewKeys32 = 20000, kFewWork32 = 28000;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
 
 // Largest i with a[i] <= x, for a[0] = 0 <= x < a[n].
@@ -208,7 +208,15 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   if (few && most > 16) {
     AttnShape s = shape(32);
     const long tiles = s.max_tiles * c.n_kv_heads, keys = static_cast<long>(c.max_pages) * c.page_tokens / kTileTokens;
-    if (most <= 32 || (s.max_tiles <= kFew32 && tiles <= kFewTiles32 && tiles * keys <= kFewKeys32)) {
+    // 32 rows to eight waves start sooner than 128 to four and are split further, but read the cache four times as often:
+    // they take sequences of up to 64 rows (8 query and 4 kv heads of 128, us of 32 and of 128: 64 blocks of 32 tokens of up
+    // to 8192 in 4 bits 65/98, in 8 bits 78/96, fp32 in 4 bits 134/223; one over 100,000 40/53), and few row tiles of all kv heads, fewer where one costs more (kFewWork32: by dp and the bf16 parts of a row),
+    // over few keys.  us of 32 and of 128, 4 kv heads in 4 bits over 3000 tokens, 32, 64, 96 row tiles: bf16
+    // 128 elements 21.3/22.8, 23.8/28.0, 26.6/30.5; 256 elements 27.9/31.6, 32.7/35.8, 38.8/41.1, 128 of them 42.6/39.9; fp32
+    // 128 elements 26.4/29.0, 32.8/35.4, 38.8/38.7, 128 of them 44.1/38.8; 256 elements 48.5/53.9, 70.5/68.1, 89.5/82.7.  16
+    // tiles over 4096 tokens in 8 bits, a layer: 15.4/18.8; 256 over up to 8192: 39/33.
+    const long work = tiles * padded_dim(c.head_dim) * (c.dt == DMOE_F32 ? 3 : 1);
+    if (most <= 64 || (s.max_tiles <= kFew32 && tiles <= kFewTiles32 && work <= kFewWork32 && tiles * keys <= kFewKeys32)) {
       s.wide = true;
       s.aim = kSplitWide / c.n_kv_heads > 1 ? kSplitWide / c.n_kv_heads : 1;
       s.split_items = 2 * s.aim;
@@ -244,7 +252,7 @@ size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
   size_t n = 0;
   for (int rows : {32, 64, 128}) {
     const size_t m = plan_ints(shape_of(rows, n_seqs, T, max_new, n_heads, n_kv_heads));
-    n = m > n && (rows > 32 || most_rows(T, max_new, n_heads / n_kv_heads) <= 32) ? m : n;
+    n = m > n && (rows > 32 || most_rows(T, max_new, n_heads / n_kv_heads) <= 64) ? m : n;
   }
   // 32 rows to an item also where there are more of them, but few (attn_shape)
   AttnShape few = shape_of(32, n_seqs, T, max_new, n_heads, n_kv_heads);
@@ -255,6 +263,7 @@ size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
 
 size_t attn_workspace_bytes(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads, int dp) {
   const long most = most_rows(T, max_new, n_heads / n_kv_heads);
+  // what a cache of few bits has of 32 rows where others have 64 or 128 (attn_shape) leaves no more to join
   const int rows = most <= 32 ? 32 : most <= 64 ? 64 : 128;
   return attn_workspace_bytes(shape_of(rows, n_seqs, T, max_new, n_heads, n_kv_heads), n_kv_heads, dp);
 }

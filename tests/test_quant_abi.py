@@ -1,5 +1,7 @@
 """CPU checks of caches of few bits: the plain definition by hand, sizes, the
 Python objects' arrays, and refusals before anything is launched."""
+import ctypes
+import itertools
 import math
 
 import numpy as np
@@ -159,3 +161,21 @@ def test_read_objects():
     att.begin(off)
     with pytest.raises(ValueError):  # rows are of the cache's dtype, not of its pages'
         att.append(0, x.to(torch.uint8), x)
+
+
+@pytest.mark.parametrize("format", [lib.DMOE_KV_PLAIN, lib.DMOE_KV_FP8, lib.DMOE_KV_FP4, lib.DMOE_KV_FP8_FP4])
+@pytest.mark.parametrize("dtype", [lib.DMOE_BF16, lib.DMOE_F32])
+def test_sizes_told_are_the_sizes_needed(L, p, format, dtype):
+    """What the size functions tell, which do not know a cache's format or capacity, is enough for the tiles that a batch is
+    cut into, whatever they are.  (Nothing is launched: there is no GPU.)"""
+    wrong = []
+    for seqs, new, group, kv, dim, pages in itertools.product([1, 2, 40], [1, 8, 20, 32, 500], [1, 2, 3, 4, 16], [1, 2, 8], [64, 256], [8, 1 << 12]):
+        T, heads = seqs * new, group * kv
+        c, b = cache(p, format=format, dt=dtype, n_kv_heads=kv, head_dim=dim, n_slots=seqs, max_pages=pages), batch(p, n_seqs=seqs, T=T, max_new=new)
+        ints = L.dmoe_attention_plan_ints(seqs, T, new, heads, kv)
+        ws = L.dmoe_attention_workspace_size(dtype, seqs, T, new, heads, kv, dim)
+        out = p + T * heads * dim * 4  # behind the queries
+        got = [status(L, "dmoe_attention_plan", ctypes.byref(c), b, heads, 32, p, ints, None),
+               status(L, "dmoe_attention", ctypes.byref(c), 0, b, heads, 32, p, heads * dim, 1.0, p, ints, out, heads * dim, None, p, ws, None)]
+        wrong += [(seqs, new, group, kv, dim, pages, L.dmoe_last_error().decode())] if BAD in got or NO in got else []
+    assert not wrong, wrong[:3]
