@@ -111,7 +111,8 @@ __device__ __forceinline__ void put8(uint8_t* to, int dp, int r, int d, const fl
 }
 
 // Rows that are written once go past the caches: through them the prompts' store and read took 83 us, so 73, the read of 48
-// sequences 110, so 101.  Codes go through them: a page's chunks of 16 bytes are written by many lanes (past them 59.5 us, so 44).
+// sequences 110, so 101.  Codes go through them: a page's chunks of 16 bytes are written by many lanes (past them the store alone 59.5 us, so 44, with
+// the rows in the memory-side cache).
 template <typename V>
 __device__ __forceinline__ void store_past(const V& x, V* p) {
   __builtin_nontemporal_store(x, p);
@@ -134,8 +135,9 @@ struct AppendShape {
 
 // blockIdx.x: tile of 32 positions.  blockIdx.y: 8 of the tile's new tokens, and of those the keys and values, or
 // queries, of some heads.  The angles' cos and sin are formed once a workgroup, in LDS (in binary64 for keys, where they cost more
-// than the row: with one in each lane's registers and rows taken by head, the prompts took 77 us, so 44); rows are
-// taken in the order they lie in.
+// than the row: with one in each lane's registers and rows taken by head, the prompts' store took 77 us, so 44, with their
+// rows in the memory-side cache; 58 without); rows are taken in the order they lie in.  Loading the first of them before the angles
+// are formed took registers, and longer: 76 us with the read, so 74; a block 57.8, so 56.1.
 template <typename T, int kK, int kV, Pairs kPairs>
 __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a, AppendShape sh) {
   extern __shared__ double angles[];  // [kTokens][rot_dim / 2][2]: cos and sin (floats for queries)
