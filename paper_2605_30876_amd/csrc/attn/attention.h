@@ -341,13 +341,15 @@ __device__ __forceinline__ bool load_item(const AttnArgs& a, int i, AttnItem& it
   return i < n;
 }
 
-// The item's rows of this wave: row index, head and what they see.
+// The item's rows of this wave: row index, head and what they see; queries loaded.
 template <typename T, int DP>
 struct RowPlace {
   int row, tok, qh;
   bool live, any;
   template <typename Rows>
   __device__ __forceinline__ RowPlace(Rows& w, const AttnArgs& a, const AttnItem& it, int g, int hk, int row_lo, int lane) {
+    constexpr int c = Types<T>::c;
+    typedef typename Types<T>::Frag Frag;
     const int row_hi = min(row_lo + 32, it.rows) - 1;
     const int pos0 = it.len - it.n;
     row = row_lo + (lane & 31);
@@ -359,15 +361,7 @@ struct RowPlace {
     // the ends grow with the rows; rows past the last are computed and dropped
     w.lo = any ? visible_end(pos0 + row_lo / g, it.len, a.mask_block) : 0;
     w.hi = any ? visible_end(pos0 + row_hi / g, it.len, a.mask_block) : 0;
-  }
-  __device__ __forceinline__ const T* query(const AttnArgs& a, const AttnItem& it) const {
-    return static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
-  }
-  template <typename Rows>
-  __device__ __forceinline__ void load(Rows& w, const AttnArgs& a, const AttnItem& it, int lane) const {
-    constexpr int c = Types<T>::c;
-    typedef typename Types<T>::Frag Frag;
-    const T* qp = query(a, it);
+    const T* qp = static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + static_cast<long>(qh) * a.cache.head_dim;
 #pragma unroll
     for (int j = 0; j < Rows::kK; ++j) {
       const int d = (2 * j + (lane >> 5)) * c;
@@ -410,45 +404,6 @@ struct RowPlace {
   }
 };
 
-// kWK waves' sums over different keys joined, two by two: the upper ones hand theirs to
-// the lower ones (fixed order) through LDS, places first .. first + kWK/2 - 1 of it.
-template <int kWK, int kB, typename Rows>
-__device__ __forceinline__ void join_waves(Rows& w, float* lds, int first, int wk, int lane) {
-  constexpr int kLen = (16 * kB + 2) * 64;
-#pragma unroll
-  for (int n = kWK / 2; n >= 1; n /= 2) {
-    float* buf = lds + (first + wk % n) * kLen;
-    if (wk >= n && wk < 2 * n) {
-      buf[lane] = w.m;
-      buf[64 + lane] = w.l;
-#pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4) =
-              f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
-    }
-    __syncthreads();
-    if (wk < n) {
-      const float om = buf[lane], ol = buf[64 + lane];
-      const float nm = fmaxf(w.m, om);
-      const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = om == nm ? 1.f : exp2_hw(om - nm);
-      w.scale(fa);
-      w.m = nm;
-      w.l += fb * ol;
-#pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
-        }
-    }
-    __syncthreads();
-  }
-}
-
 // Few rows (one token a sequence, a small block): 32 kWR of one kv head per
 // workgroup, 4 / kWR waves to 32 of them, each on every (4 / kWR)-th key tile,
 // joined through LDS.  The cache goes straight into registers, past the caches
@@ -479,7 +434,6 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
   Rows w;
   w.clear();
   const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wr, lane);
-  rows.load(w, a, it, lane);
   if constexpr (kTight) {
     Frag* ql = reinterpret_cast<Frag*>(lds) + wr * (kK * 64) + lane;
     if (wk == 0) {
@@ -563,7 +517,41 @@ __global__ __launch_bounds__(256, waves_per_simd<T>(DP)) void attention_rows_ker
   if (left) w.add_by_key(map, first_masked, kt1, kWK, scale2, half);
   w.l = other_half_sum(w.l);
 
-  join_waves<kWK, kB>(w, lds + (kTight ? kWR * kK * 256 : 0), wr * (kWK / 2), wk, lane);
+  // join the waves two by two: the upper ones hand their sums to the lower
+  // ones (fixed order)
+  constexpr int kLen = (16 * kB + 2) * 64;
+#pragma unroll
+  for (int n = kWK / 2; n >= 1; n /= 2) {
+    float* buf = lds + (kTight ? kWR * kK * 256 : 0) + (wr * (kWK / 2) + wk % n) * kLen;
+    if (wk >= n && wk < 2 * n) {
+      buf[lane] = w.m;
+      buf[64 + lane] = w.l;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4) =
+              f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
+    }
+    __syncthreads();
+    if (wk < n) {
+      const float om = buf[lane], ol = buf[64 + lane];
+      const float nm = fmaxf(w.m, om);
+      const float fa = w.m == nm ? 1.f : exp2_hw(w.m - nm), fb = om == nm ? 1.f : exp2_hw(om - nm);
+      w.scale(fa);
+      w.m = nm;
+      w.l += fb * ol;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 128 + (4 * b + i / 4) * 256 + lane * 4);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) w.o[b][i + t] += fb * x[t];
+        }
+    }
+    __syncthreads();
+  }
   if (wk == 0) rows.store(w, a, sh, it, hk, half, part_rows);
 }
 
@@ -617,7 +605,6 @@ __global__ __launch_bounds__(256 * kWK, waves_per_simd<T>(DP)) void attention_bl
   Rows w;
   w.clear();
   const RowPlace<T, DP> rows(w, a, it, sh.group, hk, it.first + 32 * wave, lane);
-  rows.load(w, a, it, lane);
   const float scale2 = a.scale * kLog2e;
   const TileMap<T, DP> map(a, it.slot, hk);
   // this wave's keys; the first half has at least as many stages

@@ -32,6 +32,11 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// A plan's shape and what kernels divide by.
+struct QuantShape : AttnShape {
+  FastDiv by_group, by_page, by_mask;  // query heads of a kv head, tiles of a page, mask_block (where there is one)
+};
+
 // bf16 parts of a row's queries and probabilities.
 template <typename T>
 constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
@@ -362,7 +367,7 @@ struct QuantPlace {
   int row, tok, qh;
   bool live, any;
   template <typename Rows>
-  __device__ __forceinline__ QuantPlace(Rows& w, const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int hk, int row_lo, int lane) {
+  __device__ __forceinline__ QuantPlace(Rows& w, const AttnArgs& a, const QuantShape& sh, const AttnItem& it, int hk, int row_lo, int lane) {
     row = row_lo + lane % kR;
     live = row < it.rows;
     any = row_lo < it.rows;
@@ -373,7 +378,7 @@ struct QuantPlace {
     w.hi = any ? seen_end(a, sh, it, sh.by_group.of(min(row_lo + kR, it.rows) - 1)) : 0;
   }
   // visible_end of the item's token
-  static __device__ __forceinline__ int seen_end(const AttnArgs& a, const AttnShape& sh, const AttnItem& it, int tok) {
+  static __device__ __forceinline__ int seen_end(const AttnArgs& a, const QuantShape& sh, const AttnItem& it, int tok) {
     const int p = it.len - it.n + tok;
     if (p < 0) return 0;
     if (a.mask_block <= 0) return it.len;
@@ -386,7 +391,7 @@ struct QuantPlace {
   // The row's sums, x(i) elements d(i) .. d(i) + 3 of them for i < kN: divided into out, or as they are into the workspace;
   // with `whole`, what belongs to the row once.
   template <int kN, typename X, typename D>
-  __device__ __forceinline__ void store(X x, D d, float m, float l, bool whole, const AttnArgs& a, const AttnShape& sh, const AttnItem& it,
+  __device__ __forceinline__ void store(X x, D d, float m, float l, bool whole, const AttnArgs& a, const QuantShape& sh, const AttnItem& it,
                                         int hk, int part_rows) const {
     if (!live) return;
     if (it.part >= 0) {
@@ -417,7 +422,7 @@ struct QuantMap {
   long layer0;
   int n_pages, tpp, per_page;  // tiles of a page of one kv head, of all
   FastDiv by_page;
-  __device__ __forceinline__ QuantMap(const AttnArgs& a, const AttnShape& sh, int slot, int hk)
+  __device__ __forceinline__ QuantMap(const AttnArgs& a, const QuantShape& sh, int slot, int hk)
       : n_pages(a.cache.n_pages), tpp(a.cache.page_tokens / kTileTokens), by_page(sh.by_page) {
     table = (const __attribute__((address_space(4))) int32_t*)(a.cache.table + static_cast<long>(slot) * a.cache.max_pages);
     per_page = tpp * a.cache.n_kv_heads;
@@ -513,7 +518,7 @@ __device__ __forceinline__ void add_by_key(Rows& w, const Map& map, int kt, int 
 // The sums of kW waves over different keys joined and stored: every wave lays its own in LDS, then takes an equal share of all.
 // (A tree of pairs had eight waves wait for 3.5 us; code that runs once costs its way into the instruction cache.)
 template <int kW, typename Rows, typename Place>
-__device__ __forceinline__ void join_store(const Rows& w, float* lds, int wave, int lane, const Place& rows, const AttnArgs& a, const AttnShape& sh,
+__device__ __forceinline__ void join_store(const Rows& w, float* lds, int wave, int lane, const Place& rows, const AttnArgs& a, const QuantShape& sh,
                                            const AttnItem& it, int hk, int part_rows) {
   constexpr int kUnits = Rows::kO * Rows::kB / 4, kLen = (4 * kUnits + 2) * 64, kMine = (kUnits + kW - 1) / kW;
   static_assert(Rows::kO == 4 || Rows::kO == 16);
@@ -567,7 +572,7 @@ constexpr int rows_waves = kParts<T> * DP * kR / 128 + DP * kR / 64 + DP * (kKB 
 // fast; through the caches 98.  For 16 rows eight waves took 94 us, so four.  A block of 32 tokens over 4096, four kv heads of 32 rows by 4: a
 // chain of one load after another, 9.5 us where 7 TB/s would take 1.
 template <typename T, int DP, int kKB, int kVB, int kR, int kW>
-__global__ __launch_bounds__(64 * kW, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+__global__ __launch_bounds__(64 * kW, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, QuantShape sh, int part_rows) {
   constexpr bool kPin = rows_waves<T, DP, kKB, kVB, kR> == 1;
   typedef QuantRows<T, DP, kR, kPin> Rows;
   typedef WaveTile<DP, kKB, kVB, kR> Tile;
@@ -723,7 +728,7 @@ constexpr int quant_waves(int dp) {
 // elements have no room for the queries' parts and spill 460 to 524 bytes a lane, which still beats 32
 // rows a workgroup: 1024 tokens over 4096 260 us, so 306.
 template <typename T, int DP, int kKB, int kVB>
-__global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(AttnArgs a, AttnShape sh, int part_rows) {
+__global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(AttnArgs a, QuantShape sh, int part_rows) {
   typedef QuantStage<DP> Stage;
   typedef QuantRows<T, DP, 32, quant_waves<T>(DP) == 1> Rows;
   constexpr int kK = Stage::kK, kTS = Stage::kTS;
@@ -869,13 +874,13 @@ __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(At
 }
 
 template <typename T, int DP, int kKB, int kVB, int kR, int kW>
-void launch_quant_rows(const AttnArgs& a, const AttnShape& sh, unsigned items, int part_rows, hipStream_t s) {
+void launch_quant_rows(const AttnArgs& a, const QuantShape& sh, unsigned items, int part_rows, hipStream_t s) {
   constexpr size_t join = kW * (kR * DP / 64 + 2) * 64 * sizeof(float), values = kW * TurnedValues<DP>::kBytes;
   quant_rows_kernel<T, DP, kKB, kVB, kR, kW><<<items, 64 * kW, join > values ? join : values, s>>>(a, sh, part_rows);
 }
 
 template <typename T, int DP, int kKB, int kVB>
-hipError_t launch_quant_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t s) {
+hipError_t launch_quant_dim(const AttnArgs& a, const QuantShape& sh, hipStream_t s) {
   const int hkv = a.cache.n_kv_heads;
   const unsigned items = static_cast<unsigned>(sh.max_items() * hkv);
   const int part_rows = static_cast<int>(sh.max_parts() * hkv * sh.tile_rows);
@@ -893,10 +898,8 @@ hipError_t launch_quant_dim(const AttnArgs& a, const AttnShape& sh, hipStream_t 
 
 template <typename T, int kKB, int kVB>
 hipError_t launch_attention_quant(const AttnArgs& a, const AttnShape& shape, hipStream_t s) {
-  AttnShape sh = shape;
-  sh.by_group = fast_div(sh.group);
-  sh.by_page = fast_div(a.cache.page_tokens / kTileTokens);
-  sh.by_mask = fast_div(a.mask_block > 0 ? a.mask_block : 1);
+  const attn::QuantShape sh{shape, fast_div(shape.group), fast_div(a.cache.page_tokens / kTileTokens),
+                            fast_div(a.mask_block > 0 ? a.mask_block : 1)};
   switch (padded_dim(a.cache.head_dim)) {
     case 32: return attn::launch_quant_dim<T, 32, kKB, kVB>(a, sh, s);
     case 64: return attn::launch_quant_dim<T, 64, kKB, kVB>(a, sh, s);

@@ -110,8 +110,8 @@ bool rows_overlap(const void* a, long a_stride, const void* b, long b_stride, lo
 }
 
 template <typename T>
-hipError_t attend(const dmoe::AttnArgs& a, const dmoe::AttnShape& sh, hipStream_t s) {
-  switch (a.cache.format) {
+hipError_t attend(dmoe_kv_format format, const dmoe::AttnArgs& a, const dmoe::AttnShape& sh, hipStream_t s) {
+  switch (format) {
     case DMOE_KV_FP8: return dmoe::launch_attention_quant<T, 8, 8>(a, sh, s);
     case DMOE_KV_FP4: return dmoe::launch_attention_quant<T, 4, 4>(a, sh, s);
     case DMOE_KV_FP8_FP4: return dmoe::launch_attention_quant<T, 8, 4>(a, sh, s);
@@ -292,9 +292,9 @@ dmoe_status dmoe_attention(const dmoe_cache* cache, int layer, dmoe_batch batch,
   const size_t need = std::max(dmoe::attn_workspace_bytes(batch.n_seqs, batch.T, batch.max_new, n_heads, cache->n_kv_heads, dp),
                                dmoe::attn_workspace_bytes(sh, cache->n_kv_heads, dp));
   REQUIRE(ws_bytes >= need, "workspace of %zu bytes is smaller than the %zu bytes needed", ws_bytes, need);
-  dmoe::AttnArgs a{*cache, layer, batch, n_heads, mask_block, q, q_stride, scale, plan, out, out_stride, lse, workspace};
+  dmoe::AttnArgs a{dmoe::attn_cache(*cache), layer, batch, n_heads, mask_block, q, q_stride, scale, plan, out, out_stride, lse, workspace};
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return hip_status(cache->dt == DMOE_BF16 ? attend<dmoe::bf16_t>(a, sh, s) : attend<float>(a, sh, s), __func__);
+  return hip_status(cache->dt == DMOE_BF16 ? attend<dmoe::bf16_t>(cache->format, a, sh, s) : attend<float>(cache->format, a, sh, s), __func__);
 }
 
 size_t dmoe_cache_update_workspace_size(int n, int max_pages, int n_pages) {

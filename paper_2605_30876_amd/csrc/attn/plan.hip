@@ -195,7 +195,6 @@ AttnShape shape_of(int tile_rows, int n_seqs, int T, int max_new, int n_heads, i
   s.even_tiles = 0;
   s.wide = false;
   s.unit = 1;
-  s.by_group = s.by_page = s.by_mask = fast_div(1);
   return s;
 }
 
