@@ -66,12 +66,15 @@ def _no_gradient(t: torch.Tensor, name: str):
 
 def _heads(t: torch.Tensor, name: str, rows: int | None, heads: int, dim: int, like: torch.dtype, device) -> torch.Tensor:
     """Checks a step's tensor [rows, heads, dim]: heads and their elements dense, rows any stride."""
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, dim) or (rows is not None and t.shape[0] < rows):
+    shape = t.shape  # a new object each time: small calls are as long as these checks
+    if len(shape) != 3 or shape[2] != dim or shape[1] != heads or (rows is not None and shape[0] < rows):
         raise ValueError(f"{name} must be [{'T' if rows is None else rows}, {heads}, {dim}], not {list(t.shape)}")
     if t.dtype != like or t.device != device:
         raise ValueError(f"{name} must be {like} on {device}, not {t.dtype} on {t.device}")
-    _no_gradient(t, name)
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    if t.requires_grad:
+        _no_gradient(t, name)
+    _, by_head, by_element = t.stride()
+    if by_element != 1 or (heads > 1 and by_head != dim):
         raise ValueError(f"{name}: heads and their elements must be dense (strides {t.stride()})")
     return t
 
@@ -237,21 +240,22 @@ class PagedCache:
         q_offsets[i] .. q_offsets[i+1] receive the tokens from starts[i] on of slot slots[i] (default i), by default its
         last ones (dmoe_cache_read).  Tokens that the sequence does not have are 0, rows of no sequence stay as they
         are.  int32 device tensors; max_tokens: an upper bound of every sequence's tokens (default: every row)."""
-        d, T = self.device, next((t.shape[0] for t in (k, v) if t is not None), None)
-        if T is None:
+        if k is None and v is None:
             raise ValueError("read() needs k or v")
-        n = q_offsets.numel() - 1
+        d, T, n = self.device, (v if k is None else k).shape[0], q_offsets.numel() - 1
         _i32(q_offsets, "q_offsets", d)
         if n < 1:
             raise ValueError("q_offsets must hold a value more than there are sequences")
-        for t, name in ((slots, "slots"), (starts, "starts")):
-            if t is not None:
-                _i32(t, name, d, n)
-        for t, name in ((k, "k"), (v, "v")):
-            if t is not None:
-                _heads(t, name, T, self.n_kv_heads, self.head_dim, self.dtype, d)
-                if t.shape[0] != T:
-                    raise ValueError(f"k and v must have the same rows, not {k.shape[0]} and {v.shape[0]}")
+        if slots is not None:
+            _i32(slots, "slots", d, n)
+        if starts is not None:
+            _i32(starts, "starts", d, n)
+        if k is not None:
+            _heads(k, "k", T, self.n_kv_heads, self.head_dim, self.dtype, d)
+        if v is not None:
+            _heads(v, "v", T, self.n_kv_heads, self.head_dim, self.dtype, d)
+            if v.shape[0] != T:
+                raise ValueError(f"k and v must have the same rows, not {T} and {v.shape[0]}")
         if T == 0:
             return
         with _On(d):
