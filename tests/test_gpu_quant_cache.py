@@ -310,6 +310,36 @@ def test_streams_and_graphs(gpu_lib):
         assert same(k.cpu().double(), Q.held(keys, 8)) and same(v.cpu().double(), Q.held(y.cpu(), 4))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("inter,rot", [(False, 64), (True, 50), (False, 36), (False, 0)])
+def test_columns_of_one_tensor_in_place(gpu_lib, dtype, inter, rot):
+    """Queries turned in place beside their keys and values, enough rows that a workgroup takes several heads, the last one
+    fewer: the bits of a call with tensors of their own, and nothing else touched."""
+    new, heads, kv, dim = [600, 0, 333], 12, 3, 64
+    T, n = sum(new) + 2, len(new)
+    g = torch.Generator().manual_seed(9)
+    wide = torch.randn(T, heads + 2 * kv, dim, generator=g).to(dtype).cuda()
+    before = wide.clone()
+    got = []
+    for fused in (False, True):
+        cache = PagedCache(1, 64, 32, kv, dim, n, 24, dtype=dtype, format="fp8_fp4")
+        cache.resize(i32(list(range(n))), i32([x + 70 for x in new]))
+        att = BlockAttention(cache, heads, n, max(new), T, rope=Rope(rot, interleaved=inter) if rot else None)
+        att.begin(i32([0, 600, 600, 933]))
+        x = wide if fused else before.clone()
+        q, k, v = x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:]
+        if fused:
+            att.append(0, k, v, q)
+            got.append((cache.k, cache.v, q))
+        else:
+            q_out = before[:, :heads].clone()
+            att.append(0, k.contiguous(), v.contiguous(), q.contiguous(), q_out)
+            got.append((cache.k, cache.v, q_out))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert torch.equal(wide[:, heads:], before[:, heads:]) and torch.equal(wide[-2:], before[-2:])
+    assert rot == 0 or not torch.equal(wide[:, :heads], before[:, :heads])
+
+
 def test_far_into_a_large_pool(gpu_lib):
     """Offsets beyond 32 bits: a page behind more than 4 GiB of others."""
     kv, dim, page = 8, 256, 1024
