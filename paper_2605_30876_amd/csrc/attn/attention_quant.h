@@ -559,17 +559,14 @@ __device__ __forceinline__ void join_store(const Rows& w, float* lds, int wave, 
                              m, l, wave == 0 && g == 0, a, sh, it, hk, part_rows);
 }
 
-// Waves of a SIMD in the kernel of few rows: two where a lane's queries, sums and codes leave room for the rest in half of the
-// registers.  64 single tokens of up to 16k, 16 and 4 heads of 256 in 4 bits: 86 us with two, 103 with one; of up to 8k in
-// 8 bits, which do not fit: 205 (spilled) and 96.  Three, where they fit, measured as two.
 template <typename T, int DP, int kKB, int kVB, int kR>
-constexpr int rows_waves = kParts<T> * DP * kR / 128 + DP * kR / 64 + DP * (kKB + kVB) / 64 < 160 ? 2 : 1;
+constexpr int rows_waves = quant_rows_waves(kParts<T>, DP, kKB + kVB, kR);
 
 // Few rows: kR of one kv head per workgroup, its kW waves each on every kW-th key tile, joined through LDS.  Codes go
 // straight into registers, past the caches, the next tile's while one is used.  Bound by those loads: 64 single tokens
 // over 363,063 (32 and 8 heads of 128 in 4 bits, page 64; 396 MB) 85 us, 4.7 TB/s, of which 70 are left with
-// loads alone; one over 131,000 (143 MB) 38 us with plan and merge.  Loads further ahead, or a third wave of a SIMD: as
-// fast; through the caches 98.  For 16 rows eight waves took 94 us, so four.  A block of 32 tokens over 4096, four kv heads of 32 rows by 4: a
+// loads alone; one over 131,000 (143 MB) 37 us with plan and merge.  Loads further ahead, or a third wave of a SIMD: as
+// fast; through the caches 98.  Eight waves take 94 us for the 64, and win where there are few (attn_shape).  A block of 32 tokens over 4096, four kv heads of 32 rows by 4: a
 // chain of one load after another, 9.5 us where 7 TB/s would take 1.
 template <typename T, int DP, int kKB, int kVB, int kR, int kW>
 __global__ __launch_bounds__(64 * kW, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, QuantShape sh, int part_rows) {
@@ -887,6 +884,8 @@ hipError_t launch_quant_dim(const AttnArgs& a, const QuantShape& sh, hipStream_t
   const long most = static_cast<long>(a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) * sh.group;
   if (sh.tile_rows == 128)
     quant_block_kernel<T, DP, kKB, kVB><<<items, 256, 0, s>>>(a, sh, part_rows);
+  else if (most <= 16 && sh.wide)
+    launch_quant_rows<T, DP, kKB, kVB, 16, rows_waves<T, DP, kKB, kVB, 16> == 2 ? 8 : 4>(a, sh, items, part_rows, s);
   else if (most <= 16)
     launch_quant_rows<T, DP, kKB, kVB, 16, 4>(a, sh, items, part_rows, s);
   else

@@ -181,6 +181,12 @@ size_t attn_workspace_bytes(int n_seqs, int T, int max_new, int n_heads, int n_k
 constexpr bool two_per_cu(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ? 4 : 2) <= 256; }
 // and in a cache of few bits, whose products are bf16 and whose fp32 queries take three registers for one
 constexpr bool quant_two_per_cu(dmoe_dtype dt, int dp) { return dp <= (dt == DMOE_F32 ? 64 : 128); }
+// Waves of a SIMD in the kernel of few rows of such a cache: two where a lane's queries (in so many bf16 parts), sums and codes leave
+// room for the rest in half of the registers.  64 single tokens of up to 16k, 16 and 4 heads of 256 in 4 bits: 86 us
+// with two, 103 with one; of up to 8k in 8 bits, which do not fit: 205 (spilled) and 96.  Three, where they fit, measured as two.
+constexpr int quant_rows_waves(int parts, int dp, int bits, int rows) {
+  return parts * dp * rows / 128 + dp * rows / 64 + dp * bits / 64 < 160 ? 2 : 1;
+}
 AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads);
 
 inline size_t plan_ints(const AttnShape& s) {

@@ -26,6 +26,7 @@ constexpr int kEvenF32 = 16;
 constexpr int kSplitWide = 256;   // items of eight waves: one a CU
 constexpr int kMinEight = 16;     // their key tiles: two a wave
 constexpr long kFew32 = 128, kFewTiles32 = 128, kFewKeys32 = 20000, kFewWork32 = 28000;
+constexpr long kFewTiles16 = 64, kFewKeys16 = 256;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
 
 // Largest i with a[i] <= x, for a[0] = 0 <= x < a[n].
@@ -204,18 +205,24 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   const long most = most_rows(b.T, b.max_new, n_heads / c.n_kv_heads);
   auto shape = [&](int rows) { return shape_of(rows, b.n_seqs, b.T, b.max_new, n_heads, c.n_kv_heads); };
   const bool few = c.format != DMOE_KV_PLAIN;  // bits: bf16 products, whatever the rows
-  if (few && most > 16) {
+  if (few) {
     AttnShape s = shape(32);
     const long tiles = s.max_tiles * c.n_kv_heads, keys = static_cast<long>(c.max_pages) * c.page_tokens / kTileTokens;
-    // 32 rows to eight waves start sooner than 128 to four and are split further, but read the cache four times as often:
-    // they take sequences of up to 64 rows (8 query and 4 kv heads of 128, us of 32 and of 128: 64 blocks of 32 tokens of up
-    // to 8192 in 4 bits 65/98, in 8 bits 78/96, fp32 in 4 bits 134/223; one over 100,000 40/53), and few row tiles of all kv heads, fewer where one costs more (kFewWork32: by dp and the bf16 parts of a row),
-    // over few keys.  us of 32 and of 128, 4 kv heads in 4 bits over 3000 tokens, 32, 64, 96 row tiles: bf16
-    // 128 elements 21.3/22.8, 23.8/28.0, 26.6/30.5; 256 elements 27.9/31.6, 32.7/35.8, 38.8/41.1, 128 of them 42.6/39.9; fp32
-    // 128 elements 26.4/29.0, 32.8/35.4, 38.8/38.7, 128 of them 44.1/38.8; 256 elements 48.5/53.9, 70.5/68.1, 89.5/82.7.  16
-    // tiles over 4096 tokens in 8 bits, a layer: 15.4/18.8; 256 over up to 8192: 39/33.
-    const long work = tiles * padded_dim(c.head_dim) * (c.dt == DMOE_F32 ? 3 : 1);
-    if (most <= 64 || (s.max_tiles <= kFew32 && tiles <= kFewTiles32 && work <= kFewWork32 && tiles * keys <= kFewKeys32)) {
+    // 32 rows to eight waves start sooner than 128 to four and are split further, but read the cache four times as often: they
+    // take sequences of up to 64 rows (8 query and 4 kv heads of 128, us of 32 and of 128: 64 blocks of 32 tokens of up to 8192 in 4
+    // bits 65/98, in 8 bits 78/96, fp32 in 4 bits 134/223; one over 100,000 40/53), and few row tiles of all kv heads over few
+    // keys, fewer where one costs more (kFewWork32: by dp and the bf16 parts of a row).  us of 32 and of 128, 4 kv heads in 4 bits over
+    // 3000 tokens, 32, 64, 96 row tiles: bf16 128 elements 21.3/22.8, 23.8/28.0, 26.6/30.5; 256 elements 27.9/31.6, 32.7/35.8,
+    // 38.8/41.1, 128 of them 42.6/39.9; fp32 128 elements 26.4/29.0, 32.8/35.4, 38.8/38.7, 128 of them 44.1/38.8; 256 elements
+    // 48.5/53.9, 70.5/68.1, 89.5/82.7.  16 tiles over 4096 tokens in 8 bits, a layer: 15.4/18.8; 256 over up to 8192: 39/33.
+    // 16 rows: to four waves, or to eight, which have half of the partial results to join but start later, where row tiles are few
+    // and may be long.  us of four and of eight, 4 bits, 32 and 8 heads of 128, in a graph: one token over 1000 keys 19.4/20.3, 4096
+    // 20.5/20.9, 16,000 25.3/23.2, 32,000 28.5/26.3, 131,000 38.8/36.8 (not a graph); 8 over 8192 22.7/21.8, 16 32.6/33.9; 16 and 4
+    // heads of 256 over 32,000 42.7/34.4.  Where eight do not fit (quant_rows_waves), four: 73.1/74.4.
+    const int parts = c.dt == DMOE_F32 ? 3 : 1, dp = padded_dim(c.head_dim);
+    const bool few16 = tiles <= kFewTiles16 && keys >= kFewKeys16 && quant_rows_waves(parts, dp, key_bits(c.format) + value_bits(c.format), 16) == 2;
+    const long work = tiles * dp * parts;
+    if (most <= 16 ? few16 : most <= 64 || (s.max_tiles <= kFew32 && tiles <= kFewTiles32 && work <= kFewWork32 && tiles * keys <= kFewKeys32)) {
       s.wide = true;
       s.aim = kSplitWide / c.n_kv_heads > 1 ? kSplitWide / c.n_kv_heads : 1;
       s.split_items = 2 * s.aim;

@@ -182,6 +182,28 @@ def test_what_rows_do_not_see(gpu_lib, fmt, dtype, heads, capacity, dim):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("capacity,dim", [(0, 64), (1 << 14, 64), (1 << 14, 128), (1 << 14, 256)])
+def test_what_few_rows_do_not_see(gpu_lib, fmt, dtype, capacity, dim):
+    """As above with 16 rows or fewer to a workgroup, of four waves and, where sequences may be long, of eight."""
+    s = Setup(fmt, dtype, 2, 2, dim, 32, [900, 30], [12, 3], 1, capacity=capacity)
+    s.check(*s.run())
+    spoil(s, 1, 0, 893, 0, 255)
+    spoil(s, 0, 0, 895, 1, 255)
+    out, lse = s.run()
+    rows, ref, (tol, ltol) = s.reference(0)
+    for t in range(12):
+        for h, first in ((0, 893), (1, 895)):
+            if 888 + t >= first:
+                assert bool(out[t, h].isnan().any())
+            else:
+                assert bool(((out[t, h].double() - ref[0][t, h]).abs() <= tol[t, h]).all()), (t, h)
+    assert bool(((lse[:12, 0].double() - ref[1][:, 0]).abs() <= ltol[:, 0]).all())
+    rows, ref, (tol, ltol) = s.reference(1)
+    assert bool(((out[rows].double() - ref[0]).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("group", [1, 2, 4])
 def test_pages_that_are_not_there(gpu_lib, fmt, group):
     """Ids outside the pool are never followed: no key is seen there."""
