@@ -907,7 +907,7 @@ constexpr long kMergeGrid = 1024;
 template <typename T, int DP>
 hipError_t launch_merge(const AttnArgs& a, const AttnShape& sh, int part_rows, hipStream_t s) {
   // no sequence is long enough to be split: nothing to join
-  if (static_cast<long>(a.cache.max_pages) * a.cache.page_tokens <= static_cast<long>(sh.min_tiles) * kTileTokens) return hipGetLastError();
+  if (static_cast<long>(a.cache.max_pages) * a.cache.page_tokens <= static_cast<long>(sh.whole_tiles) * kTileTokens) return hipGetLastError();
   const long units = sh.split_items * a.cache.n_kv_heads * (sh.tile_rows / kMergeRows);
   attention_merge_kernel<T, DP><<<static_cast<unsigned>(units < kMergeGrid ? units : kMergeGrid), 64 * kMergeWaves, 0, s>>>(a, sh, part_rows);
   return hipGetLastError();

@@ -565,7 +565,7 @@ constexpr int rows_waves = quant_rows_waves(kParts<T>, DP, kKB + kVB, kR);
 // Few rows: kR of one kv head per workgroup, its kW waves each on every kW-th key tile, joined through LDS.  Codes go
 // straight into registers, past the caches, the next tile's while one is used.  Bound by those loads: 64 single tokens
 // over 363,063 (32 and 8 heads of 128 in 4 bits, page 64; 396 MB) 85 us, 4.7 TB/s, of which 70 are left with
-// loads alone; one over 131,000 (143 MB) 37 us with plan and merge.  Loads further ahead, or a third wave of a SIMD: as
+// loads alone; one over 131,000 (143 MB) 35 us with plan and merge.  Loads further ahead, or a third wave of a SIMD: as
 // fast; through the caches 98.  Eight waves take 94 us for the 64, and win where there are few (attn_shape).  A block of 32 tokens over 4096, four kv heads of 32 rows by 4: a
 // chain of one load after another, 9.5 us where 7 TB/s would take 1.
 template <typename T, int DP, int kKB, int kVB, int kR, int kW>

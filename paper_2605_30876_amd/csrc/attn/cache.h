@@ -163,6 +163,7 @@ struct AttnShape {
   int group;       // query heads of a kv head
   int tile_rows;   // rows of an item
   int min_tiles;   // key tiles of an item at least, where rows are split
+  int whole_tiles; // key tiles that are not split
   long max_tiles;  // row tiles of the batch at most
   long split_items;  // items that splitting along the keys may add, and merges, at most
   int aim;           // items that splitting aims at: at most split_items

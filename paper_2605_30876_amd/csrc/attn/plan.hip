@@ -24,7 +24,9 @@ constexpr int kMinWide = 8;
 constexpr int kEvenBf16 = 48;
 constexpr int kEvenF32 = 16;
 constexpr int kSplitWide = 256;   // items of eight waves: one a CU
-constexpr int kMinEight = 16;     // their key tiles: two a wave
+// Their key tiles: one or two a wave (a block over 4096 tokens, eight layers: 118.7 us with 12, 121.5 with 10, 122.7 with 16), but
+// up to kWholeEight stay with one (a block over 400: 20.0 us in two pieces, which have to be joined, 17.1 in one).
+constexpr int kMinEight = 12, kWholeEight = 20;
 constexpr long kFew32 = 128, kFewTiles32 = 128, kFewKeys32 = 20000, kFewWork32 = 28000;
 constexpr long kFewTiles16 = 64, kFewKeys16 = 256;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
@@ -127,6 +129,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   if (sh.tile_rows == 128 && many && 10l * longest * n_tiles > 13 * all)
     len = min(len, max(static_cast<long>(sh.even_tiles), (all + 2 * split - 1) / (2 * split)));
   const int chunk = static_cast<int>(len);
+  auto pieces_of = [&](int kt) { return kt <= sh.whole_tiles ? 1 : (kt + chunk - 1) / chunk; };
 
   AttnPlanHead* head = reinterpret_cast<AttnPlanHead*>(plan);
   AttnItem* out = reinterpret_cast<AttnItem*>(head + 1);
@@ -134,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
   int n_items = 0, n_parts = 0, n_merges = 0;
   for (int t0 = 0; t0 < n_tiles; t0 += kThreads) {
     if (t0 > 0) r = load_tile(t0 + tid);
-    const int pieces = t0 + tid < n_tiles ? max(1, (r.kt + chunk - 1) / chunk) : 0;
+    const int pieces = t0 + tid < n_tiles ? pieces_of(r.kt) : 0;
     tile[tid] = r;
     // three sums at once, 21 bits each: a pass has at most kThreads + split items
     const long mine = pieces | (pieces > 1 ? static_cast<long>(pieces) << 21 | 1l << 42 : 0);
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(dmoe_cache c, dmoe_batch
     for (int x = tid; x < total; x += kThreads) {
       const int j = find(items, kThreads, x);
       const Tile& u = tile[j];
-      const int p = x - items[j], n = max(1, (u.kt + chunk - 1) / chunk);
+      const int p = x - items[j], n = pieces_of(u.kt);
       AttnItem it{u.q.slot, u.q.row0, u.q.n, u.q.len, u.first, u.rows, 0, 0, parts[j] < 0 ? -1 : parts[j] + p, {}, 0};
       const long units = (u.kt + sh.unit - 1) / sh.unit;
       it.kt0 = static_cast<int>(units * p / n) * sh.unit;
@@ -193,6 +196,7 @@ AttnShape shape_of(int tile_rows, int n_seqs, int T, int max_new, int n_heads, i
   // twice the aim where the plan may go for it: always with 32 rows, with 128 where it may find many row tiles
   s.split_items = tile_rows == 32 || (tile_rows == 128 && s.max_tiles > s.aim / 2) ? 2 * s.aim : s.aim;
   s.min_tiles = tile_rows == 32 ? kMinRows : tile_rows == 64 ? kMinTwo : kMinBlock;
+  s.whole_tiles = s.min_tiles;
   s.even_tiles = 0;
   s.wide = false;
   s.unit = 1;
@@ -227,6 +231,7 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
       s.aim = kSplitWide / c.n_kv_heads > 1 ? kSplitWide / c.n_kv_heads : 1;
       s.split_items = 2 * s.aim;
       s.min_tiles = kMinEight;
+      s.whole_tiles = kWholeEight;
       return s;
     }
   }
@@ -248,7 +253,7 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
   const bool half = few ? quant_two_per_cu(c.dt, dp) : two_per_cu(c.dt, dp);
   s.wide = !few && half && s.max_tiles * c.n_kv_heads < kSplitBlock / 2;
   if (!half || s.wide) s.aim = s.aim > 1 ? s.aim / 2 : 1;
-  if (s.wide) s.min_tiles = kMinWide;
+  if (s.wide) s.min_tiles = s.whole_tiles = kMinWide;
   s.even_tiles = c.dt == DMOE_F32 && !few ? kEvenF32 : kEvenBf16;
   s.unit = stage_tiles(few ? DMOE_BF16 : c.dt, dp);
   return s;
