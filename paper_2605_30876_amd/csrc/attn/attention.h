@@ -32,6 +32,10 @@ __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
   *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4);
 }
 
+// A row's sums over the sum of its probabilities.  Where that is 0 (`some` false) the row is 0 whatever they are: a
+// probability of 0 times a value that is not finite has made them NaN.
+__device__ __forceinline__ f32x4 divided(const f32x4& o, bool some, float inv) { return some ? o * inv : f32x4{0.f, 0.f, 0.f, 0.f}; }
+
 // c: values of a 16-byte chunk; a matrix operand (1 KiB, one chunk per lane)
 // covers 2c elements of the head dimension (keys) or 2c tokens (values).
 template <typename T>
@@ -397,7 +401,7 @@ struct RowPlace {
       for (int i = 0; i < 16; i += 4) {
         const int d = 32 * b + tile_key(i, half);
         if (d < a.cache.head_dim)
-          store4(op + d, f32x4{w.o[b][i] * inv, w.o[b][i + 1] * inv, w.o[b][i + 2] * inv, w.o[b][i + 3] * inv});
+          store4(op + d, divided(f32x4{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]}, some, inv));
       }
     if (a.lse && half == 0)
       a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = some ? (w.m + log2f(w.l)) * kLn2 : -INFINITY;
@@ -896,7 +900,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attention_merge_kernel(AttnA
     T* op = static_cast<T*>(a.out) + (mg.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim + col * 4;
 #pragma unroll
     for (int j = 0; j < kV; ++j)
-      if (32 * j + col * 4 < a.cache.head_dim) store4(op + 32 * j, o[j] * inv);
+      if (32 * j + col * 4 < a.cache.head_dim) store4(op + 32 * j, divided(o[j], some, inv));
     if (a.lse && col == 0)
       a.lse[static_cast<long>(mg.row0 + tok) * a.n_heads + qh] = some ? (mm + log2f(l)) * kLn2 : -INFINITY;
   } while ((u += gridDim.x) < units);

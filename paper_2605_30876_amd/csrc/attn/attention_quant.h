@@ -408,7 +408,7 @@ struct QuantPlace {
     T* op = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + static_cast<long>(qh) * a.cache.head_dim;
 #pragma unroll
     for (int i = 0; i < kN; ++i)
-      if (d(i) < a.cache.head_dim) store4(op + d(i), x(i) * inv);
+      if (d(i) < a.cache.head_dim) store4(op + d(i), divided(x(i), some, inv));
     if (whole && a.lse) a.lse[static_cast<long>(it.row0 + tok) * a.n_heads + qh] = some ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
 };

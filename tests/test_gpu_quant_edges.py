@@ -1,0 +1,60 @@
+"""Attention over caches of few bits, and of none, where the other tests do not go: rows whose scores are all -inf.  Marked ``gpu``."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as R
+from paper_2605_30876_amd.attention import BlockAttention, PagedCache
+from test_gpu_quant_attention import BF16, F32, FORMATS, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", ["plain"] + FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group,new,capacity", [(1, 3, 0), (1, 3, 1 << 14), (1, 24, 0), (4, 12, 0), (4, 40, 0), (4, 40, 1 << 17)])
+@pytest.mark.parametrize("lens", [[40, 60], [900, 60]])
+def test_rows_whose_scores_are_all_minus_infinity(gpu_lib, fmt, dtype, group, new, capacity, lens):
+    """They are 0 with log-sum-exp -inf, also where they see values that are not finite, in every form and joined from pieces;
+    the rows beside them are the definition's."""
+    kv, dim, heads = 2, 64, 2 * group
+    g = torch.Generator().manual_seed(11)
+    width = max(max(lens) // 32 + 2, capacity // 32)
+    cache = PagedCache(1, sum(lens) // 32 + 8, 32, kv, dim, 2, width, dtype=dtype, format=fmt)
+    cache.resize(i32([0, 1]), i32(lens))
+    k, v = (torch.randn(sum(lens), kv, dim, generator=g) for _ in range(2))
+    k[:, :, 0] = 2.0 + k[:, :, 0].abs()  # never rounded to 0: largest of its group, or a quarter of it at least
+    k[:, :, 1:32] = k[:, :, 1:32].clamp(-2, 2)
+    v[7, 0, 3] = math.inf
+    v[20, 1, 40] = math.nan
+    fill = BlockAttention(cache, kv, 2, max(lens), sum(lens))
+    fill.begin(i32([0, lens[0], sum(lens)]))
+    fill.append(0, k.to(dtype).cuda(), v.to(dtype).cuda())
+    q = torch.randn(2 * new, heads, dim, generator=g)
+    q[::2] = 0.0
+    q[::2, :, 0] = -3e38
+    q = q.to(dtype)
+    att = BlockAttention(cache, heads, 2, new, 2 * new)
+    att.begin(i32([0, new, 2 * new]))
+    att.plan()
+    lse = torch.full((2 * new, heads), 7.0, device="cuda")
+    out = att.attend(0, q.cuda(), lse=lse).cpu()
+    assert bool((out[::2] == 0).all()) and bool((lse[::2] == -math.inf).all())
+    held = [torch.zeros(sum(lens), kv, dim, dtype=dtype, device="cuda") for _ in range(2)]
+    cache.read(0, i32([0, lens[0], sum(lens)]), *held)
+    held = [x.cpu() for x in held]
+    parts = 3 if dtype == F32 and fmt != "plain" else 1
+    for i, at in enumerate((slice(0, lens[0]), slice(lens[0], sum(lens)))):
+        rows = torch.arange(i * new, (i + 1) * new)
+        rows = rows[rows % 2 == 1]
+        # a sum with a NaN is NaN, which the bounds leave out: the first sequence's values of the elements that are finite
+        vv = held[1][at].clone()
+        bad = ~vv.isfinite().all(0)
+        vv[:, bad] = 0
+        ref = R.attention(q[rows], held[0][at], vv, [lens[i]] * len(rows), 1 / math.sqrt(dim))
+        tol, ltol = R.bounds(dtype, parts * dim, parts * lens[i], *ref)
+        bad = bad.repeat_interleave(group, 0)[None].expand(len(rows), -1, -1)
+        err = (out[rows].double() - ref[0]).abs()
+        assert bool((err[~bad] <= tol[~bad]).all()) and bool((~out[rows][bad].isfinite()).all())
+        assert bool(((lse[rows].cpu().double() - ref[1]).abs() <= ltol).all())
