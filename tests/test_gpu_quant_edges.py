@@ -1,14 +1,46 @@
-"""Attention over caches of few bits, and of none, where the other tests do not go: rows whose scores are all -inf.  Marked ``gpu``."""
+"""Attention over caches of few bits, and of none, where the other tests do not go: 16 rows or fewer at every width of a head,
+rows whose scores are all -inf, what the bytes of codes and scales stand for, results that repeat.  Marked ``gpu``."""
 import math
 
 import pytest
 import torch
 
 import attention_ref as R
+import quant_ref as Q
 from paper_2605_30876_amd.attention import BlockAttention, PagedCache
-from test_gpu_quant_attention import BF16, F32, FORMATS, i32
+from test_gpu_quant_attention import BF16, F32, FORMATS, Setup, i32, spoil
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [8, 32, 64, 80, 96, 128, 160, 192, 256])
+@pytest.mark.parametrize("capacity", [0, 1 << 14])
+@pytest.mark.parametrize("group,new", [(1, [12, 3]), (4, [4, 1])])
+def test_few_rows_of_every_width(gpu_lib, fmt, dtype, dim, capacity, group, new):
+    """16 rows of a kv head to a workgroup of four waves and, where sequences may be long, of eight, split along the keys or not."""
+    s = Setup(fmt, dtype, 2 * group, 2, dim, 32, [900, 30], new, 1, capacity=capacity)
+    s.check(*s.run())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("capacity", [0, 1 << 14])
+@pytest.mark.parametrize("dim", [32, 80, 96, 192])
+def test_what_few_rows_of_other_widths_do_not_see(gpu_lib, fmt, dtype, capacity, dim):
+    s = Setup(fmt, dtype, 2, 2, dim, 32, [900, 30], [12, 3], 1, capacity=capacity)
+    spoil(s, 1, 0, 893, 0, 255)
+    spoil(s, 0, 0, 895, 1, 255)
+    out, lse = s.run()
+    rows, ref, (tol, ltol) = s.reference(0)
+    for t in range(12):
+        for h, first in ((0, 893), (1, 895)):
+            if 888 + t >= first:
+                assert bool(out[t, h].isnan().any())
+            else:
+                assert bool(((out[t, h].double() - ref[0][t, h]).abs() <= tol[t, h]).all()), (t, h)
+    assert bool(((lse[:12, 0].double() - ref[1][:, 0]).abs() <= ltol[:, 0]).all())
 
 
 @pytest.mark.parametrize("fmt", ["plain"] + FORMATS)
@@ -58,3 +90,32 @@ def test_rows_whose_scores_are_all_minus_infinity(gpu_lib, fmt, dtype, group, ne
         err = (out[rows].double() - ref[0]).abs()
         assert bool((err[~bad] <= tol[~bad]).all()) and bool((~out[rows][bad].isfinite()).all())
         assert bool(((lse[rows].cpu().double() - ref[1]).abs() <= ltol).all())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_results_repeat_in_every_form(gpu_lib, fmt, dtype):
+    for group, new, lens, capacity in ((2, 1, [3000, 70], 0), (2, 1, [3000, 70], 1 << 14), (2, 20, [3000, 70], 0), (4, 32, [2000, 64], 0),
+                                       (4, 40, [2000, 64], 1 << 17)):
+        s = Setup(fmt, dtype, 2 * group, 2, 128, 32, lens, [new, new], 32, capacity=capacity)
+        first = s.run()
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(first, s.run()))
+
+
+@pytest.mark.parametrize("fmt,bits", [("fp8", 8), ("fp4", 4)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_what_every_byte_stands_for(gpu_lib, fmt, bits, dtype):
+    """Every code at every scale byte, also those that are never stored, in arrays that were given: code times scale, rounded to bf16."""
+    dim, n = 256, 256
+    codes = (torch.arange(dim) % (1 << bits)).repeat(n, 1, 1)
+    scales = torch.arange(n)[:, None, None].expand(n, 1, dim // 32)
+    pool = torch.zeros(Q.page_bytes(bits, n, 1, dim), dtype=torch.uint8)
+    Q.put(pool, bits, n, dim, torch.arange(n), torch.zeros(n), codes, scales)
+    given = [pool.view(1, 1, -1).cuda() for _ in range(2)]
+    cache = PagedCache(1, 1, n, 1, dim, 1, 1, dtype=dtype, k=given[0], v=given[1], table=i32([[0]]), lens=i32([n]), format=fmt)
+    got = [torch.full((n, 1, dim), 7.0, dtype=dtype, device="cuda") for _ in range(2)]
+    cache.read(0, i32([0, n]), *got)
+    want = Q.values(codes, scales, bits).to(BF16).to(dtype)
+    for x in got:
+        assert bool(((x.cpu() == want) | (x.cpu().isnan() & want.isnan())).all())
