@@ -259,7 +259,7 @@ class PagedCache:
         if T == 0:
             return
         with _On(d):
-            batch = lib.dmoe_batch(lib.ptr(q_offsets), lib.ptr(slots), n, T, T if max_tokens is None else max_tokens)
+            batch = lib.dmoe_batch(lib.ptr(q_offsets), lib.ptr(slots), n, T, T if max_tokens is None else min(max_tokens, T))
             lib.dmoe_cache_read(self.c, layer, batch, starts, k, v, stream)
 
     def copy_pages(self, pairs: torch.Tensor, stream=None):

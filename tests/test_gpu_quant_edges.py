@@ -119,3 +119,18 @@ def test_what_every_byte_stands_for(gpu_lib, fmt, bits, dtype):
     want = Q.values(codes, scales, bits).to(BF16).to(dtype)
     for x in got:
         assert bool(((x.cpu() == want) | (x.cpu().isnan() & want.isnan())).all())
+
+
+@pytest.mark.parametrize("fmt", ["plain"] + FORMATS)
+def test_a_bound_of_any_size(gpu_lib, fmt):
+    """An upper bound of a read's tokens may be any number that is large enough."""
+    cache = PagedCache(1, 4, 32, 2, 64, 1, 4, format=fmt)
+    cache.resize(i32([0]), i32([70]))
+    att = BlockAttention(cache, 2, 1, 70, 70)
+    att.begin(i32([0, 70]))
+    x = torch.randn(70, 2, 64, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    att.append(0, x, x)
+    got = [torch.zeros_like(x) for _ in range(3)]
+    for y, most in zip(got, (None, 70, 1 << 40)):
+        cache.read(0, i32([0, 70]), y, max_tokens=most)
+    assert bool((got[0] != 0).any()) and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
