@@ -65,7 +65,8 @@ def _no_gradient(t: torch.Tensor, name: str):
 
 
 def _heads(t: torch.Tensor, name: str, rows: int | None, heads: int, dim: int, like: torch.dtype, device) -> torch.Tensor:
-    """Checks a step's tensor [rows, heads, dim]: heads and their elements dense, rows any stride."""
+    """Checks a step's tensor [rows, heads, dim]: heads and their elements dense, rows any stride.  Returns it, a single row with
+    the stride of dense ones (it may have any, which says nothing)."""
     shape = t.shape  # a new object each time: small calls are as long as these checks
     if len(shape) != 3 or shape[2] != dim or shape[1] != heads or (rows is not None and shape[0] < rows):
         raise ValueError(f"{name} must be [{'T' if rows is None else rows}, {heads}, {dim}], not {list(t.shape)}")
@@ -73,9 +74,11 @@ def _heads(t: torch.Tensor, name: str, rows: int | None, heads: int, dim: int, l
         raise ValueError(f"{name} must be {like} on {device}, not {t.dtype} on {t.device}")
     if t.requires_grad:
         _no_gradient(t, name)
-    _, by_head, by_element = t.stride()
+    by_row, by_head, by_element = t.stride()
     if by_element != 1 or (heads > 1 and by_head != dim):
         raise ValueError(f"{name}: heads and their elements must be dense (strides {t.stride()})")
+    if (by_row < heads * dim or by_row % 8) and shape[0] == 1:
+        return t.as_strided(shape, (heads * dim, dim, 1))
     return t
 
 
@@ -100,13 +103,14 @@ class Rope:
         """x [T, heads, dim] rotated at positions [T] (int32) into out (default: x itself).  inverse: the gradient
         of a forward call with respect to x, given the gradient of its output."""
         T, heads, dim = x.shape
-        _heads(x, "x", T, heads, dim, x.dtype, self.turns.device)
-        out = x if out is None else _heads(out, "out", T, heads, dim, x.dtype, x.device)
+        row = _heads(x, "x", T, heads, dim, x.dtype, self.turns.device)
+        to = row if out is None else _heads(out, "out", T, heads, dim, x.dtype, x.device)
+        out = x if out is None else out
         if T == 0:
             return out
         _i32(positions, "positions", x.device, T)
         with _On(x.device):
-            lib.dmoe_rope(x, out, T, heads, dim, positions, self.c, inverse, stream)
+            lib.dmoe_rope(row, to, T, heads, dim, positions, self.c, inverse, stream)
         return out
 
 
@@ -251,9 +255,9 @@ class PagedCache:
         if starts is not None:
             _i32(starts, "starts", d, n)
         if k is not None:
-            _heads(k, "k", T, self.n_kv_heads, self.head_dim, self.dtype, d)
+            k = _heads(k, "k", T, self.n_kv_heads, self.head_dim, self.dtype, d)
         if v is not None:
-            _heads(v, "v", T, self.n_kv_heads, self.head_dim, self.dtype, d)
+            v = _heads(v, "v", T, self.n_kv_heads, self.head_dim, self.dtype, d)
             if v.shape[0] != T:
                 raise ValueError(f"k and v must have the same rows, not {T} and {v.shape[0]}")
         if T == 0:
@@ -327,10 +331,10 @@ class BlockAttention:
         """Stores the new keys (rotated) and values [T, n_kv_heads, head_dim] and rotates q [T, n_heads, head_dim]
         into q_out (default: q itself)."""
         c = self.cache
-        _heads(k, "k", self.T, c.n_kv_heads, c.head_dim, c.dtype, c.device)
-        _heads(v, "v", self.T, c.n_kv_heads, c.head_dim, c.dtype, c.device)
+        k = _heads(k, "k", self.T, c.n_kv_heads, c.head_dim, c.dtype, c.device)
+        v = _heads(v, "v", self.T, c.n_kv_heads, c.head_dim, c.dtype, c.device)
         if q is not None:
-            _heads(q, "q", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
+            q = _heads(q, "q", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
             q_out = q if q_out is None else _heads(q_out, "q_out", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
         elif q_out is not None:
             raise ValueError("q_out needs q")
@@ -343,19 +347,19 @@ class BlockAttention:
         """Attention of the (rotated) queries over the cache, into out [T, n_heads, head_dim] (default: a new tensor,
         allocated on the call's stream); lse [T, n_heads] (float32) receives the log-sum-exp of every row."""
         c = self.cache
-        _heads(q, "q", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
+        q = _heads(q, "q", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
         if out is None:
             with _stream(stream):
-                out = torch.empty_like(q)
+                out = to = torch.empty_like(q)
         else:
-            _heads(out, "out", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
+            to = _heads(out, "out", self.T, self.n_heads, c.head_dim, c.dtype, c.device)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < self.T * self.n_heads
                                 or lse.device != c.device):
             raise ValueError(f"lse must be contiguous float32 [{self.T}, {self.n_heads}] on {c.device}")
         if not self._planned:
             raise RuntimeError("plan() has not been called since begin()")
         with _On(c.device):
-            lib.dmoe_attention(c.c, layer, self._started(), self.n_heads, self.mask_block, q, self.scale, self._plan, out, lse,
+            lib.dmoe_attention(c.c, layer, self._started(), self.n_heads, self.mask_block, q, self.scale, self._plan, to, lse,
                                self.workspace, stream)
         return out
 

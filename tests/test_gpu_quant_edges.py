@@ -7,7 +7,7 @@ import torch
 
 import attention_ref as R
 import quant_ref as Q
-from paper_2605_30876_amd.attention import BlockAttention, PagedCache
+from paper_2605_30876_amd.attention import BlockAttention, PagedCache, Rope
 from test_gpu_quant_attention import BF16, F32, FORMATS, Setup, i32, spoil
 
 pytestmark = pytest.mark.gpu
@@ -134,3 +134,30 @@ def test_a_bound_of_any_size(gpu_lib, fmt):
     for y, most in zip(got, (None, 70, 1 << 40)):
         cache.read(0, i32([0, 70]), y, max_tokens=most)
     assert bool((got[0] != 0).any()) and torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("fmt", ["plain"] + FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_one_row_of_any_stride(gpu_lib, fmt, dtype):
+    """The distance between rows of a tensor that has one row says nothing: views [1, heads, dim] of heads that lie one after
+    another are taken like any others."""
+    heads, kv, dim = 4, 2, 64
+    g = torch.Generator().manual_seed(2)
+    rows = [torch.randn(h, 1, dim, generator=g).to(dtype).cuda() for h in (kv, kv, heads)]
+    rope, got = Rope(dim), []
+    for flip in (False, True):
+        new = lambda h: torch.zeros(h, 1, dim, dtype=dtype, device="cuda").transpose(0, 1) if flip else torch.zeros(1, h, dim, dtype=dtype, device="cuda")  # noqa: E731
+        k, v, q = (x.clone().transpose(0, 1) if flip else x.transpose(0, 1).clone(memory_format=torch.contiguous_format) for x in rows)
+        assert q.stride(0) == (dim if flip else heads * dim)
+        cache = PagedCache(1, 2, 32, kv, dim, 1, 2, dtype=dtype, format=fmt)
+        cache.resize(i32([0]), i32([3]))
+        att = BlockAttention(cache, heads, 1, 1, 1, rope=rope)
+        att.begin(i32([0, 1]))
+        q_out, out, k_out, v_out, turned = new(heads), new(heads), new(kv), new(kv), new(heads)
+        att.append(0, k, v, q, q_out)
+        att.plan()
+        att.attend(0, q_out, out)
+        cache.read(0, i32([0, 1]), k_out, v_out)
+        rope.apply(q, i32([7]), turned)
+        got.append((cache.k, cache.v, q_out, out, att.attend(0, q_out), k_out, v_out, turned))
+    assert all(bool((x != 0).any()) and torch.equal(x, y) for x, y in zip(*got))
