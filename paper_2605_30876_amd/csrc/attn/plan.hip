@@ -4,6 +4,8 @@
 // 5.4 us for one sequence, 6.6 for 64: half of it the launch, the rest three
 // round trips (offsets and slots, lengths, page ids) and the barriers; 1024
 // threads took 2.7 more.
+#include <algorithm>
+
 #include "cache.h"
 
 namespace dmoe {
@@ -27,7 +29,7 @@ constexpr int kSplitWide = 256;   // items of eight waves: one a CU
 // Their key tiles: one or two a wave (a block over 4096 tokens, eight layers: 118.7 us with 12, 121.5 with 10, 122.7 with 16), but
 // up to kWholeEight stay with one (a block over 400: 20.0 us in two pieces, which have to be joined, 17.1 in one).
 constexpr int kMinEight = 12, kWholeEight = 20;
-constexpr long kFew32 = 128, kFewTiles32 = 128, kFewKeys32 = 20000, kFewWork32 = 28000;
+constexpr long kFewTiles32 = 128, kFewKeys32 = 20000, kFewWork32 = 28000;
 constexpr long kFewTiles16 = 64, kFewKeys16 = 256;
 constexpr long kFewTiles = 16, kFewKeys = 2048;
 
@@ -226,7 +228,7 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
     const int parts = c.dt == DMOE_F32 ? 3 : 1, dp = padded_dim(c.head_dim);
     const bool few16 = tiles <= kFewTiles16 && keys >= kFewKeys16 && quant_rows_waves(parts, dp, key_bits(c.format) + value_bits(c.format), 16) == 2;
     const long work = tiles * dp * parts;
-    if (most <= 16 ? few16 : most <= 64 || (s.max_tiles <= kFew32 && tiles <= kFewTiles32 && work <= kFewWork32 && tiles * keys <= kFewKeys32)) {
+    if (most <= 16 ? few16 : most <= 64 || (tiles <= kFewTiles32 && work <= kFewWork32 && tiles * keys <= kFewKeys32)) {
       s.wide = true;
       s.aim = kSplitWide / c.n_kv_heads > 1 ? kSplitWide / c.n_kv_heads : 1;
       s.split_items = 2 * s.aim;
@@ -267,7 +269,7 @@ size_t plan_ints(int n_seqs, int T, int max_new, int n_heads, int n_kv_heads) {
   }
   // 32 rows to an item also where there are more of them, but few (attn_shape)
   AttnShape few = shape_of(32, n_seqs, T, max_new, n_heads, n_kv_heads);
-  if (few.max_tiles > kFew32) few.max_tiles = kFew32;
+  few.max_tiles = std::min(few.max_tiles, kFewTiles32 / n_kv_heads);
   n = plan_ints(few) > n ? plan_ints(few) : n;
   return n;
 }
