@@ -617,7 +617,8 @@ dmoe_status dmoe_rope(const void* x, long x_stride, void* out, long out_stride, 
  * |element| is at most 464 (FP4: 7) times the scale; not below 17, and
  * not above 246 (252), where the largest codes reach bf16's range (elements beyond
  * become the largest code).  Codes are rounded to nearest, ties to the even
- * code.  A group with an element that is not finite has b = 255 and codes of 0: all of it is NaN.
+ * code.  A group with an element that is not finite has b = 255 and codes of 0: all of it is NaN.  In arrays that come from
+ * elsewhere every other byte means 2^(b - 127) too; a product that bf16 does not hold exactly is rounded to it.
  */
 typedef enum dmoe_kv_format {
   DMOE_KV_PLAIN = 0,

@@ -7,8 +7,11 @@
 // rows are contiguous and a quad's codes are one 16-byte chunk (or two) of the page.
 // Keys and values lie in the page alike, token by token, so nothing is turned.
 // Both ways are bound by memory: prompts of 11753 tokens (32 heads of 128 with queries, 8 of keys in 8 bits and values
-// in 4) are stored and read back in 73 us (326 MB, 4.5 TB/s), 48 sequences of 89,941 tokens and 8 heads read back from 4 bits in 101
-// us (466 MB, 4.6 TB/s), where a large copy reaches 5.2.  A block of 32 tokens is bound by its latency: 4.4 and 2.9 us.
+// in 4) are stored and read back in 73 us (326 MB, 4.5 TB/s), 48 sequences of 89,941 tokens and 8 heads read back from 4 bits in 104
+// us (466 MB, 4.5 TB/s), where a large copy reaches 5.2.  A block of 32 tokens is bound by its latency: 4.5 and 3.5 us alone, 7.0
+// together in a graph.  Further from the bytes: rotated halves in the store (Turn8), 90 us for prompts of 263 MB; rows of
+// float32 read from 4 bits, 336 for 743 MB; a plain cache's values, whose elements lie apart and are loaded one by one, with its
+// keys 330 for 972 MB of bf16, 549 for 2.1 GB of float32.
 #include "quant.h"
 #include "rotate.h"
 
@@ -40,7 +43,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 
 // Elements d .. d+7 of a head at x, f, rotated with the token's (cos, sin) of every pair: own cos -+ partner sin.  Queries
 // in float32, as rope.hip does; keys in binary64, rounded to float32 and from there to T: which of two codes a key next to
-// their border takes does not depend on how a product was summed.
+// their border takes does not depend on how a product was summed.  Halves cost more than adjacent pairs: the partners are loaded
+// again, and a lane holds eight angles instead of four (177 registers for bf16 against 95: two waves a SIMD, not five).
 enum Pairs { kNoPairs, kAdjacent, kHalves, kAnyHalves };  // kHalves: eight elements are of one half
 template <typename T, typename A, Pairs kPairs>
 struct Turn8 {

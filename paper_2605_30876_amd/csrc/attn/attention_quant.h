@@ -567,7 +567,7 @@ constexpr int rows_waves = quant_rows_waves(kParts<T>, DP, kKB + kVB, kR);
 // over 363,063 (32 and 8 heads of 128 in 4 bits, page 64; 396 MB) 85 us, 4.7 TB/s, of which 70 are left with
 // loads alone; one over 131,000 (143 MB) 35 us with plan and merge.  Loads further ahead, or a third wave of a SIMD: as
 // fast; through the caches 98.  Eight waves take 94 us for the 64, and win where there are few (attn_shape).  A block of 32 tokens over 4096, four kv heads of 32 rows by 4: a
-// chain of one load after another, 9.5 us where 7 TB/s would take 1.
+// chain of one load after another, 10 us where 7 TB/s would take 1.
 template <typename T, int DP, int kKB, int kVB, int kR, int kW>
 __global__ __launch_bounds__(64 * kW, (rows_waves<T, DP, kKB, kVB, kR>)) void quant_rows_kernel(AttnArgs a, QuantShape sh, int part_rows) {
   constexpr bool kPin = rows_waves<T, DP, kKB, kVB, kR> == 1;
@@ -721,9 +721,10 @@ constexpr int quant_waves(int dp) {
 // Many rows: 128 of one kv head per workgroup, 32 to a wave, all four waves on the same keys.  Codes of kTS tiles
 // are loaded two stages ahead, opened into LDS one stage ahead, each by one of the
 // threads; one barrier a stage.  Bound by matrix products and the exponentials between them: 4096 rows of 16 heads of 128
-// over 16384 keys in 4 bits, 525 us, 920 TFLOP/s (a library product 1210; a cache of bf16 490 us).  fp32 rows of 256
-// elements have no room for the queries' parts and spill 460 to 524 bytes a lane, which still beats 32
-// rows a workgroup: 1024 tokens over 4096 260 us, so 306.
+// over 16384 keys in 4 bits, 525 us, 920 TFLOP/s (a library product 1210; a cache of bf16 490 us); the first calls after a
+// pause take 570 to 650, until the clock has risen.  fp32 rows of 256 elements have no room for the queries' parts and spill 460
+// to 524 bytes a lane; so does the form of 32 rows (440 to 484), which took 303 us for 1024 tokens of 8 and 4 heads over 4096 where
+// this one took 258.
 template <typename T, int DP, int kKB, int kVB>
 __global__ __launch_bounds__(256, quant_waves<T>(DP)) void quant_block_kernel(AttnArgs a, QuantShape sh, int part_rows) {
   typedef QuantStage<DP> Stage;

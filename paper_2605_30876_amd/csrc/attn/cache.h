@@ -183,8 +183,12 @@ constexpr bool two_per_cu(dmoe_dtype dt, int dp) { return dp * (dt == DMOE_F32 ?
 // and in a cache of few bits, whose products are bf16 and whose fp32 queries take three registers for one
 constexpr bool quant_two_per_cu(dmoe_dtype dt, int dp) { return dp <= (dt == DMOE_F32 ? 64 : 128); }
 // Waves of a SIMD in the kernel of few rows of such a cache: two where a lane's queries (in so many bf16 parts), sums and codes leave
-// room for the rest in half of the registers.  64 single tokens of up to 16k, 16 and 4 heads of 256 in 4 bits: 86 us
-// with two, 103 with one; of up to 8k in 8 bits, which do not fit: 205 (spilled) and 96.  Three, where they fit, measured as two.
+// room for the rest in half of the registers, or nearly.  64 single tokens of up to 16k, 16 and 4 heads of 256 in 4 bits: 86 us
+// with two, 103 with one; of up to 8k in 8 bits, which are far from fitting: 205 (spilled) and 96.  Forms of 16 rows that spill some
+// bytes a lane with two, 64 tokens of up to 8k, 16 and 4 heads: fp32 192 elements in 4 bits (84 bytes) 78 us, 91 with one; with keys in 8 (80
+// bytes) 79 and 84; bf16 256 elements, keys in 8 and values in 4 (36 bytes), 72 and 75; a token over 16,000 31, 31 and 32 with
+// two, 31, 32 and 33 with one.  Three, where they fit, measured as two.  fp32, 256 elements, 32 rows do not fit one wave either: 440 to 484
+// bytes a lane spill.
 constexpr int quant_rows_waves(int parts, int dp, int bits, int rows) {
   return parts * dp * rows / 128 + dp * rows / 64 + dp * bits / 64 < 160 ? 2 : 1;
 }

@@ -221,6 +221,10 @@ AttnShape attn_shape(const dmoe_cache& c, const dmoe_batch& b, int n_heads) {
     // 3000 tokens, 32, 64, 96 row tiles: bf16 128 elements 21.3/22.8, 23.8/28.0, 26.6/30.5; 256 elements 27.9/31.6, 32.7/35.8,
     // 38.8/41.1, 128 of them 42.6/39.9; fp32 128 elements 26.4/29.0, 32.8/35.4, 38.8/38.7, 128 of them 44.1/38.8; 256 elements
     // 48.5/53.9, 70.5/68.1, 89.5/82.7.  16 tiles over 4096 tokens in 8 bits, a layer: 14.9/18.8; 256 over up to 8192: 39/33.
+    // `keys` is what the tables have room for (lengths are the device's), in these measurements hardly more than the sequences held.
+    // Where there is room for far more, few rows over short sequences get the form of long ones: one block of 32 tokens in 8 bits, 16
+    // and 4 heads of 128, a layer of eight, with room for just the sequence and for 131,072 tokens: over 400 10.3/12.9, 4096
+    // 14.8/18.7, 16,384 20.7/30.3; two blocks over 4096 16.6/23.0, four 20.7/26.4, eight 32.4/31.8.  One token: no difference.
     // 16 rows: to four waves, or to eight, which have half of the partial results to join but start later, where row tiles are few
     // and may be long.  us of four and of eight, 4 bits, 32 and 8 heads of 128, in a graph: one token over 1000 keys 19.4/20.3, 4096
     // 20.5/20.9, 16,000 25.3/23.2, 32,000 28.5/26.3, 131,000 38.8/36.8 (not a graph); 8 over 8192 22.7/21.8, 16 32.6/33.9; 16 and 4
